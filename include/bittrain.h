@@ -71,7 +71,7 @@ enum {
     BT_ERR_TIMEOUT = 6,    /* device: a bounded wait inside the kernel ran out         */
     BT_ERR_CUDA = 7,       /* the CUDA runtime reported an error at launch             */
     BT_ERR_TOO_LARGE = 8,  /* n exceeds what the call can handle (bt_compress_noalloc) */
-    BT_ERR_SHAPE = 9       /* a dimension the call cannot take (bt_maxpool2x2_*: odd or zero) */
+    BT_ERR_SHAPE = 9       /* a dimension the call cannot take (bt_maxpool2x2_*: odd or zero), or a setting */
 };
 
 /* ======================================================================================
@@ -526,6 +526,106 @@ int bt_relu_fwd_compress_host(const void *host_pre_act, uint64_t n, int dtype, v
 int bt_relu_bwd_from_bitmap_host(const uint32_t *host_bitmap, const void *host_grad_out,
                                  uint64_t n, int dtype, void *host_grad_in,
                                  void *dev_staging, size_t dev_staging_bytes, void *stream);
+
+/* ======================================================================================
+ * Operators of a transformer block's training step.  (No counterpart in the paper, whose models are
+ * convolutional: the gated feed-forward block is where such a model's sparse activations arise, the norms stand
+ * around it, and the clipping ends the step.)  General rules as above: flat row-major tensors of one
+ * element type per call, sums in binary32 (BT_F64: binary64), every output rounded once.
+ * ====================================================================================== */
+
+/* activations of the gated feed-forward block; GELU_TANH is the tanh approximation of GELU */
+enum { BT_ACT_RELU = 0, BT_ACT_SILU = 1, BT_ACT_GELU = 2, BT_ACT_GELU_TANH = 3 };
+
+/*
+ * Gated feed-forward block, both projections, the activation and the product in one kernel:
+ *   g = x w_gate^T,  u = x w_up^T,  h = act(g) * u
+ * x is rows x d_in, w_gate and w_up are d_ff x d_in, h is rows x d_ff.  For a backward pass g_out and u_out
+ * (rows x d_ff, each may be NULL) receive what bt_glu_bwd reads: g -- with BT_ACT_RELU max(g, 0), as sparse as
+ * h, so that bt_compress and bt_mask_compress can stash both under one bitmap -- and u.  No output may overlap
+ * an input or another output.  workspace_bytes >= bt_glu_workspace_bytes(rows, d_in, d_ff, dtype, 0); the
+ * workspace may be NULL where that is 0, its contents need no initialisation, and calls that run concurrently
+ * must not share it.  *dev_status (may be NULL): BT_OK, or BT_ERR_TIMEOUT if a bounded wait inside a kernel
+ * ran out (every output is then undefined; the context stays usable).  rows == 0 touches *dev_status alone;
+ * d_in and d_ff are at least 1 (BT_ERR_SHAPE) and at most 2^24, rows below 2^31 (BT_ERR_TOO_LARGE).  An
+ * unknown activation is BT_ERR_SHAPE.
+ */
+size_t bt_glu_workspace_bytes(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, int backward);
+
+int bt_glu_fwd(const void *x, uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, int activation,
+               const void *w_gate, const void *w_up, void *h, void *g_out, void *u_out, void *workspace,
+               size_t workspace_bytes, int32_t *dev_status, void *stream);
+
+/*
+ * Its gradients from the stored g and u (as bt_glu_fwd wrote them) and grad_h (rows x d_ff):
+ *   du = grad_h * act(g),  dg = grad_h * u * act'(g)     (both rounded to the element type)
+ *   grad_x = dg w_gate + du w_up,  grad_w_gate = dg^T x,  grad_w_up = du^T x
+ * With BT_ACT_RELU a closed gate's dg and du are +0 whatever grad_h and u hold there.  grad_x may be NULL, or
+ * grad_w_gate and grad_w_up both; what only the missing output needs (the weights, or x) may then be NULL too.
+ * rows == 0 sets the weights' gradients to +0.  workspace_bytes >= bt_glu_workspace_bytes(.., 1).  Other
+ * parameters and limits as bt_glu_fwd.
+ */
+int bt_glu_bwd(const void *grad_h, uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, int activation,
+               const void *g, const void *u, const void *x, const void *w_gate, const void *w_up, void *grad_x,
+               void *grad_w_gate, void *grad_w_up, void *workspace, size_t workspace_bytes,
+               int32_t *dev_status, void *stream);
+
+/*
+ * The norms around a block, its gate and the scale of its residual sum, in one pass over rows x d elements:
+ *   p     = w_post ? rms(f) * w_post : f          rms(v) = v / sqrt(mean(v^2) + eps), row by row
+ *   x_out = x + scale * gate * p
+ *   n_out = rms(x_out) * w_pre                    (of the sum before it is rounded to the element type)
+ * f: the block's output; NULL for the first norm of a network (then gate, w_post and x_out are NULL too and
+ * n_out = rms(x) * w_pre).  gate: NULL, or ceil(rows / gate_rows) rows of d elements, one for gate_rows consecutive
+ * rows (gate_rows = rows: a gate per channel; 1: a gate per row; >= 1 in any case).  w_pre and n_out: both or
+ * neither.  x_out may alias x, and n_out may alias f; no other buffers may overlap.
+ * rows == 0 does nothing.  d >= 1, eps >= 0, scale not a NaN (BT_ERR_SHAPE); d <= 2^24, rows * d <= 2^40
+ * (BT_ERR_TOO_LARGE).
+ */
+int bt_block_norm_fwd(const void *x, uint64_t rows, uint64_t d, uint64_t gate_rows, int dtype, float scale, float eps,
+                      const void *f, const void *gate, const void *w_post, const void *w_pre,
+                      void *x_out, void *n_out, void *stream);
+
+/*
+ * Its gradients, from x_out as the forward pass wrote it (without f: from x), f, the weights and the gradients of n_out
+ * (grad_n, with w_pre or not at all) and of x_out (grad_x_out; may be NULL if grad_n is given): grad_x (also the
+ * gradient of the residual stream), grad_f, grad_gate (the gate's shape), grad_w_post and grad_w_pre (d elements).
+ * Any output may be NULL; no output may overlap an input.  The sums over rows are added in a fixed order.  workspace_bytes >=
+ * bt_block_norm_workspace_bytes(rows, d, dtype) (asked with the same device current), contents as for
+ * bt_glu_fwd; it may be NULL where neither grad_gate nor a weight's gradient is wanted and a row has at most
+ * 1024 16-byte vectors (d a multiple of a vector) or 4096 elements.  rows == 0 sets the weights' gradients to +0.
+ */
+size_t bt_block_norm_workspace_bytes(uint64_t rows, uint64_t d, int dtype);
+
+int bt_block_norm_bwd(const void *x_out, uint64_t rows, uint64_t d, uint64_t gate_rows, int dtype, float scale, float eps,
+                      const void *f, const void *gate, const void *w_post, const void *w_pre,
+                      const void *grad_n, const void *grad_x_out, void *grad_x, void *grad_f, void *grad_gate,
+                      void *grad_w_post, void *grad_w_pre, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Norm and clipping of a step's gradients: `count` tensors of one element type (items[k].dense, items[k].n elements;
+ * the batch's other fields but y_out are ignored), any count, at most 1024 non-empty tensors per launch.
+ *   bt_grad_norm_batch    *sumsq = (accumulate ? *sumsq : 0) + sum of all squares (binary64, device; may be NULL without
+ *                         accumulate), *norm_out = sqrt(*sumsq) (binary32, device; may be NULL if sumsq is given)
+ *   bt_grad_scale_batch   y_out = c * dense, c = min(1, max_norm / (sqrt(*sumsq) + 1e-6)); y_out may alias dense
+ *   bt_grad_clip_batch    both in two launches: the norm of these tensors and their products; *norm_out may be NULL
+ * The first two serve a step whose gradients have several element types (accumulate over the types, then scale
+ * each).  Squares are exact or rounded to binary32, sums are binary64 in a fixed order; a gradient of any finite
+ * magnitude counts.  c is rounded to binary32 (BT_F64: binary64) and each product once.  An infinite norm
+ * gives c = 0, a NaN makes every gradient a NaN.  In place, c == 1 leaves the tensors unread and unwritten.  max_norm
+ * >= 0, not a NaN (BT_ERR_SHAPE).  Tensors of one call must not overlap (the same tensor twice would be scaled twice).
+ * items[k].n <= 2^46 (BT_ERR_TOO_LARGE).  workspace_bytes >= bt_grad_workspace_bytes(n of every item, count).
+ */
+size_t bt_grad_workspace_bytes(const uint64_t *n /* host */, uint32_t count);
+
+int bt_grad_norm_batch(const bt_batch_item *items /* host */, uint32_t count, int dtype, int accumulate,
+                       double *sumsq, float *norm_out, void *workspace, size_t workspace_bytes, void *stream);
+
+int bt_grad_scale_batch(const bt_batch_item *items /* host */, uint32_t count, int dtype, float max_norm,
+                        const double *sumsq, void *stream);
+
+int bt_grad_clip_batch(const bt_batch_item *items /* host */, uint32_t count, int dtype, float max_norm,
+                       float *norm_out, void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

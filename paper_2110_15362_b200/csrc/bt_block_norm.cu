@@ -1,0 +1,775 @@
+// The norms around a block of a residual network, with the block's gate and the scale of its residual sum:
+//
+//   p  = w_post ? rms(f) * w_post : f            rms(v) = v / sqrt(mean v^2 + eps)
+//   x' = x + scale * gate * p                    (gate: one row for gate_rows consecutive rows)
+//   n  = rms(x') * w_pre
+//
+// and their gradients.  Bound by HBM: the forward pass reads x and f and writes x' and n, the backward pass reads x', f, dn
+// and dx' and writes dx and df; weights and gate stay in the caches.  A row is read once and kept in registers between its
+// sums and its outputs; only rows longer than a CTA's registers are read again (from the caches).
+//
+// Backward: with r, rf the two norms' factors, q = scale * gate * w_post * f and wn = dn * w_pre,
+//
+//   t  = dx' + r wn - r^2 c x'   (= dx),   c  = r mean(wn x')
+//   df = scale gate w_post rf t - rf^3 mean(t q) f,   mean(t q) = mean(dx' q) + r mean(wn q) - r^2 c mean(x' q)
+//
+// so that one reduction of six sums per row serves both norms.  The sums over rows (w_pre, w_post, gate) are held in
+// binary32 by the threads that own the columns, one partial row per CTA (gate: per chunk of rows), and added up in a fixed
+// order by a second kernel: no atomics, the same bits every time.
+#include "bt_numeric.cuh"
+
+namespace bt {
+namespace {
+
+struct NormArgs {
+    const void *x, *f, *gate, *w_post, *w_pre;     // backward: x is x'
+    const void *dn, *dy;                           // backward: gradients of n and of x' (either may be NULL)
+    void       *x_out, *n_out;                     // forward; backward: dx, df
+    void       *dgate, *dw_post, *dw_pre;          // backward
+    float      *part_pre, *part_post, *part_gate;  // backward: partial rows (double where sums are)
+    void       *stats;                             // backward, long rows: r, c, rf, mean(t q) of each row
+    uint64_t    rows, d, gate_rows, chunk_rows;    // chunk_rows: consecutive rows of one team
+    uint32_t    chunks;
+    double      scale, eps;
+};
+
+constexpr int      kMaxTeam   = 512;                                    // threads of a CTA that takes a row
+constexpr int      kMaxWarps  = kMaxTeam / 32;
+constexpr uint32_t kWarpTeams = 4;                                      // warps of a CTA whose teams are warps
+
+// kVector: 16-byte accesses, else single elements (rows that do not all begin on a 16-byte boundary)
+template <int DT, bool kVector>
+struct Access {
+    using Elem              = typename Num<DT>::Elem;
+    using Acc               = typename Num<DT>::Acc;
+    static constexpr int kW = kVector ? kLanes<DT> : 1;
+    using Raw               = typename std::conditional<kVector, uint4, Elem>::type;
+    __device__ static __forceinline__ Raw load(const void *row, const uint32_t i)
+    {
+        return static_cast<const Raw *>(row)[i];
+    }
+    __device__ static __forceinline__ void widen(const Raw &w, Acc (&v)[kW])
+    {
+        if constexpr (kVector) widen_vec<DT>(w, v);
+        else v[0] = Num<DT>::widen(w);
+    }
+    __device__ static __forceinline__ void read(const void *row, const uint32_t i, Acc (&v)[kW]) { widen(load(row, i), v); }
+    // weights and gates, which no output overlaps
+    __device__ static __forceinline__ void read_shared(const void *row, const uint32_t i, Acc (&v)[kW])
+    {
+        widen(__ldg(static_cast<const Raw *>(row) + i), v);
+    }
+    __device__ static __forceinline__ void store(void *row, const uint32_t i, const Acc (&v)[kW], const Extent &e)
+    {
+        Raw *const p = static_cast<Raw *>(row) + i;
+        if (!e.holds(p, sizeof(Raw))) return;
+        if constexpr (kVector) *p = narrow_vec<DT>(v);
+        else *p = Num<DT>::narrow(v[0]);
+    }
+};
+
+template <typename Elem>
+__device__ __forceinline__ const void *row_of(const void *base, const uint64_t row, const uint64_t d)
+{
+    return base ? static_cast<const void *>(static_cast<const Elem *>(base) + row * d) : nullptr;
+}
+template <typename Elem>
+__device__ __forceinline__ void *row_of(void *base, const uint64_t row, const uint64_t d)
+{
+    return base ? static_cast<void *>(static_cast<Elem *>(base) + row * d) : nullptr;
+}
+
+__device__ __forceinline__ float  root_of(float v) { return rsqrtf(v); }
+__device__ __forceinline__ double root_of(double v) { return rsqrt(v); }
+
+// The sums of a team: a warp, or (kCta) the CTA.  `turn` alternates between two sets of words, so that one barrier serves a
+// reduction: words are written again only behind the barrier of the reduction in between.
+template <bool kCta, int kSums, typename A>
+__device__ __forceinline__ void team_sums(A (&s)[kSums], A (*words)[kSums][kMaxWarps], uint32_t &turn)
+{
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) s[k] = warp_sum(s[k]);
+    if constexpr (kCta) {
+        const uint32_t warps = blockDim.x / 32;
+        A (&w)[kSums][kMaxWarps] = words[turn & 1];
+        ++turn;
+        if (threadIdx.x % 32 == 0) {
+#pragma unroll
+            for (int k = 0; k < kSums; ++k) w[k][threadIdx.x / 32] = s[k];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < kSums; ++k) {
+            const A v = threadIdx.x % 32 < warps ? w[k][threadIdx.x % 32] : A(0);
+            s[k]      = warp_sum(v);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- forward
+// kHold accesses of each of x and f per thread; 0: rows of any length, read again for each use.
+template <int DT, bool kVector, int kHold, bool kCta>
+__global__ void __launch_bounds__(kCta ? kMaxTeam : 32 * kWarpTeams)
+block_norm_fwd_kernel(const NormArgs a)
+{
+    in_stream_order();
+    using X                = Access<DT, kVector>;
+    using Elem             = typename X::Elem;
+    using Acc              = typename X::Acc;
+    constexpr int  kW      = X::kW;
+    __shared__ Acc words[2][1][kMaxWarps];
+    uint32_t       turn    = 0;
+    const uint32_t team    = kCta ? blockDim.x : 32;
+    const uint32_t t       = kCta ? threadIdx.x : threadIdx.x % 32;
+    const uint32_t count   = static_cast<uint32_t>(a.d / kW);
+    const Acc      scale = static_cast<Acc>(a.scale), eps = static_cast<Acc>(a.eps), of_d = Acc(1) / static_cast<Acc>(a.d);
+    const uint64_t first   = kCta ? blockIdx.x : static_cast<uint64_t>(blockIdx.x) * (blockDim.x / 32) + threadIdx.x / 32;
+    const uint64_t step    = kCta ? gridDim.x : static_cast<uint64_t>(gridDim.x) * (blockDim.x / 32);
+    const Extent   all_x = extent_of(a.x_out, a.rows * a.d * sizeof(Elem)), all_n = extent_of(a.n_out, a.rows * a.d * sizeof(Elem));
+    for (uint64_t row = first; row < a.rows; row += step) {
+        const void *x = row_of<Elem>(a.x, row, a.d), *f = row_of<Elem>(a.f, row, a.d);
+        const void *gate = a.gate ? row_of<Elem>(a.gate, row / a.gate_rows, a.d) : nullptr;
+        void       *x_out = row_of<Elem>(a.x_out, row, a.d), *n_out = row_of<Elem>(a.n_out, row, a.d);
+        if constexpr (kHold > 0) {
+            Acc v[kHold][kW];
+            if (f) {
+                Acc fv[kHold][kW], s[1] = {0};
+#pragma unroll
+                for (int j = 0; j < kHold; ++j)
+                    if (j * team + t < count) {
+                        X::read(f, j * team + t, fv[j]);
+                        X::read(x, j * team + t, v[j]);
+                    }
+                Acc rf = 1;
+                if (a.w_post) {
+#pragma unroll
+                    for (int j = 0; j < kHold; ++j)
+                        if (j * team + t < count) {
+#pragma unroll
+                            for (int k = 0; k < kW; ++k) s[0] += fv[j][k] * fv[j][k];
+                        }
+                    team_sums<kCta>(s, words, turn);
+                    rf = root_of(s[0] * of_d + eps);
+                }
+                rf *= scale;
+#pragma unroll
+                for (int j = 0; j < kHold; ++j)
+                    if (j * team + t < count) {
+                        Acc w[kW];
+#pragma unroll
+                        for (int k = 0; k < kW; ++k) fv[j][k] *= rf;
+                        if (a.w_post) {
+                            X::read_shared(a.w_post, j * team + t, w);
+#pragma unroll
+                            for (int k = 0; k < kW; ++k) fv[j][k] *= w[k];
+                        }
+                        if (gate) {
+                            X::read_shared(gate, j * team + t, w);
+#pragma unroll
+                            for (int k = 0; k < kW; ++k) fv[j][k] *= w[k];
+                        }
+#pragma unroll
+                        for (int k = 0; k < kW; ++k) v[j][k] += fv[j][k];
+                        X::store(x_out, j * team + t, v[j], all_x);
+                    }
+            } else {
+#pragma unroll
+                for (int j = 0; j < kHold; ++j)
+                    if (j * team + t < count) X::read(x, j * team + t, v[j]);
+            }
+            if (!n_out) continue;
+            Acc s[1] = {0};
+#pragma unroll
+            for (int j = 0; j < kHold; ++j)
+                if (j * team + t < count) {
+#pragma unroll
+                    for (int k = 0; k < kW; ++k) s[0] += v[j][k] * v[j][k];
+                }
+            team_sums<kCta>(s, words, turn);
+            const Acc r = root_of(s[0] * of_d + eps);
+#pragma unroll
+            for (int j = 0; j < kHold; ++j)
+                if (j * team + t < count) {
+                    Acc w[kW];
+                    X::read_shared(a.w_pre, j * team + t, w);
+#pragma unroll
+                    for (int k = 0; k < kW; ++k) v[j][k] = v[j][k] * r * w[k];
+                    X::store(n_out, j * team + t, v[j], all_n);
+                }
+        } else {
+            Acc rf = 1;
+            if (f && a.w_post) {
+                Acc s[1] = {0};
+                for (uint32_t i = t; i < count; i += team) {
+                    Acc w[kW];
+                    X::read(f, i, w);
+#pragma unroll
+                    for (int k = 0; k < kW; ++k) s[0] += w[k] * w[k];
+                }
+                team_sums<kCta>(s, words, turn);
+                rf = root_of(s[0] * of_d + eps);
+            }
+            rf *= scale;
+            const auto sum_at = [&](const uint32_t i, Acc (&v)[kW]) {
+                X::read(x, i, v);
+                if (!f) return;
+                Acc p[kW], w[kW];
+                X::read(f, i, p);
+#pragma unroll
+                for (int k = 0; k < kW; ++k) p[k] *= rf;
+                if (a.w_post) {
+                    X::read_shared(a.w_post, i, w);
+#pragma unroll
+                    for (int k = 0; k < kW; ++k) p[k] *= w[k];
+                }
+                if (gate) {
+                    X::read_shared(gate, i, w);
+#pragma unroll
+                    for (int k = 0; k < kW; ++k) p[k] *= w[k];
+                }
+#pragma unroll
+                for (int k = 0; k < kW; ++k) v[k] += p[k];
+            };
+            Acc r = 0;
+            if (n_out) {
+                Acc s[1] = {0};
+                for (uint32_t i = t; i < count; i += team) {
+                    Acc v[kW];
+                    sum_at(i, v);
+#pragma unroll
+                    for (int k = 0; k < kW; ++k) s[0] += v[k] * v[k];
+                }
+                team_sums<kCta>(s, words, turn);
+                r = root_of(s[0] * of_d + eps);
+            }
+            for (uint32_t i = t; i < count; i += team) {
+                Acc v[kW], w[kW];
+                sum_at(i, v);
+                if (f) X::store(x_out, i, v, all_x);
+                if (!n_out) continue;
+                X::read_shared(a.w_pre, i, w);
+#pragma unroll
+                for (int k = 0; k < kW; ++k) v[k] = v[k] * r * w[k];
+                X::store(n_out, i, v, all_n);
+            }
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------- backward
+// What a row's outputs need besides its elements.
+template <typename Acc>
+struct RowFactors {
+    Acc r, rrc;      // dn's factor; r^2 c
+    Acc rf, rf3m;    // df's factor; rf^3 mean(t q)
+};
+template <typename Acc>
+__device__ __forceinline__ RowFactors<Acc> factors_of(const Acc (&s)[6], const Acc of_d, const Acc eps, const bool post)
+{
+    RowFactors<Acc> q;
+    q.r            = root_of(s[0] * of_d + eps);
+    q.rrc          = q.r * q.r * (q.r * (s[1] * of_d));
+    q.rf           = post ? root_of(s[2] * of_d + eps) : Acc(1);
+    const Acc mean = (s[3] + q.r * s[4] - q.rrc * s[5]) * of_d;
+    q.rf3m         = post ? q.rf * q.rf * q.rf * mean : Acc(0);
+    return q;
+}
+
+// one element's share of a row's six sums: x', f, dx', wn = dn w_pre and gw = scale gate w_post
+template <typename Acc>
+__device__ __forceinline__ void add_sums(Acc (&s)[6], const Acc x, const Acc f, const Acc dy, const Acc wn, const Acc gw)
+{
+    const Acc q = gw * f;
+    s[0] += x * x;
+    s[1] += wn * x;
+    s[2] += f * f;
+    s[3] += dy * q;
+    s[4] += wn * q;
+    s[5] += x * q;
+}
+
+// The chunk of rows of a team, and the groups of rows (with a gate row each) that it meets: a group that lies inside one chunk
+// has its gradient written at once; of one that crosses chunks every chunk leaves a partial row -- where the group begins in
+// the chunk in slot 2 * chunk + 1, where it came from the chunk before in slot 2 * chunk.
+struct Chunk {
+    uint64_t first, end;
+};
+__device__ __forceinline__ Chunk chunk_of(const NormArgs &a, const uint32_t chunk)
+{
+    Chunk c;
+    c.first = chunk * a.chunk_rows;
+    c.end   = c.first + a.chunk_rows < a.rows ? c.first + a.chunk_rows : a.rows;
+    return c;
+}
+// where the sum over the rows [.., row] of a chunk's last group goes: true if it is whole
+__device__ __forceinline__ bool whole_group(const NormArgs &a, const Chunk &c, const uint64_t group, const uint32_t chunk, uint64_t &slot)
+{
+    const uint64_t begin = group * a.gate_rows, end = begin + a.gate_rows < a.rows ? begin + a.gate_rows : a.rows;
+    slot = 2ull * chunk + (begin >= c.first ? 1 : 0);
+    return begin >= c.first && end <= c.end;
+}
+
+// kHold accesses of every operand per thread, held in registers with the column sums.
+template <int DT, bool kVector, int kHold, bool kCta>
+__global__ void __launch_bounds__(kCta ? kMaxTeam : 32 * kWarpTeams)
+block_norm_bwd_kernel(const NormArgs a)
+{
+    in_stream_order();
+    using X                = Access<DT, kVector>;
+    using Elem             = typename X::Elem;
+    using Acc              = typename X::Acc;
+    constexpr int  kW      = X::kW;
+    __shared__ Acc words[2][6][kMaxWarps];
+    uint32_t       turn    = 0;
+    const uint32_t team    = kCta ? blockDim.x : 32;
+    const uint32_t t       = kCta ? threadIdx.x : threadIdx.x % 32;
+    const uint32_t chunk   = kCta ? blockIdx.x : blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32;
+    const uint32_t count   = static_cast<uint32_t>(a.d / kW);
+    const Acc      scale = static_cast<Acc>(a.scale), eps = static_cast<Acc>(a.eps), of_d = Acc(1) / static_cast<Acc>(a.d);
+    const uint64_t bytes = a.rows * a.d * sizeof(Elem);
+    const Extent   all_x = extent_of(a.x_out, bytes), all_f = extent_of(a.n_out, bytes);
+    const Extent   all_g = extent_of(a.dgate, round_up_div(a.rows, a.gate_rows) * a.d * sizeof(Elem));
+    const Extent   part_g = extent_of(a.part_gate, 2ull * a.chunks * a.d * sizeof(Acc));
+    const Extent   part_w = extent_of(a.part_pre, a.chunks * a.d * sizeof(Acc)), part_p = extent_of(a.part_post, a.chunks * a.d * sizeof(Acc));
+    if (chunk >= a.chunks) return;                                     // (a whole team; a CTA team is a CTA)
+    const Chunk c = chunk_of(a, chunk);
+    Acc         sum_pre[kHold][kW] = {}, sum_post[kHold][kW] = {}, sum_gate[kHold][kW] = {};
+    for (uint64_t row = c.first; row < c.end; ++row) {
+        const void *x = row_of<Elem>(a.x, row, a.d), *f = row_of<Elem>(a.f, row, a.d);
+        const void *dn = row_of<Elem>(a.dn, row, a.d), *dy = row_of<Elem>(a.dy, row, a.d);
+        const uint64_t group = row / a.gate_rows;
+        const void    *gate  = a.gate ? row_of<Elem>(a.gate, group, a.d) : nullptr;
+        // the operands wait in registers as they lie in memory; weights and gate are read again from the L1
+        typename X::Raw xr[kHold], fr[kHold], nr[kHold], yr[kHold];
+        Acc             s[6] = {};
+#pragma unroll
+        for (int j = 0; j < kHold; ++j) {
+            const uint32_t i = j * team + t;
+            if (i >= count) continue;
+            xr[j] = X::load(x, i);
+            if (f) fr[j] = X::load(f, i);
+            if (dn) nr[j] = X::load(dn, i);
+            if (dy) yr[j] = X::load(dy, i);
+        }
+        // element values of access j: x', f, dx', dn, w_pre, scale * gate, w_post
+        const auto element = [&](const int j, Acc (&xv)[kW], Acc (&fv)[kW], Acc (&dyv)[kW], Acc (&dnv)[kW], Acc (&wpre)[kW], Acc (&gw)[kW], Acc (&pw)[kW]) {
+            const uint32_t i = j * team + t;
+#pragma unroll
+            for (int k = 0; k < kW; ++k) fv[k] = dnv[k] = dyv[k] = 0, wpre[k] = pw[k] = gw[k] = 1;
+            X::widen(xr[j], xv);
+            if (f) X::widen(fr[j], fv);
+            if (dn) X::widen(nr[j], dnv), X::read_shared(a.w_pre, i, wpre);
+            if (dy) X::widen(yr[j], dyv);
+            if (a.w_post) X::read_shared(a.w_post, i, pw);
+            if (gate) X::read_shared(gate, i, gw);
+#pragma unroll
+            for (int k = 0; k < kW; ++k) gw[k] *= scale;
+        };
+#pragma unroll
+        for (int j = 0; j < kHold; ++j) {
+            if (j * team + t >= count) continue;
+            Acc xv[kW], fv[kW], dyv[kW], dnv[kW], wpre[kW], gw[kW], pw[kW];
+            element(j, xv, fv, dyv, dnv, wpre, gw, pw);
+#pragma unroll
+            for (int k = 0; k < kW; ++k) add_sums(s, xv[k], fv[k], dyv[k], dnv[k] * wpre[k], gw[k] * pw[k]);
+        }
+        team_sums<kCta>(s, words, turn);
+        const RowFactors<Acc> q = factors_of(s, of_d, eps, a.w_post != nullptr);
+        void *dx = row_of<Elem>(a.x_out, row, a.d), *df = row_of<Elem>(a.n_out, row, a.d);
+#pragma unroll
+        for (int j = 0; j < kHold; ++j) {
+            const uint32_t i = j * team + t;
+            if (i >= count) continue;
+            Acc xv[kW], fv[kW], dyv[kW], dnv[kW], wpre[kW], gw[kW], pw[kW];
+            element(j, xv, fv, dyv, dnv, wpre, gw, pw);
+#pragma unroll
+            for (int k = 0; k < kW; ++k) {
+                const Acc tv = dyv[k] + q.r * (dnv[k] * wpre[k]) - q.rrc * xv[k];
+                sum_pre[j][k] += dnv[k] * (xv[k] * q.r);
+                const Acc fh = fv[k] * q.rf, dp = tv * gw[k];
+                sum_gate[j][k] += scale * tv * (fh * pw[k]);
+                sum_post[j][k] += dp * fh;
+                fv[k]  = dp * pw[k] * q.rf - q.rf3m * fv[k];
+                dyv[k] = tv;
+            }
+            if (dx) X::store(dx, i, dyv, all_x);
+            if (df) X::store(df, i, fv, all_f);
+        }
+        // the last of the group's rows in this chunk: its gate's gradient, or this chunk's share of it
+        if (a.dgate && (row + 1 == c.end || (row + 1) % a.gate_rows == 0)) {
+            uint64_t   slot;
+            const bool whole = whole_group(a, c, group, chunk, slot);
+#pragma unroll
+            for (int j = 0; j < kHold; ++j) {
+                const uint32_t i = j * team + t;
+                if (i < count) {
+                    if (whole) X::store(row_of<Elem>(a.dgate, group, a.d), i, sum_gate[j], all_g);
+                    else
+#pragma unroll
+                        for (int k = 0; k < kW; ++k) {
+                            Acc *const o = reinterpret_cast<Acc *>(a.part_gate) + slot * a.d + i * kW + k;
+                            if (part_g.holds(o, sizeof(Acc))) *o = sum_gate[j][k];
+                        }
+                }
+#pragma unroll
+                for (int k = 0; k < kW; ++k) sum_gate[j][k] = 0;
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < kHold; ++j) {
+        const uint32_t i = j * team + t;
+        if (i >= count) continue;
+#pragma unroll
+        for (int k = 0; k < kW; ++k) {
+            const uint64_t o = chunk * a.d + i * kW + k;
+            if (a.dw_pre && part_w.holds(reinterpret_cast<Acc *>(a.part_pre) + o, sizeof(Acc))) reinterpret_cast<Acc *>(a.part_pre)[o] = sum_pre[j][k];
+            if (a.dw_post && part_p.holds(reinterpret_cast<Acc *>(a.part_post) + o, sizeof(Acc))) reinterpret_cast<Acc *>(a.part_post)[o] = sum_post[j][k];
+        }
+    }
+}
+
+// Rows longer than a CTA's registers: dx and df by a kernel that reads a row twice and leaves its factors behind ...
+template <int DT>
+__global__ void __launch_bounds__(kMaxTeam)
+block_norm_bwd_rows_kernel(const NormArgs a)
+{
+    in_stream_order();
+    using X    = Access<DT, false>;
+    using Elem = typename X::Elem;
+    using Acc  = typename X::Acc;
+    __shared__ Acc words[2][6][kMaxWarps];
+    uint32_t       turn = 0;
+    const Acc      scale = static_cast<Acc>(a.scale), eps = static_cast<Acc>(a.eps), of_d = Acc(1) / static_cast<Acc>(a.d);
+    const uint64_t bytes = a.rows * a.d * sizeof(Elem);
+    const Extent   all_x = extent_of(a.x_out, bytes), all_f = extent_of(a.n_out, bytes), all_s = extent_of(a.stats, a.rows * sizeof(RowFactors<Acc>));
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const Elem *x = static_cast<const Elem *>(a.x) + row * a.d, *gate = static_cast<const Elem *>(row_of<Elem>(a.gate, row / a.gate_rows, a.d));
+        const Elem *f = static_cast<const Elem *>(row_of<Elem>(a.f, row, a.d)), *dn = static_cast<const Elem *>(row_of<Elem>(a.dn, row, a.d));
+        const Elem *dy = static_cast<const Elem *>(row_of<Elem>(a.dy, row, a.d));
+        const Elem *w_pre = static_cast<const Elem *>(a.w_pre), *w_post = static_cast<const Elem *>(a.w_post);
+        const auto  at = [](const Elem *p, const uint64_t i, const Acc none) { return p ? static_cast<Acc>(Num<DT>::widen(p[i])) : none; };
+        Acc         s[6] = {};
+        for (uint64_t i = threadIdx.x; i < a.d; i += blockDim.x)
+            add_sums(s, at(x, i, 0), at(f, i, 0), at(dy, i, 0), dn ? at(dn, i, 0) * at(w_pre, i, 1) : Acc(0), scale * at(gate, i, 1) * at(w_post, i, 1));
+        team_sums<true>(s, words, turn);
+        const RowFactors<Acc> q = factors_of(s, of_d, eps, w_post != nullptr);
+        if (threadIdx.x == 0 && all_s.holds(static_cast<RowFactors<Acc> *>(a.stats) + row, sizeof(q))) static_cast<RowFactors<Acc> *>(a.stats)[row] = q;
+        void *dx = row_of<Elem>(a.x_out, row, a.d), *df = row_of<Elem>(a.n_out, row, a.d);
+        for (uint64_t i = threadIdx.x; i < a.d; i += blockDim.x) {
+            const Acc xv = at(x, i, 0), wn = dn ? at(dn, i, 0) * at(w_pre, i, 1) : Acc(0), gw = scale * at(gate, i, 1) * at(w_post, i, 1);
+            Acc       t[1] = {at(dy, i, 0) + q.r * wn - q.rrc * xv};
+            Acc       o[1] = {t[0] * gw * q.rf - q.rf3m * at(f, i, 0)};
+            if (dx) X::store(dx, static_cast<uint32_t>(i), t, all_x);
+            if (df) X::store(df, static_cast<uint32_t>(i), o, all_f);
+        }
+    }
+}
+// ... and the column sums by one that gives every thread a column of a chunk.
+template <int DT>
+__global__ void block_norm_bwd_columns_kernel(const NormArgs a)
+{
+    in_stream_order();
+    using Elem = typename Num<DT>::Elem;
+    using Acc  = typename Num<DT>::Acc;
+    const uint64_t i     = static_cast<uint64_t>(blockIdx.x % static_cast<uint32_t>(round_up_div(a.d, blockDim.x))) * blockDim.x + threadIdx.x;
+    const uint32_t chunk = blockIdx.x / static_cast<uint32_t>(round_up_div(a.d, blockDim.x));
+    if (i >= a.d || chunk >= a.chunks) return;
+    const Acc    scale  = static_cast<Acc>(a.scale);
+    const Extent all_g  = extent_of(a.dgate, round_up_div(a.rows, a.gate_rows) * a.d * sizeof(Elem));
+    const Extent part_g = extent_of(a.part_gate, 2ull * a.chunks * a.d * sizeof(Acc));
+    const Extent part_w = extent_of(a.part_pre, a.chunks * a.d * sizeof(Acc)), part_p = extent_of(a.part_post, a.chunks * a.d * sizeof(Acc));
+    const auto   at = [i](const void *p, const uint64_t row, const uint64_t d, const Acc none) {
+        return p ? static_cast<Acc>(Num<DT>::widen(static_cast<const Elem *>(p)[row * d + i])) : none;
+    };
+    const Acc   w_pre = at(a.w_pre, 0, a.d, 1), w_post = at(a.w_post, 0, a.d, 1);
+    const Chunk c = chunk_of(a, chunk);
+    Acc         sum_pre = 0, sum_post = 0, sum_gate = 0;
+    for (uint64_t row = c.first; row < c.end; ++row) {
+        const RowFactors<Acc> q     = static_cast<const RowFactors<Acc> *>(a.stats)[row];
+        const uint64_t        group = row / a.gate_rows;
+        const Acc x = at(a.x, row, a.d, 0), dn = at(a.dn, row, a.d, 0), fh = at(a.f, row, a.d, 0) * q.rf;
+        const Acc t = at(a.dy, row, a.d, 0) + q.r * (a.dn ? dn * w_pre : Acc(0)) - q.rrc * x;
+        sum_pre += dn * (x * q.r);
+        sum_gate += scale * t * (fh * w_post);
+        sum_post += scale * t * at(a.gate, group, a.d, 1) * fh;
+        if (a.dgate && (row + 1 == c.end || (row + 1) % a.gate_rows == 0)) {
+            uint64_t   slot;
+            const bool whole = whole_group(a, c, group, chunk, slot);
+            if (whole) {
+                Elem *const o = static_cast<Elem *>(a.dgate) + group * a.d + i;
+                if (all_g.holds(o, sizeof(Elem))) *o = Num<DT>::narrow(sum_gate);
+            } else {
+                Acc *const o = reinterpret_cast<Acc *>(a.part_gate) + slot * a.d + i;
+                if (part_g.holds(o, sizeof(Acc))) *o = sum_gate;
+            }
+            sum_gate = 0;
+        }
+    }
+    const uint64_t o = chunk * a.d + i;
+    if (a.dw_pre && part_w.holds(reinterpret_cast<Acc *>(a.part_pre) + o, sizeof(Acc))) reinterpret_cast<Acc *>(a.part_pre)[o] = sum_pre;
+    if (a.dw_post && part_p.holds(reinterpret_cast<Acc *>(a.part_post) + o, sizeof(Acc))) reinterpret_cast<Acc *>(a.part_post)[o] = sum_post;
+}
+
+// The partial rows added up: blockIdx.y = 0 w_pre, 1 w_post, 2 + k the k-th chunk border's gate group.  A thread takes every
+// kSplit-th partial row of its column; the CTA adds the kSplit sums in order.
+constexpr int kFinishColumns = 32, kSplit = 16;
+template <int DT>
+__global__ void __launch_bounds__(kFinishColumns *kSplit)
+block_norm_finish_kernel(const NormArgs a)
+{
+    in_stream_order();
+    using Elem = typename Num<DT>::Elem;
+    using Acc  = typename Num<DT>::Acc;
+    __shared__ Acc part[kSplit][kFinishColumns];
+    const uint32_t columns = static_cast<uint32_t>(round_up_div(a.d, kFinishColumns));
+    const uint32_t what    = blockIdx.x / columns;
+    const uint32_t lane = threadIdx.x % kFinishColumns, share = threadIdx.x / kFinishColumns;
+    const uint64_t i    = static_cast<uint64_t>(blockIdx.x % columns) * kFinishColumns + lane;
+    const Acc     *from;
+    Elem          *to;
+    uint64_t       count, stride = a.d, size = a.d;
+    if (what < 2) {
+        from  = reinterpret_cast<const Acc *>(what == 0 ? a.part_pre : a.part_post);
+        to    = static_cast<Elem *>(what == 0 ? a.dw_pre : a.dw_post);
+        count = a.chunks;
+        if (!to) return;
+    } else {
+        // the group that crosses from chunk `what - 2` into the next one, if that is where it begins to cross
+        if (!a.dgate) return;
+        const uint64_t border = (what - 1) * a.chunk_rows;              // the next chunk's first row
+        if (border >= a.rows || border % a.gate_rows == 0) return;
+        const uint64_t group = border / a.gate_rows, begin = group * a.gate_rows;
+        if (begin / a.chunk_rows != what - 2) return;
+        const uint64_t end = begin + a.gate_rows < a.rows ? begin + a.gate_rows : a.rows;
+        // slot 2 * chunk + 1 of the first chunk, then slot 2 * chunk of the others, one after the other every second row
+        from   = reinterpret_cast<const Acc *>(a.part_gate) + (2ull * (what - 2) + 1) * a.d;
+        to     = static_cast<Elem *>(a.dgate) + group * a.d;
+        count  = (end - 1) / a.chunk_rows - (what - 2) + 1;
+        stride = 0;
+    }
+    Acc s = 0;
+    if (i < a.d) {
+        for (uint64_t k = share; k < count; k += kSplit) s += from[(stride ? k * a.d : (k == 0 ? 0 : (2 * k - 1) * a.d)) + i];
+    }
+    part[share][lane] = s;
+    __syncthreads();
+    if (share != 0 || i >= a.d) return;
+#pragma unroll
+    for (int k = 1; k < kSplit; ++k) s += part[k][lane];
+    if (extent_of(to, size * sizeof(Elem)).holds(to + i, sizeof(Elem))) to[i] = Num<DT>::narrow(s);
+}
+
+// ---------------------------------------------------------------------------------------------- host side
+constexpr uint32_t kMaxChunks  = 4096;      // chunks of rows of a backward pass
+constexpr uint32_t kLongChunks = 64;        // the same for rows longer than a CTA's registers
+
+// Can a CTA's registers hold a row of the backward pass?
+bool row_fits(uint64_t d, int es)
+{
+    const uint64_t lanes = 16 / static_cast<uint64_t>(es);
+    return d <= kMaxTeam * (d % lanes == 0 ? 2 * lanes : 8);
+}
+
+template <int DT, bool kVector, int kHold, bool kCta>
+cudaError_t start_fwd(const NormArgs &a, uint32_t threads, cudaStream_t stream)
+{
+    const int sms = sm_count();
+    if (sms == 0) return cudaErrorInvalidDevice;
+    const uint64_t teams = kCta ? 1 : kWarpTeams, want = round_up_div(a.rows, teams);
+    const uint64_t most  = static_cast<uint64_t>(sms) * (2048 / threads);
+    return launch(block_norm_fwd_kernel<DT, kVector, kHold, kCta>, static_cast<unsigned>(want < most ? want : most), threads, 0, stream, a);
+}
+template <int DT, bool kVector>
+cudaError_t fwd_of(const NormArgs &a, cudaStream_t stream)
+{
+    constexpr uint64_t kW    = Access<DT, kVector>::kW;
+    const uint64_t     count = a.d / kW;
+    if (count <= 32) return start_fwd<DT, kVector, 1, false>(a, 32 * kWarpTeams, stream);
+    if (count <= 64) return start_fwd<DT, kVector, 2, false>(a, 32 * kWarpTeams, stream);
+    if (count <= 128) return start_fwd<DT, kVector, 4, false>(a, 32 * kWarpTeams, stream);
+    const auto team = [&](uint64_t hold) { return static_cast<uint32_t>(round_up_div(round_up_div(count, hold), 32) * 32); };
+    if (count <= 2 * kMaxTeam) return start_fwd<DT, kVector, 2, true>(a, team(2), stream);
+    if (count <= 4 * kMaxTeam) return start_fwd<DT, kVector, 4, true>(a, team(4), stream);
+    return start_fwd<DT, kVector, 0, true>(a, kMaxTeam, stream);
+}
+
+template <int DT, bool kVector, int kHold, bool kCta>
+cudaError_t start_bwd(const NormArgs &a, uint32_t threads, cudaStream_t stream)
+{
+    const uint32_t teams = kCta ? 1 : kWarpTeams;
+    return launch(block_norm_bwd_kernel<DT, kVector, kHold, kCta>, static_cast<unsigned>(round_up_div(a.chunks, teams)), threads, 0, stream, a);
+}
+template <int DT, bool kVector>
+cudaError_t bwd_of(const NormArgs &a, cudaStream_t stream)
+{
+    constexpr uint64_t kW    = Access<DT, kVector>::kW;
+    const uint64_t     count = a.d / kW;
+    const auto team = [&](uint64_t hold) { return static_cast<uint32_t>(round_up_div(round_up_div(count, hold), 32) * 32); };
+    if (count <= 32) return start_bwd<DT, kVector, 1, false>(a, 32 * kWarpTeams, stream);
+    if (count <= 64) return start_bwd<DT, kVector, 2, false>(a, 32 * kWarpTeams, stream);
+    if (count <= kMaxTeam) return start_bwd<DT, kVector, 1, true>(a, team(1), stream);
+    if (kVector || count <= 2 * kMaxTeam) return start_bwd<DT, kVector, 2, true>(a, team(2), stream);
+    return start_bwd<DT, kVector, kVector ? 2 : 8, true>(a, team(8), stream);
+}
+
+// the chunks of a backward pass: enough teams to fill the SMs twice over
+uint32_t chunks_of(uint64_t rows, uint64_t d, int es, int sms)
+{
+    const uint64_t lanes = 16 / static_cast<uint64_t>(es), count = d % lanes == 0 ? d / lanes : d;
+    uint64_t       most;
+    if (!row_fits(d, es)) most = kLongChunks;
+    else if (count <= 64) most = static_cast<uint64_t>(sms) * 24;
+    else most = static_cast<uint64_t>(sms) * (count <= 256 ? 6 : count <= 512 ? 3 : 2);
+    if (most > kMaxChunks) most = kMaxChunks;
+    if (most > rows) most = rows;
+    const uint64_t chunk_rows = round_up_div(rows, most);
+    return static_cast<uint32_t>(round_up_div(rows, chunk_rows));
+}
+
+template <int DT>
+cudaError_t forward(const NormArgs &a, cudaStream_t stream)
+{
+    return a.d % kLanes<DT> == 0 ? fwd_of<DT, true>(a, stream) : fwd_of<DT, false>(a, stream);
+}
+
+template <int DT>
+cudaError_t backward(const NormArgs &a, cudaStream_t stream)
+{
+    constexpr int es = static_cast<int>(sizeof(typename Num<DT>::Elem));
+    cudaError_t   e;
+    if (!row_fits(a.d, es)) {
+        const int sms = sm_count();
+        if (sms == 0) return cudaErrorInvalidDevice;
+        const uint64_t most = static_cast<uint64_t>(sms) * 4;
+        e = launch(block_norm_bwd_rows_kernel<DT>, static_cast<unsigned>(a.rows < most ? a.rows : most), kMaxTeam, 0, stream, a);
+        if (e != cudaSuccess) return e;
+        if (!a.dgate && !a.dw_pre && !a.dw_post) return cudaSuccess;
+        e = launch(block_norm_bwd_columns_kernel<DT>, static_cast<unsigned>(round_up_div(a.d, 128) * a.chunks), 128, 0, stream, a);
+    } else {
+        e = a.d % kLanes<DT> == 0 ? bwd_of<DT, true>(a, stream) : bwd_of<DT, false>(a, stream);
+    }
+    if (e != cudaSuccess || (!a.dgate && !a.dw_pre && !a.dw_post)) return e;
+    const uint64_t borders = a.dgate ? a.chunks - 1 : 0;
+    return launch(block_norm_finish_kernel<DT>, static_cast<unsigned>(round_up_div(a.d, kFinishColumns) * (2 + borders)), kFinishColumns * kSplit, 0,
+                  stream, a);
+}
+
+size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
+
+struct Parts {
+    uint32_t chunks;
+    uint64_t chunk_rows;
+    size_t   pre, post, gate, stats, bytes;      // offsets
+};
+// the workspace of a backward pass; sms: 0 for the most that any GPU could ask for
+Parts parts_of(uint64_t rows, uint64_t d, int es, int sms)
+{
+    const size_t acc = es == 8 ? 8 : 4;
+    Parts        p{};
+    p.chunks     = chunks_of(rows, d, es, sms);
+    p.chunk_rows = round_up_div(rows, p.chunks);
+    const size_t row = d * acc;
+    p.pre   = 0;
+    p.post  = round_up(p.chunks * row);
+    p.gate  = p.post + round_up(p.chunks * row);
+    p.stats = p.gate + round_up(2ull * p.chunks * row);
+    p.bytes = p.stats + (row_fits(d, es) ? 0 : round_up(rows * 4 * acc));
+    return p;
+}
+
+int check_common(const void *x, const void *f, const void *gate, const void *w_post, const void *w_pre, uint64_t rows, uint64_t d, uint64_t gate_rows,
+                 int dtype, float scale, float eps)
+{
+    if (element_size(dtype) == 0) return BT_ERR_DTYPE;
+    if (d == 0 || gate_rows == 0) return BT_ERR_SHAPE;
+    if (!(eps >= 0.0f) || scale != scale) return BT_ERR_SHAPE;
+    if (d > (1ull << 24) || rows > (1ull << 40) / d) return BT_ERR_TOO_LARGE;
+    if (rows == 0) return BT_OK;
+    if (!x || (!f && (gate || w_post))) return BT_ERR_NULL;
+    for (const void *p : {x, f, gate, w_post, w_pre})
+        if (!on_boundary(p, 16)) return BT_ERR_ALIGN;
+    return BT_OK;
+}
+
+template <typename F>
+int dispatch(int dtype, const F &go)
+{
+    cudaError_t e;
+    switch (dtype) {
+    case BT_F32: e = go(std::integral_constant<int, BT_F32>()); break;
+    case BT_F16: e = go(std::integral_constant<int, BT_F16>()); break;
+    case BT_BF16: e = go(std::integral_constant<int, BT_BF16>()); break;
+    default: e = go(std::integral_constant<int, BT_F64>()); break;
+    }
+    return e == cudaSuccess ? BT_OK : BT_ERR_CUDA;
+}
+
+}  // namespace
+}  // namespace bt
+
+extern "C" {
+
+size_t bt_block_norm_workspace_bytes(uint64_t rows, uint64_t d, int dtype)
+{
+    const int es = bt::element_size(dtype);
+    if (es == 0 || rows == 0 || d == 0) return 0;
+    if (d > (1ull << 24) || rows > (1ull << 40) / d) return 0;
+    const int sms = bt::sm_count();
+    return bt::parts_of(rows, d, es, sms ? sms : 148).bytes;
+}
+
+int bt_block_norm_fwd(const void *x, uint64_t rows, uint64_t d, uint64_t gate_rows, int dtype, float scale, float eps, const void *f,
+                      const void *gate, const void *w_post, const void *w_pre, void *x_out, void *n_out, void *stream)
+{
+    const int st = bt::check_common(x, f, gate, w_post, w_pre, rows, d, gate_rows, dtype, scale, eps);
+    if (st != BT_OK || rows == 0) return st;
+    if ((f != nullptr) != (x_out != nullptr) || (n_out != nullptr) != (w_pre != nullptr) || (!x_out && !n_out)) return BT_ERR_NULL;
+    if (!bt::on_boundary(x_out, 16) || !bt::on_boundary(n_out, 16)) return BT_ERR_ALIGN;
+    bt::NormArgs a{};
+    a.x = x, a.f = f, a.gate = gate, a.w_post = w_post, a.w_pre = w_pre;
+    a.x_out = x_out, a.n_out = n_out;
+    a.rows = rows, a.d = d, a.gate_rows = gate_rows;
+    a.scale = scale, a.eps = eps;
+    return bt::dispatch(dtype, [&](auto dt) { return bt::forward<decltype(dt)::value>(a, static_cast<cudaStream_t>(stream)); });
+}
+
+int bt_block_norm_bwd(const void *x_out, uint64_t rows, uint64_t d, uint64_t gate_rows, int dtype, float scale, float eps, const void *f,
+                      const void *gate, const void *w_post, const void *w_pre, const void *grad_n, const void *grad_x_out, void *grad_x,
+                      void *grad_f, void *grad_gate, void *grad_w_post, void *grad_w_pre, void *workspace, size_t workspace_bytes, void *stream)
+{
+    int st = bt::check_common(x_out, f, gate, w_post, w_pre, rows, d, gate_rows, dtype, scale, eps);
+    if (st != BT_OK) return st;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if ((grad_gate && !gate && rows) || (grad_w_post && !w_post && rows) || (grad_f && !f && rows)) return BT_ERR_NULL;
+    for (const void *p : {static_cast<const void *>(grad_x), static_cast<const void *>(grad_f), static_cast<const void *>(grad_gate),
+                          static_cast<const void *>(grad_w_post), static_cast<const void *>(grad_w_pre), grad_n, grad_x_out,
+                          static_cast<const void *>(workspace)})
+        if (!bt::on_boundary(p, 16)) return BT_ERR_ALIGN;
+    const int es = bt::element_size(dtype);
+    if (rows == 0) {                                                    // sums over no rows
+        for (void *p : {grad_w_post, grad_w_pre})
+            if (p && bt::reported(cudaMemsetAsync(p, 0, d * es, s)) != cudaSuccess) return BT_ERR_CUDA;
+        return BT_OK;
+    }
+    if ((grad_n != nullptr) != (w_pre != nullptr) || (grad_w_pre && !w_pre) || (!grad_n && !grad_x_out)) return BT_ERR_NULL;
+    const int sms = bt::sm_count();
+    if (sms == 0) return BT_ERR_CUDA;
+    const bt::Parts p = bt::parts_of(rows, d, es, sms);
+    const bool needs  = grad_gate || grad_w_post || grad_w_pre || !bt::row_fits(d, es);
+    if (needs && !workspace) return BT_ERR_NULL;
+    if (needs && workspace_bytes < p.bytes) return BT_ERR_WORKSPACE;
+    unsigned char *w = static_cast<unsigned char *>(workspace);
+    bt::NormArgs   a{};
+    a.x = x_out, a.f = f, a.gate = gate, a.w_post = w_post, a.w_pre = w_pre, a.dn = grad_n, a.dy = grad_x_out;
+    a.x_out = grad_x, a.n_out = grad_f, a.dgate = grad_gate, a.dw_post = grad_w_post, a.dw_pre = grad_w_pre;
+    if (needs) {
+        a.part_pre = reinterpret_cast<float *>(w + p.pre), a.part_post = reinterpret_cast<float *>(w + p.post);
+        a.part_gate = reinterpret_cast<float *>(w + p.gate), a.stats = w + p.stats;
+    }
+    a.rows = rows, a.d = d, a.gate_rows = gate_rows, a.chunks = p.chunks, a.chunk_rows = p.chunk_rows;
+    a.scale = scale, a.eps = eps;
+    return bt::dispatch(dtype, [&](auto dt) { return bt::backward<decltype(dt)::value>(a, s); });
+}
+
+}  // extern "C"

@@ -1,0 +1,313 @@
+// The gated feed-forward block: g = x Wg^T, u = x Wu^T, h = act(g) * u in one kernel, and its gradients from the stored g
+// and u: du = dh act(g), dg = dh u act'(g), dx = dg Wg + du Wu, dWg = dg^T x, dWu = du^T x.
+//
+// This file holds the checks, the elementwise part of the backward pass, and the products for every type and size on the
+// CUDA cores: tiles of 64 x 64 outputs, 16 of the summed axis at a time in shared memory, 4 x 4 outputs per thread.
+#include <type_traits>
+
+#include "bt_glu.cuh"
+
+namespace bt {
+namespace {
+
+// ---------------------------------------------------------------------------------------------- products, any type and size
+// out[i, j] = sum_k A(i, k) B(j, k), operands by their strides (in elements).
+struct ProductArgs {
+    const void *a[2], *b[2];
+    void       *out[3];
+    uint64_t    i, j, k;
+    uint64_t    a_i, a_k, b_j, b_k;
+    uint32_t    tiles_j;
+    uint64_t    tiles;
+    int32_t    *dev_status;
+};
+enum { kForward, kInputGrad, kWeightGrad };
+
+constexpr int kTile = 64, kDepth = 16, kThreads = 256, kEach = 4;
+
+template <int DT>
+__device__ __forceinline__ void load_tile(typename Num<DT>::Acc (&to)[kDepth][kTile + 4], const void *from, const uint64_t i0, const uint64_t k0,
+                                          const uint64_t i_end, const uint64_t k_end, const uint64_t stride_i, const uint64_t stride_k)
+{
+    using Elem       = typename Num<DT>::Elem;
+    const Elem *base = static_cast<const Elem *>(from);
+#pragma unroll
+    for (int v = 0; v < kTile * kDepth / kThreads; ++v) {
+        const int e = threadIdx.x + v * kThreads;
+        // neighbouring threads along the axis that is contiguous in memory
+        const int i = stride_k == 1 ? e / kDepth : e % kTile, k = stride_k == 1 ? e % kDepth : e / kTile;
+        to[k][i]    = i0 + i < i_end && k0 + k < k_end ? Num<DT>::widen(base[(i0 + i) * stride_i + (k0 + k) * stride_k]) : typename Num<DT>::Acc(0);
+    }
+}
+
+template <int DT, int kMode, int kAct>
+__global__ void __launch_bounds__(kThreads)
+product_kernel(const ProductArgs p)
+{
+    in_stream_order();
+    using Elem           = typename Num<DT>::Elem;
+    using Acc            = typename Num<DT>::Acc;
+    constexpr bool kDual = kMode == kForward;                          // two B's, two sums
+    __shared__ Acc as[kDepth][kTile + 4], bs[kDual ? 2 : 1][kDepth][kTile + 4];
+    if (p.dev_status && blockIdx.x == 0 && threadIdx.x == 0) *p.dev_status = BT_OK;
+    const uint64_t tile = kMode == kWeightGrad ? blockIdx.x % p.tiles : blockIdx.x;
+    const uint32_t which = kMode == kWeightGrad ? static_cast<uint32_t>(blockIdx.x / p.tiles) : 0;
+    const uint64_t i0 = tile / p.tiles_j * kTile, j0 = tile % p.tiles_j * kTile;
+    const int      ti = threadIdx.x / 16 * kEach, tj = threadIdx.x % 16 * kEach;
+    Acc            sum[kDual ? 2 : 1][kEach][kEach] = {};
+    for (int pair = 0; pair < (kMode == kInputGrad ? 2 : 1); ++pair) {
+        const void *a = p.a[kMode == kWeightGrad ? which : pair], *b = p.b[kMode == kInputGrad ? pair : 0];
+        for (uint64_t k0 = 0; k0 < p.k; k0 += kDepth) {
+            load_tile<DT>(as, a, i0, k0, p.i, p.k, p.a_i, p.a_k);
+            load_tile<DT>(bs[0], b, j0, k0, p.j, p.k, p.b_j, p.b_k);
+            if constexpr (kDual) load_tile<DT>(bs[1], p.b[1], j0, k0, p.j, p.k, p.b_j, p.b_k);
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < kDepth; ++k) {
+                Acc av[kEach];
+#pragma unroll
+                for (int m = 0; m < kEach; ++m) av[m] = as[k][ti + m];
+#pragma unroll
+                for (int q = 0; q < (kDual ? 2 : 1); ++q)
+#pragma unroll
+                    for (int n = 0; n < kEach; ++n) {
+                        const Acc bv = bs[q][k][tj + n];
+#pragma unroll
+                        for (int m = 0; m < kEach; ++m) sum[q][m][n] += av[m] * bv;
+                    }
+            }
+            __syncthreads();
+        }
+    }
+    const Extent e0 = extent_of(p.out[which], p.i * p.j * sizeof(Elem));
+#pragma unroll
+    for (int m = 0; m < kEach; ++m)
+#pragma unroll
+        for (int n = 0; n < kEach; ++n) {
+            const uint64_t i = i0 + ti + m, j = j0 + tj + n, o = i * p.j + j;
+            if (i >= p.i || j >= p.j) continue;
+            if constexpr (kMode == kForward) {
+                const Acc g = sum[0][m][n], u = sum[kDual ? 1 : 0][m][n], act = act_of<kAct>(g);
+                Elem *const h = static_cast<Elem *>(p.out[0]) + o;
+                if (e0.holds(h, sizeof(Elem))) *h = Num<DT>::narrow(act * u);
+                if (p.out[1]) {
+                    Elem *const og = static_cast<Elem *>(p.out[1]) + o;
+                    if (extent_of(p.out[1], p.i * p.j * sizeof(Elem)).holds(og, sizeof(Elem))) *og = Num<DT>::narrow(kAct == BT_ACT_RELU ? act : g);
+                }
+                if (p.out[2]) {
+                    Elem *const ou = static_cast<Elem *>(p.out[2]) + o;
+                    if (extent_of(p.out[2], p.i * p.j * sizeof(Elem)).holds(ou, sizeof(Elem))) *ou = Num<DT>::narrow(u);
+                }
+            } else {
+                Elem *const y = static_cast<Elem *>(p.out[which]) + o;
+                if (e0.holds(y, sizeof(Elem))) *y = Num<DT>::narrow(sum[0][m][n]);
+            }
+        }
+}
+
+template <int DT, int kMode, int kAct>
+cudaError_t start_product(ProductArgs p, cudaStream_t stream)
+{
+    p.tiles_j           = static_cast<uint32_t>(round_up_div(p.j, kTile));
+    p.tiles             = round_up_div(p.i, kTile) * p.tiles_j;
+    const uint64_t grid = p.tiles * (kMode == kWeightGrad ? 2 : 1);
+    if (grid > 0x7FFFFFFFull) return cudaErrorInvalidValue;
+    return launch(product_kernel<DT, kMode, kAct>, static_cast<unsigned>(grid), kThreads, 0, stream, p);
+}
+
+template <int DT>
+cudaError_t forward_of(const GluCall &c, cudaStream_t stream)
+{
+    ProductArgs p{};
+    p.a[0] = c.x, p.b[0] = c.w_gate, p.b[1] = c.w_up;
+    p.out[0] = c.h, p.out[1] = c.g, p.out[2] = c.u;
+    p.i = c.rows, p.j = c.d_ff, p.k = c.d_in;
+    p.a_i = p.b_j = c.d_in, p.a_k = p.b_k = 1;
+    p.dev_status = c.dev_status;
+    return with_act<DT>(c.act, [&](auto dt, auto act) { return start_product<decltype(dt)::value, kForward, decltype(act)::value>(p, stream); });
+}
+
+template <int DT>
+cudaError_t backward_of(const GluCall &c, cudaStream_t stream)
+{
+    ProductArgs p{};
+    p.a[0] = c.dg, p.a[1] = c.du;
+    if (c.dx) {
+        p.b[0] = c.w_gate, p.b[1] = c.w_up, p.out[0] = c.dx;
+        p.i = c.rows, p.j = c.d_in, p.k = c.d_ff;
+        p.a_i = c.d_ff, p.a_k = 1, p.b_j = 1, p.b_k = c.d_in;
+        const cudaError_t e = start_product<DT, kInputGrad, 0>(p, stream);
+        if (e != cudaSuccess) return e;
+    }
+    if (c.dw_gate) {
+        p.b[0] = c.x, p.out[0] = c.dw_gate, p.out[1] = c.dw_up;
+        p.i = c.d_ff, p.j = c.d_in, p.k = c.rows;
+        p.a_i = 1, p.a_k = c.d_ff, p.b_j = 1, p.b_k = c.d_in;
+        return start_product<DT, kWeightGrad, 0>(p, stream);
+    }
+    return cudaSuccess;
+}
+
+// ---------------------------------------------------------------------------------------------- slopes
+// du = dh act(g), dg = dh u act'(g): 16 bytes of each per thread.  Bound by HBM.  ReLU: a select, so that a closed gate's
+// gradient is +0 whatever dh and u hold.
+struct SlopeArgs {
+    const void *dh, *g, *u;
+    void       *dg, *du;
+    uint64_t    n;
+    int32_t    *dev_status;
+};
+template <int DT, int kAct>
+__device__ __forceinline__ void slopes(const typename Num<DT>::Acc dh, const typename Num<DT>::Acc g, const typename Num<DT>::Acc u,
+                                       typename Num<DT>::Acc &dg, typename Num<DT>::Acc &du)
+{
+    using Acc = typename Num<DT>::Acc;
+    if constexpr (kAct == BT_ACT_RELU) {
+        const bool off = g <= Acc(0);
+        dg             = off ? Acc(0) : dh * u;
+        du             = off ? Acc(0) : dh * g;
+    } else {
+        dg = dh * u * act_slope<kAct>(g);
+        du = dh * act_of<kAct>(g);
+    }
+}
+template <int DT, int kAct>
+__global__ void __launch_bounds__(kThreads)
+slopes_kernel(const SlopeArgs p)
+{
+    in_stream_order();
+    using Elem         = typename Num<DT>::Elem;
+    using Acc          = typename Num<DT>::Acc;
+    constexpr int  kW  = kLanes<DT>;
+    const uint64_t i   = static_cast<uint64_t>(blockIdx.x) * kThreads + threadIdx.x, vecs = p.n / kW;
+    const Extent   eg = extent_of(p.dg, p.n * sizeof(Elem)), eu = extent_of(p.du, p.n * sizeof(Elem));
+    if (p.dev_status && i == 0) *p.dev_status = BT_OK;
+    if (i < vecs) {
+        Acc dh[kW], g[kW], u[kW];
+        widen_vec<DT>(__ldg(static_cast<const uint4 *>(p.dh) + i), dh);
+        widen_vec<DT>(__ldg(static_cast<const uint4 *>(p.g) + i), g);
+        widen_vec<DT>(__ldg(static_cast<const uint4 *>(p.u) + i), u);
+#pragma unroll
+        for (int k = 0; k < kW; ++k) slopes<DT, kAct>(dh[k], g[k], u[k], g[k], u[k]);
+        if (eg.holds(static_cast<uint4 *>(p.dg) + i, 16)) static_cast<uint4 *>(p.dg)[i] = narrow_vec<DT>(g);
+        if (eu.holds(static_cast<uint4 *>(p.du) + i, 16)) static_cast<uint4 *>(p.du)[i] = narrow_vec<DT>(u);
+    }
+    if (i < p.n - vecs * kW) {                                          // the last n % kW elements
+        const uint64_t e = vecs * kW + i;
+        const auto     at = [e](const void *q) { return Num<DT>::widen(static_cast<const Elem *>(q)[e]); };
+        Acc            dg, du;
+        slopes<DT, kAct>(at(p.dh), at(p.g), at(p.u), dg, du);
+        if (eg.holds(static_cast<Elem *>(p.dg) + e, sizeof(Elem))) static_cast<Elem *>(p.dg)[e] = Num<DT>::narrow(dg);
+        if (eu.holds(static_cast<Elem *>(p.du) + e, sizeof(Elem))) static_cast<Elem *>(p.du)[e] = Num<DT>::narrow(du);
+    }
+}
+template <int DT>
+cudaError_t slopes_of(const SlopeArgs &p, int act, cudaStream_t stream)
+{
+    const uint64_t grid = round_up_div(round_up_div(p.n, kLanes<DT>), kThreads);
+    if (grid > 0x7FFFFFFFull) return cudaErrorInvalidValue;
+    return with_act<DT>(act, [&](auto dt, auto a) {
+        return launch(slopes_kernel<decltype(dt)::value, decltype(a)::value>, static_cast<unsigned>(grid), kThreads, 0, stream, p);
+    });
+}
+
+template <typename F>
+int dispatch(int dtype, const F &go)
+{
+    cudaError_t e;
+    switch (dtype) {
+    case BT_F32: e = go(std::integral_constant<int, BT_F32>()); break;
+    case BT_F16: e = go(std::integral_constant<int, BT_F16>()); break;
+    case BT_BF16: e = go(std::integral_constant<int, BT_BF16>()); break;
+    default: e = go(std::integral_constant<int, BT_F64>()); break;
+    }
+    return e == cudaSuccess ? BT_OK : BT_ERR_CUDA;
+}
+
+int check_sizes(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype)
+{
+    if (element_size(dtype) == 0) return BT_ERR_DTYPE;
+    if (d_in == 0 || d_ff == 0) return BT_ERR_SHAPE;
+    if (d_in > (1ull << 24) || d_ff > (1ull << 24) || rows > (1ull << 31) - 1) return BT_ERR_TOO_LARGE;
+    return BT_OK;
+}
+
+size_t padded(uint64_t rows, uint64_t d_ff, int es) { return (rows * d_ff * static_cast<uint64_t>(es) + 255) / 256 * 256; }
+
+size_t workspace_of(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, bool backward)
+{
+    (void)d_in;
+    return backward ? 2 * padded(rows, d_ff, element_size(dtype)) : 0;
+}
+
+}  // namespace
+}  // namespace bt
+
+extern "C" {
+
+size_t bt_glu_workspace_bytes(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, int backward)
+{
+    return bt::check_sizes(rows, d_in, d_ff, dtype) == BT_OK ? bt::workspace_of(rows, d_in, d_ff, dtype, backward != 0) : 0;
+}
+
+int bt_glu_fwd(const void *x, uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, int activation, const void *w_gate, const void *w_up, void *h,
+               void *g_out, void *u_out, void *workspace, size_t workspace_bytes, int32_t *dev_status, void *stream)
+{
+    const int st = bt::check_sizes(rows, d_in, d_ff, dtype);
+    if (st != BT_OK) return st;
+    if (activation < BT_ACT_RELU || activation > BT_ACT_GELU_TANH) return BT_ERR_SHAPE;
+    if (!bt::on_boundary(dev_status, 4)) return BT_ERR_ALIGN;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (rows == 0) {
+        if (dev_status && bt::reported(cudaMemsetAsync(dev_status, 0, sizeof(int32_t), s)) != cudaSuccess) return BT_ERR_CUDA;
+        return BT_OK;
+    }
+    if (!x || !w_gate || !w_up || !h) return BT_ERR_NULL;
+    for (const void *p : {x, w_gate, w_up, static_cast<const void *>(h), static_cast<const void *>(g_out), static_cast<const void *>(u_out),
+                          static_cast<const void *>(workspace)})
+        if (!bt::on_boundary(p, 16)) return BT_ERR_ALIGN;
+    const size_t need = bt::workspace_of(rows, d_in, d_ff, dtype, false);
+    if (need != 0 && !workspace) return BT_ERR_NULL;
+    if (workspace_bytes < need) return BT_ERR_WORKSPACE;
+    bt::GluCall c{};
+    c.x = x, c.w_gate = w_gate, c.w_up = w_up, c.h = h, c.g = g_out, c.u = u_out;
+    c.rows = rows, c.d_in = d_in, c.d_ff = d_ff, c.dtype = dtype, c.act = activation, c.dev_status = dev_status;
+    return bt::dispatch(dtype, [&](auto dt) { return bt::forward_of<decltype(dt)::value>(c, s); });
+}
+
+int bt_glu_bwd(const void *grad_h, uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, int activation, const void *g, const void *u,
+               const void *x, const void *w_gate, const void *w_up, void *grad_x, void *grad_w_gate, void *grad_w_up, void *workspace, size_t workspace_bytes,
+               int32_t *dev_status, void *stream)
+{
+    const int st = bt::check_sizes(rows, d_in, d_ff, dtype);
+    if (st != BT_OK) return st;
+    if (activation < BT_ACT_RELU || activation > BT_ACT_GELU_TANH) return BT_ERR_SHAPE;
+    for (const void *p : {grad_h, g, u, x, w_gate, w_up, static_cast<const void *>(grad_x), static_cast<const void *>(grad_w_gate),
+                          static_cast<const void *>(grad_w_up), static_cast<const void *>(workspace)})
+        if (!bt::on_boundary(p, 16)) return BT_ERR_ALIGN;
+    if (!bt::on_boundary(dev_status, 4)) return BT_ERR_ALIGN;
+    if ((grad_w_gate != nullptr) != (grad_w_up != nullptr)) return BT_ERR_NULL;
+    cudaStream_t   s  = static_cast<cudaStream_t>(stream);
+    const uint64_t es = static_cast<uint64_t>(bt::element_size(dtype));
+    if (rows == 0) {                                                    // sums over no rows
+        for (void *p : {grad_w_gate, grad_w_up})
+            if (p && bt::reported(cudaMemsetAsync(p, 0, d_in * d_ff * es, s)) != cudaSuccess) return BT_ERR_CUDA;
+        if (dev_status && bt::reported(cudaMemsetAsync(dev_status, 0, sizeof(int32_t), s)) != cudaSuccess) return BT_ERR_CUDA;
+        return BT_OK;
+    }
+    if (!grad_h || !g || !u || (!grad_x && !grad_w_gate)) return BT_ERR_NULL;
+    if ((grad_x && (!w_gate || !w_up)) || (grad_w_gate && !x)) return BT_ERR_NULL;
+    if (!workspace) return BT_ERR_NULL;
+    if (workspace_bytes < bt::workspace_of(rows, d_in, d_ff, dtype, true)) return BT_ERR_WORKSPACE;
+    unsigned char *w = static_cast<unsigned char *>(workspace);
+    bt::SlopeArgs  slope{grad_h, g, u, w, w + bt::padded(rows, d_ff, static_cast<int>(es)), rows * d_ff, dev_status};
+    bt::GluCall    c{};
+    c.x = x, c.w_gate = w_gate, c.w_up = w_up, c.dg = slope.dg, c.du = slope.du, c.dx = grad_x, c.dw_gate = grad_w_gate, c.dw_up = grad_w_up;
+    c.rows = rows, c.d_in = d_in, c.d_ff = d_ff, c.dtype = dtype, c.act = activation, c.dev_status = dev_status;
+    return bt::dispatch(dtype, [&](auto dt) {
+        const cudaError_t e = bt::slopes_of<decltype(dt)::value>(slope, activation, s);
+        return e != cudaSuccess ? e : bt::backward_of<decltype(dt)::value>(c, s);
+    });
+}
+
+}  // extern "C"

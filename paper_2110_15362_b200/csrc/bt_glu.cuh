@@ -1,0 +1,70 @@
+// The gated feed-forward block's activations, and the launchers of its kernels.
+#pragma once
+
+#include "bt_numeric.cuh"
+
+namespace bt {
+
+__device__ __forceinline__ float  exp_of(float v) { return expf(v); }
+__device__ __forceinline__ double exp_of(double v) { return exp(v); }
+__device__ __forceinline__ float  erfc_of(float v) { return erfcf(v); }
+__device__ __forceinline__ double erfc_of(double v) { return erfc(v); }
+
+template <typename A>
+__device__ __forceinline__ A sigmoid_of(const A v)
+{
+    return A(1) / (A(1) + exp_of(-v));
+}
+
+// act(g), in the sums' type.  The Gaussian's distribution comes from erfc and the tanh form from the logistic function, which
+// keep their digits for negative g where 1 + erf and 1 + tanh cancel.
+template <int kAct, typename A>
+__device__ __forceinline__ A act_of(const A g)
+{
+    if constexpr (kAct == BT_ACT_RELU) return g <= A(0) ? A(0) : g;                  // a NaN passes
+    else if constexpr (kAct == BT_ACT_SILU) return g * sigmoid_of(g);
+    else if constexpr (kAct == BT_ACT_GELU) return A(0.5) * g * erfc_of(-A(0.70710678118654752440) * g);
+    else return g * sigmoid_of(A(1.5957691216057307118) * (g + A(0.044715) * g * g * g));
+}
+// act'(g), given a stored gate (ReLU: the gate as it is stored, max(g, 0))
+template <int kAct, typename A>
+__device__ __forceinline__ A act_slope(const A g)
+{
+    if constexpr (kAct == BT_ACT_RELU) {
+        return g <= A(0) ? A(0) : A(1);
+    } else if constexpr (kAct == BT_ACT_SILU) {
+        const A s = sigmoid_of(g);
+        return s * (A(1) + g * (A(1) - s));
+    } else if constexpr (kAct == BT_ACT_GELU) {
+        return A(0.5) * erfc_of(-A(0.70710678118654752440) * g) + g * A(0.39894228040143267794) * exp_of(A(-0.5) * g * g);
+    } else {
+        if (g > A(64) || g < A(-64)) return g > A(0) ? A(1) : A(0);                  // g^2 must not overflow below
+        const A s = sigmoid_of(A(1.5957691216057307118) * (g + A(0.044715) * g * g * g));
+        return s + g * s * (A(1) - s) * A(1.5957691216057307118) * (A(1) + A(3 * 0.044715) * g * g);
+    }
+}
+
+// One call of the block, forward or backward (sizes checked, none of them 0).
+struct GluCall {
+    const void *x, *w_gate, *w_up;                 // [rows, d_in], [d_ff, d_in] twice
+    void       *h, *g, *u;                         // forward: [rows, d_ff]; g and u may be NULL
+    const void *dg, *du;                           // backward: [rows, d_ff], made by launch_glu_slopes
+    void       *dx, *dw_gate, *dw_up;              // backward: any may be NULL
+    uint64_t    rows, d_in, d_ff;
+    int         dtype, act;
+    int32_t    *dev_status;
+};
+
+// calls launch(std::integral_constant<int, DT>, std::integral_constant<int, ACT>) for a call's type and activation
+template <int DT, typename F>
+cudaError_t with_act(int act, const F &go)
+{
+    switch (act) {
+    case BT_ACT_RELU: return go(std::integral_constant<int, DT>(), std::integral_constant<int, BT_ACT_RELU>());
+    case BT_ACT_SILU: return go(std::integral_constant<int, DT>(), std::integral_constant<int, BT_ACT_SILU>());
+    case BT_ACT_GELU: return go(std::integral_constant<int, DT>(), std::integral_constant<int, BT_ACT_GELU>());
+    default: return go(std::integral_constant<int, DT>(), std::integral_constant<int, BT_ACT_GELU_TANH>());
+    }
+}
+
+}  // namespace bt

@@ -1,0 +1,344 @@
+// The norm of all gradients of a step and their clipping: norm = sqrt(sum g^2) over many tensors, c = min(1, max_norm /
+// (norm + 1e-6)), y = c * g.
+//
+// Bound by HBM: every gradient is read once for the sum and once for the product, and written once; what the first pass
+// leaves in the L2 the second finds there, so it walks the tiles from the last to the first.
+//
+// Sums: the squares of a 16-byte vector are added in binary32 (16-bit elements: every square is exact there), vectors in
+// binary64.  A vector whose binary32 sum may have overflowed, or may have lost squares to underflow, is added again in
+// binary64, so that gradients of any magnitude count.  Tiles go to CTAs by their number and partial sums are added in the
+// CTAs' order, without atomics: a call gives the same bits every time on the same kind of GPU.
+#include "bt_numeric.cuh"
+
+namespace bt {
+namespace {
+
+constexpr int      kThreads   = 256;
+constexpr int      kUnroll    = 8;                                     // independent 16-byte vectors per thread
+constexpr uint32_t kTileBytes = kThreads * kUnroll * 16;
+constexpr uint32_t kMaxCtas   = 1024;                                  // of the summing kernel: its partial sums per launch
+constexpr uint32_t kFew = 64, kMany = 1024;                            // tensors of one launch (two sizes of the parameters)
+
+struct GradTensor {
+    const void *g;
+    void       *y;
+    uint64_t    n;
+};
+template <uint32_t kTensors>
+struct GradParams {
+    GradTensor t[kTensors];
+    uint32_t   first_tile[kTensors];                                   // the number of the tensor's first tile
+    uint32_t   tensors, tiles;
+};
+
+template <uint32_t kTensors>
+__device__ __forceinline__ uint32_t tensor_of(const GradParams<kTensors> &p, const uint32_t tile)
+{
+    uint32_t lo = 0, hi = p.tensors;                                   // first_tile[lo] <= tile < first_tile[hi]
+    while (hi - lo > 1) {
+        const uint32_t mid = (lo + hi) / 2;
+        if (p.first_tile[mid] <= tile) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+
+template <int DT>
+__device__ __forceinline__ double squares(const uint4 &w)
+{
+    typename Num<DT>::Acc v[kLanes<DT>];
+    widen_vec<DT>(w, v);
+    if constexpr (DT == BT_F64) {
+        return v[0] * v[0] + v[1] * v[1];
+    } else {
+        float s = v[0] * v[0];
+#pragma unroll
+        for (int k = 1; k < kLanes<DT>; ++k) s = fmaf(v[k], v[k], s);
+        // below 1e-24 a square that underflowed (under 1.2e-38) could have counted; a sum that is not finite may be a
+        // sum of finite squares
+        if (!(s >= 1e-24f && s <= 3e38f) && ((w.x | w.y | w.z | w.w) & 0x7FFFFFFFu)) {
+            double d = 0;
+#pragma unroll
+            for (int k = 0; k < kLanes<DT>; ++k) d += static_cast<double>(v[k]) * v[k];
+            return d;
+        }
+        return static_cast<double>(s);
+    }
+}
+
+__device__ __forceinline__ double block_sum(double v)
+{
+    __shared__ double part[kThreads / 32];
+    v = warp_sum(v);
+    if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = v;
+    __syncthreads();
+    double s = 0;
+#pragma unroll
+    for (int k = 0; k < kThreads / 32; ++k) s += part[k];
+    return s;
+}
+
+template <int DT, uint32_t kTensors>
+__global__ void __launch_bounds__(kThreads)
+sum_squares_kernel(const __grid_constant__ GradParams<kTensors> p, double *__restrict__ partial)
+{
+    in_stream_order();
+    constexpr int      kVec      = kLanes<DT>;
+    constexpr uint32_t kTileVecs = kThreads * kUnroll;
+    using Elem                   = typename Num<DT>::Elem;
+    double sum = 0;
+    for (uint32_t tile = blockIdx.x; tile < p.tiles; tile += gridDim.x) {
+        const uint32_t    k    = tensor_of(p, tile);
+        const uint64_t    n    = p.t[k].n, vecs = n / kVec;
+        const uint64_t    v0   = static_cast<uint64_t>(tile - p.first_tile[k]) * kTileVecs + threadIdx.x;
+        const uint4      *g    = static_cast<const uint4 *>(p.t[k].g);
+        uint4             w[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) w[u] = v0 + u * kThreads < vecs ? __ldg(g + v0 + u * kThreads) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) sum += squares<DT>(w[u]);
+        // the last n % kVec elements with the tensor's first tile
+        if (tile == p.first_tile[k] && threadIdx.x < n - vecs * kVec) {
+            const double d = Num<DT>::widen(static_cast<const Elem *>(p.t[k].g)[vecs * kVec + threadIdx.x]);
+            sum += d * d;
+        }
+    }
+    sum = block_sum(sum);
+    if (threadIdx.x == 0 && extent_of(partial, 8ull * gridDim.x).holds(partial + blockIdx.x, 8)) partial[blockIdx.x] = sum;
+}
+
+// the sum of `count` doubles, the same in every thread of the CTA
+__device__ __forceinline__ double sum_of(const double *__restrict__ partial, const uint32_t count)
+{
+    double s = 0;
+    for (uint32_t k = threadIdx.x; k < count; k += kThreads) s += partial[k];
+    return block_sum(s);
+}
+
+__global__ void __launch_bounds__(kThreads)
+finish_kernel(const double *__restrict__ partial, const uint32_t count, double *sumsq, const int accumulate, float *norm_out)
+{
+    in_stream_order();
+    double s = sum_of(partial, count);
+    if (threadIdx.x != 0) return;
+    if (sumsq) {
+        if (accumulate) s += *sumsq;
+        *sumsq = s;
+    }
+    if (norm_out) *norm_out = static_cast<float>(sqrt(s));
+}
+
+// y = min(1, max_norm / (norm + 1e-6)) * g.  A factor of exactly 1 leaves a tensor that is scaled in place as it is: nothing
+// is read or written.  A norm that is infinite gives the factor 0, a NaN a NaN, as the formula says.
+template <int DT, uint32_t kTensors>
+__global__ void __launch_bounds__(kThreads)
+scale_kernel(const __grid_constant__ GradParams<kTensors> p, const double *__restrict__ partial, const uint32_t count, const float max_norm, float *norm_out)
+{
+    in_stream_order();
+    constexpr int      kVec      = kLanes<DT>;
+    constexpr uint32_t kTileVecs = kThreads * kUnroll;
+    using Elem                   = typename Num<DT>::Elem;
+    using Acc                    = typename Num<DT>::Acc;
+    const double norm = sqrt(sum_of(partial, count));
+    if (norm_out && blockIdx.x == 0 && threadIdx.x == 0) *norm_out = static_cast<float>(norm);
+    const double q = static_cast<double>(max_norm) / (norm + 1e-6);
+    const Acc    c = static_cast<Acc>(q > 1.0 ? 1.0 : q);
+    for (uint32_t i = blockIdx.x; i < p.tiles; i += gridDim.x) {
+        const uint32_t tile = p.tiles - 1 - i;                         // the L2 holds the end of what was read before
+        const uint32_t k    = tensor_of(p, tile);
+        if (c == Acc(1) && p.t[k].y == p.t[k].g) continue;
+        const uint64_t n    = p.t[k].n, vecs = n / kVec;
+        const uint64_t v0   = static_cast<uint64_t>(tile - p.first_tile[k]) * kTileVecs + threadIdx.x;
+        const uint4   *g    = static_cast<const uint4 *>(p.t[k].g);
+        uint4         *y    = static_cast<uint4 *>(p.t[k].y);
+        const Extent   out  = extent_of(y, n * sizeof(Elem));
+        uint4          w[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+            if (v0 + u * kThreads < vecs) w[u] = g[v0 + u * kThreads];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            if (v0 + u * kThreads >= vecs) continue;
+            Acc v[kVec];
+            widen_vec<DT>(w[u], v);
+#pragma unroll
+            for (int j = 0; j < kVec; ++j) v[j] *= c;
+            if (out.holds(y + v0 + u * kThreads, 16)) y[v0 + u * kThreads] = narrow_vec<DT>(v);
+        }
+        if (tile == p.first_tile[k] && threadIdx.x < n - vecs * kVec) {
+            const uint64_t e = vecs * kVec + threadIdx.x;
+            Elem          *o = static_cast<Elem *>(p.t[k].y) + e;
+            if (out.holds(o, sizeof(Elem))) *o = Num<DT>::narrow(Num<DT>::widen(static_cast<const Elem *>(p.t[k].g)[e]) * c);
+        }
+    }
+}
+
+// ---- host side
+uint64_t tiles_of(uint64_t n, int es) { return round_up_div(n * static_cast<uint64_t>(es), kTileBytes); }
+
+template <int DT, uint32_t kTensors>
+cudaError_t launch_group(const GradTensor *t, uint32_t count, uint64_t tiles, bool scale, double *partial, uint32_t &partials,
+                         float max_norm, float *norm_out, cudaStream_t stream)
+{
+    GradParams<kTensors> p;                                            // (not cleared: only the first `tensors` are looked at)
+    uint32_t             tile = 0;
+    for (uint32_t k = 0; k < count; ++k) {
+        p.t[k]          = t[k];
+        p.first_tile[k] = tile;
+        tile += static_cast<uint32_t>(tiles_of(t[k].n, static_cast<int>(sizeof(typename Num<DT>::Elem))));
+    }
+    p.tensors = count, p.tiles = static_cast<uint32_t>(tiles);
+    const int sms = sm_count();
+    if (sms == 0) return cudaErrorInvalidDevice;
+    unsigned grid = static_cast<unsigned>(sms) * 4;
+    if (grid > kMaxCtas) grid = kMaxCtas;
+    if (grid > tiles) grid = static_cast<unsigned>(tiles);
+    if (scale) return launch(scale_kernel<DT, kTensors>, grid, kThreads, 0, stream, p, partial, partials, max_norm, norm_out);
+    const cudaError_t e = launch(sum_squares_kernel<DT, kTensors>, grid, kThreads, 0, stream, p, partial + partials);
+    partials += grid;
+    return e;
+}
+
+template <int DT>
+cudaError_t launch_typed(const GradTensor *t, uint32_t count, uint64_t tiles, bool scale, double *partial, uint32_t &partials,
+                         float max_norm, float *norm_out, cudaStream_t stream)
+{
+    return count <= kFew ? launch_group<DT, kFew>(t, count, tiles, scale, partial, partials, max_norm, norm_out, stream)
+                         : launch_group<DT, kMany>(t, count, tiles, scale, partial, partials, max_norm, norm_out, stream);
+}
+
+int check_items(const bt_batch_item *items, uint32_t count, int dtype, bool outputs)
+{
+    if (element_size(dtype) == 0) return BT_ERR_DTYPE;
+    if (count != 0 && !items) return BT_ERR_NULL;
+    for (uint32_t k = 0; k < count; ++k) {
+        const bt_batch_item &it = items[k];
+        if (it.n == 0) continue;
+        if (!it.dense || (outputs && !it.y_out)) return BT_ERR_NULL;
+        if (!on_boundary(it.dense, 16) || (outputs && !on_boundary(it.y_out, 16))) return BT_ERR_ALIGN;
+        if (it.n > (1ull << 46)) return BT_ERR_TOO_LARGE;              // tiles are counted in 32 bits
+    }
+    return BT_OK;
+}
+
+// One pass over all tensors, kMany of them at most per launch: the sums (scale == false; appends to partial[0 .. partials)),
+// or the products by the factor that the partial sums give (norm_out: written by the first launch).
+cudaError_t pass(const bt_batch_item *items, uint32_t count, int dtype, bool scale, double *partial, uint32_t &partials, float max_norm,
+                 float *norm_out, cudaStream_t stream)
+{
+    const int  es = element_size(dtype);
+    GradTensor t[kMany];
+    uint32_t   m     = 0;
+    uint64_t   tiles = 0;
+    for (uint32_t k = 0; k <= count; ++k) {
+        const uint64_t mine = k < count ? tiles_of(items[k].n, es) : 0;
+        if (m != 0 && (k == count || m == kMany || tiles + mine > 0xFFFFFFF0ull)) {
+            cudaError_t e;
+            switch (dtype) {
+            case BT_F32: e = launch_typed<BT_F32>(t, m, tiles, scale, partial, partials, max_norm, norm_out, stream); break;
+            case BT_F16: e = launch_typed<BT_F16>(t, m, tiles, scale, partial, partials, max_norm, norm_out, stream); break;
+            case BT_BF16: e = launch_typed<BT_BF16>(t, m, tiles, scale, partial, partials, max_norm, norm_out, stream); break;
+            default: e = launch_typed<BT_F64>(t, m, tiles, scale, partial, partials, max_norm, norm_out, stream); break;
+            }
+            if (e != cudaSuccess) return e;
+            norm_out = nullptr;
+            m = 0, tiles = 0;
+        }
+        if (mine != 0) {
+            t[m++] = GradTensor{items[k].dense, items[k].y_out, items[k].n};
+            tiles += mine;
+        }
+    }
+    return cudaSuccess;
+}
+
+bool any_element(const bt_batch_item *items, uint32_t count)
+{
+    for (uint32_t k = 0; k < count; ++k)
+        if (items[k].n != 0) return true;
+    return false;
+}
+
+// Bytes for the partial sums of the launches that `pass` makes at most: a group ends at kMany tensors, or where its tiles no
+// longer fit 32 bits (elements of 8 bytes: the most tiles).  n(k): the elements of tensor k.
+template <typename N>
+size_t workspace_of(uint32_t count, const N &n)
+{
+    uint64_t groups = 1, in_group = 0, tiles = 0;
+    for (uint32_t k = 0; k < count; ++k) {
+        if (n(k) == 0) continue;
+        const uint64_t mine = tiles_of(n(k), 8);
+        if (in_group == kMany || tiles + mine > 0xFFFFFFF0ull) ++groups, in_group = 0, tiles = 0;
+        ++in_group;
+        tiles += mine;
+    }
+    return groups * kMaxCtas * sizeof(double);
+}
+
+int check_workspace(const bt_batch_item *items, uint32_t count, const void *workspace, size_t workspace_bytes)
+{
+    if (!workspace) return BT_ERR_NULL;
+    if (!on_boundary(workspace, 16)) return BT_ERR_ALIGN;
+    return workspace_bytes < workspace_of(count, [=](uint32_t k) { return items[k].n; }) ? BT_ERR_WORKSPACE : BT_OK;
+}
+
+}  // namespace
+}  // namespace bt
+
+extern "C" {
+
+size_t bt_grad_workspace_bytes(const uint64_t *n, uint32_t count)
+{
+    return bt::workspace_of(n ? count : 0, [=](uint32_t k) { return n[k]; });
+}
+
+int bt_grad_norm_batch(const bt_batch_item *items, uint32_t count, int dtype, int accumulate, double *sumsq, float *norm_out, void *workspace,
+                       size_t workspace_bytes, void *stream)
+{
+    int st = bt::check_items(items, count, dtype, false);
+    if (st != BT_OK) return st;
+    if (!sumsq && (accumulate || !norm_out)) return BT_ERR_NULL;
+    if (!bt::on_boundary(sumsq, 8) || !bt::on_boundary(norm_out, 4)) return BT_ERR_ALIGN;
+    st = bt::check_workspace(items, count, workspace, workspace_bytes);
+    if (st != BT_OK) return st;
+    cudaStream_t s        = static_cast<cudaStream_t>(stream);
+    double      *partial  = static_cast<double *>(workspace);
+    uint32_t     partials = 0;
+    if (bt::pass(items, count, dtype, false, partial, partials, 0.0f, nullptr, s) != cudaSuccess) return BT_ERR_CUDA;
+    return bt::launch(bt::finish_kernel, 1, bt::kThreads, 0, s, partial, partials, sumsq, accumulate, norm_out) == cudaSuccess ? BT_OK : BT_ERR_CUDA;
+}
+
+int bt_grad_scale_batch(const bt_batch_item *items, uint32_t count, int dtype, float max_norm, const double *sumsq, void *stream)
+{
+    const int st = bt::check_items(items, count, dtype, true);
+    if (st != BT_OK) return st;
+    if (!sumsq) return BT_ERR_NULL;
+    if (!bt::on_boundary(sumsq, 8)) return BT_ERR_ALIGN;
+    if (!(max_norm >= 0.0f)) return BT_ERR_SHAPE;
+    uint32_t partials = 1;                                             // the sum itself is the one partial sum
+    return bt::pass(items, count, dtype, true, const_cast<double *>(sumsq), partials, max_norm, nullptr, static_cast<cudaStream_t>(stream)) == cudaSuccess
+               ? BT_OK
+               : BT_ERR_CUDA;
+}
+
+int bt_grad_clip_batch(const bt_batch_item *items, uint32_t count, int dtype, float max_norm, float *norm_out, void *workspace,
+                       size_t workspace_bytes, void *stream)
+{
+    int st = bt::check_items(items, count, dtype, true);
+    if (st != BT_OK) return st;
+    if (!bt::on_boundary(norm_out, 4)) return BT_ERR_ALIGN;
+    if (!(max_norm >= 0.0f)) return BT_ERR_SHAPE;
+    st = bt::check_workspace(items, count, workspace, workspace_bytes);
+    if (st != BT_OK) return st;
+    cudaStream_t s        = static_cast<cudaStream_t>(stream);
+    double      *partial  = static_cast<double *>(workspace);
+    uint32_t     partials = 0;
+    if (!bt::any_element(items, count)) {                              // the norm of nothing is 0
+        if (!norm_out) return BT_OK;
+        return bt::launch(bt::finish_kernel, 1, bt::kThreads, 0, s, partial, 0u, nullptr, 0, norm_out) == cudaSuccess ? BT_OK : BT_ERR_CUDA;
+    }
+    if (bt::pass(items, count, dtype, false, partial, partials, 0.0f, nullptr, s) != cudaSuccess) return BT_ERR_CUDA;
+    return bt::pass(items, count, dtype, true, partial, partials, max_norm, norm_out, s) == cudaSuccess ? BT_OK : BT_ERR_CUDA;
+}
+
+}  // extern "C"

@@ -1,0 +1,198 @@
+"""What the calls of the transformer-block operators refuse, before anything is launched (no GPU needed: fake addresses that
+no kernel sees)."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2110_15362_b200 import binding as B
+from paper_2110_15362_b200 import build
+
+A = 0x10000
+OK, NULL, DTYPE, ALIGN, WORKSPACE, TOO_LARGE, SHAPE = (B.BT_OK, B.BT_ERR_NULL, B.BT_ERR_DTYPE, B.BT_ERR_ALIGN, B.BT_ERR_WORKSPACE,
+                                                       B.BT_ERR_TOO_LARGE, B.BT_ERR_SHAPE)
+
+
+@pytest.fixture(scope="module")
+def L():
+    build.build_library()
+    return B.lib()
+
+
+def glu_fwd(L, **kw):
+    a = dict(x=A, wg=A, wu=A, rows=8, d=16, ff=32, dt=B.BT_BF16, act=1, h=A, g=A, u=A, ws=A, wsb=1 << 40, st=A)
+    a.update(kw)
+    return L.bt_glu_fwd(a["x"], a["rows"], a["d"], a["ff"], a["dt"], a["act"], a["wg"], a["wu"], a["h"], a["g"], a["u"], a["ws"], a["wsb"],
+                        a["st"], None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dt=7), DTYPE), (dict(d=0), SHAPE), (dict(ff=0), SHAPE), (dict(act=-1), SHAPE), (dict(act=4), SHAPE), (dict(x=None), NULL),
+    (dict(wg=None), NULL), (dict(wu=None), NULL), (dict(h=None), NULL), (dict(x=A + 2), ALIGN), (dict(wg=A + 8), ALIGN), (dict(h=A + 4), ALIGN),
+    (dict(g=A + 8), ALIGN), (dict(u=A + 8), ALIGN), (dict(st=A + 2), ALIGN), (dict(ws=A + 4), ALIGN), (dict(d=(1 << 24) + 1), TOO_LARGE),
+    (dict(ff=(1 << 24) + 1), TOO_LARGE), (dict(rows=1 << 31), TOO_LARGE), (dict(rows=0, st=None, x=None, h=None), OK)])
+def test_glu_forward(L, kw, status):
+    assert glu_fwd(L, **kw) == status
+
+
+def glu_bwd(L, **kw):
+    a = dict(dh=A, g=A, u=A, x=A, wg=A, wu=A, rows=8, d=16, ff=32, dt=B.BT_BF16, act=1, dx=A, dwg=A, dwu=A, ws=A, wsb=1 << 40, st=A)
+    a.update(kw)
+    return L.bt_glu_bwd(a["dh"], a["rows"], a["d"], a["ff"], a["dt"], a["act"], a["g"], a["u"], a["x"], a["wg"], a["wu"], a["dx"], a["dwg"],
+                        a["dwu"], a["ws"], a["wsb"], a["st"], None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dt=4), DTYPE), (dict(d=0), SHAPE), (dict(act=9), SHAPE), (dict(dh=None), NULL), (dict(g=None), NULL), (dict(u=None), NULL),
+    (dict(x=None), NULL), (dict(wg=None), NULL), (dict(dwg=None), NULL), (dict(dwu=None), NULL), (dict(dx=None, dwg=None, dwu=None), NULL),
+    (dict(ws=None), NULL), (dict(wsb=0), WORKSPACE), (dict(dx=A + 8), ALIGN), (dict(dwu=A + 2), ALIGN), (dict(st=A + 1), ALIGN),
+    (dict(rows=1 << 31), TOO_LARGE), (dict(rows=0, dwg=None, dwu=None, st=None), OK)])
+def test_glu_backward(L, kw, status):
+    assert glu_bwd(L, **kw) == status
+
+
+@pytest.mark.parametrize("dtype,es", [(B.BT_F32, 4), (B.BT_F16, 2), (B.BT_BF16, 2), (B.BT_F64, 8)])
+def test_glu_workspace(L, dtype, es):
+    assert L.bt_glu_workspace_bytes(100, 64, 96, dtype, 1) >= 2 * 100 * 96 * es       # the two slopes
+    assert L.bt_glu_workspace_bytes(100, 64, 96, 11, 1) == 0
+    short = L.bt_glu_workspace_bytes(100, 64, 96, dtype, 1) - 1
+    assert glu_bwd(L, rows=100, d=64, ff=96, dt=dtype, wsb=short) == WORKSPACE
+
+
+def norm_fwd(L, **kw):
+    a = dict(x=A, f=A, gate=A, wpost=A, wpre=A, rows=8, d=16, gr=8, dt=B.BT_BF16, scale=1.0, eps=1e-6, y=A, n=A)
+    a.update(kw)
+    return L.bt_block_norm_fwd(a["x"], a["rows"], a["d"], a["gr"], a["dt"], a["scale"], a["eps"], a["f"], a["gate"], a["wpost"], a["wpre"],
+                               a["y"], a["n"], None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(dt=5), DTYPE), (dict(d=0), SHAPE), (dict(gr=0), SHAPE), (dict(eps=-1.0), SHAPE), (dict(eps=float("nan")), SHAPE),
+    (dict(scale=float("nan")), SHAPE), (dict(x=None), NULL), (dict(f=None), NULL), (dict(f=None, gate=None, wpost=None), NULL),
+    (dict(y=None), NULL), (dict(n=None), NULL), (dict(wpre=None), NULL), (dict(x=A + 8), ALIGN), (dict(gate=A + 2), ALIGN), (dict(n=A + 4), ALIGN),
+    (dict(y=A + 4), ALIGN), (dict(d=(1 << 24) + 1), TOO_LARGE), (dict(rows=1 << 40), TOO_LARGE), (dict(rows=0, x=None), OK)])
+def test_block_norm_forward(L, kw, status):
+    assert norm_fwd(L, **kw) == status
+
+
+def test_block_norm_backward(L, monkeypatch):
+    def call(**kw):
+        a = dict(x=A, f=A, gate=A, wpost=A, wpre=A, dn=A, dy=A, rows=8, d=16, gr=8, dt=B.BT_BF16, scale=1.0, eps=1e-6, dx=A, df=A, dgate=A,
+                 dwpost=A, dwpre=A, ws=A, wsb=1 << 40)
+        a.update(kw)
+        return L.bt_block_norm_bwd(a["x"], a["rows"], a["d"], a["gr"], a["dt"], a["scale"], a["eps"], a["f"], a["gate"], a["wpost"], a["wpre"],
+                                   a["dn"], a["dy"], a["dx"], a["df"], a["dgate"], a["dwpost"], a["dwpre"], a["ws"], a["wsb"], None)
+    assert call(dt=5) == DTYPE and call(gr=0) == SHAPE and call(eps=-1.0) == SHAPE
+    assert call(x=None) == NULL and call(gate=None) == NULL and call(wpost=None) == NULL and call(wpre=None) == NULL
+    assert call(f=None) == NULL and call(dn=None) == NULL
+    assert call(dn=None, wpre=None, dwpre=None, dy=None) == NULL
+    assert call(dx=A + 8) == ALIGN and call(dwpre=A + 8) == ALIGN and call(ws=A + 8) == ALIGN and call(dy=A + 2) == ALIGN
+    assert call(rows=0, dwpost=None, dwpre=None) == OK
+
+
+def grad_items(**kw):
+    items = (B.BatchItem * 2)()
+    for it in items:
+        it.dense, it.y_out, it.n = A, A, 100
+    for k, v in kw.items():
+        setattr(items[1], k, v)
+    return items
+
+
+@pytest.mark.parametrize("call", ["clip", "norm", "scale"])
+def test_gradient_calls(L, call):
+    def go(items=None, count=2, dt=B.BT_F32, max_norm=1.0, sumsq=A, norm=A, ws=A, wsb=1 << 30, accumulate=0):
+        items = grad_items() if items is None else items
+        if call == "clip":
+            return L.bt_grad_clip_batch(items, count, dt, max_norm, norm, ws, wsb, None)
+        if call == "norm":
+            return L.bt_grad_norm_batch(items, count, dt, accumulate, sumsq, norm, ws, wsb, None)
+        return L.bt_grad_scale_batch(items, count, dt, max_norm, sumsq, None)
+    assert go(dt=9) == DTYPE and go(items=grad_items(dense=None)) == NULL and go(items=grad_items(dense=A + 4)) == ALIGN
+    assert go(items=grad_items(n=(1 << 46) + 1)) == TOO_LARGE
+    assert L.bt_grad_scale_batch(None, 2, B.BT_F32, 1.0, A, None) == NULL
+    if call != "norm":
+        assert go(items=grad_items(y_out=None)) == NULL and go(items=grad_items(y_out=A + 8)) == ALIGN
+        assert go(max_norm=-1.0) == SHAPE and go(max_norm=float("nan")) == SHAPE
+    if call != "scale":
+        assert go(norm=A + 2) == ALIGN and go(ws=None) == NULL and go(ws=A + 8) == ALIGN and go(wsb=8) == WORKSPACE
+    if call != "clip":
+        assert go(sumsq=A + 4) == ALIGN
+    if call == "norm":
+        assert go(sumsq=None, accumulate=1) == NULL and go(sumsq=None, norm=None) == NULL
+    if call == "scale":
+        assert go(sumsq=None) == NULL and go(count=0) == OK
+
+
+def test_gradient_workspace(L):
+    few, many = L.bt_grad_workspace_bytes((ctypes.c_uint64 * 3)(1, 2, 3), 3), B.bt_grad_workspace_bytes([5] * 3000)
+    assert 0 < few < many
+    assert B.bt_grad_workspace_bytes([]) > 0 and L.bt_grad_workspace_bytes(None, 0) > 0
+
+
+def test_what_the_binding_refuses():
+    x, w, h = torch.zeros(4, 16), torch.zeros(32, 16), torch.zeros(4, 32)
+    with pytest.raises(ValueError, match="h must have the shape"):
+        B.bt_glu_fwd(x, w, w, torch.zeros(4, 16), None, None, x)
+    with pytest.raises(ValueError, match="x must have the shape"):
+        B.bt_glu_fwd(torch.zeros(4, 8), w, w, h, None, None, x)
+    with pytest.raises(ValueError, match="w_up must have"):
+        B.bt_glu_fwd(x, w, torch.zeros(16, 32), h, None, None, x)
+    with pytest.raises(ValueError, match="activation"):
+        B.bt_glu_fwd(x, w, w, h, None, None, x, activation="tanh")
+    with pytest.raises(ValueError, match="one element type"):
+        B.bt_glu_fwd(x, w.bfloat16(), w, h, None, None, x)
+    with pytest.raises(ValueError, match="contiguous"):
+        B.bt_glu_fwd(torch.zeros(16, 4).T, w, w, h, None, None, x)
+    with pytest.raises(ValueError, match="element type"):
+        B.bt_glu_fwd(x.long(), w.long(), w.long(), h.long(), None, None, x)
+    with pytest.raises(ValueError, match="grad_w_up must have"):
+        B.bt_glu_bwd(h, h, h, x, w, w, x, w, torch.zeros(16, 32), x)
+    with pytest.raises(ValueError, match="gate must have"):
+        B.bt_block_norm_fwd(x, x, torch.zeros(3, 16), None, torch.zeros(16), torch.zeros(4, 16), torch.zeros(4, 16))
+    with pytest.raises(ValueError, match="w_pre must have"):
+        B.bt_block_norm_fwd(x, x, None, None, torch.zeros(15), torch.zeros(4, 16), torch.zeros(4, 16))
+    with pytest.raises(ValueError, match="another size"):
+        B.grad_items([x, h], [x, x])
+    with pytest.raises(ValueError, match="as many"):
+        B.grad_items([x, h], [x])
+    with pytest.raises(ValueError, match="one element type"):
+        B.grad_items([x, h.half()])
+
+
+def test_items_name_their_tensors():
+    g, y = [torch.zeros(5), torch.zeros(0), torch.zeros(3, 4)], [torch.zeros(5), torch.zeros(0), torch.zeros(12)]
+    items = B.grad_items(g, y)
+    assert [(it.dense or 0, it.y_out or 0, it.n) for it in items] == [(a.data_ptr(), b.data_ptr(), a.numel()) for a, b in zip(g, y)]
+    assert all(it.bitmap is None and it.dev_status is None for it in items)
+    assert len(B.grad_items([])) == 0
+
+
+@pytest.mark.parametrize("name", B.WIDE_CALLS)
+def test_calls_with_two_floats_and_many_words(L, name, tmp_path):
+    """The wide calls pass what ctypes passes: distinct ordinary values for every parameter, in registers and on the stack."""
+    import subprocess
+    fn = getattr(L, name)
+    types = fn.argtypes
+    c_name = {ctypes.c_void_p: "void *", ctypes.c_uint64: "unsigned long long", ctypes.c_int: "int", ctypes.c_float: "float", ctypes.c_size_t: "unsigned long long"}
+    args = ", ".join("%s a%d" % (c_name[t], k) for k, t in enumerate(types))
+    body = "".join("seen[%d] = (double)(unsigned long long)a%d;" % (k, k) if t is not ctypes.c_float else "seen[%d] = a%d;" % (k, k) for k, t in enumerate(types))
+    (tmp_path / "s.c").write_text("double seen[32]; int %s(%s) { %s return 0; }" % (name, args, body))
+    subprocess.check_call(["gcc", "-O1", "-w", "-shared", "-fPIC", "-o", str(tmp_path / "s.so"), str(tmp_path / "s.c")])
+    S = ctypes.CDLL(str(tmp_path / "s.so"))
+    stub = getattr(S, name)
+    stub.argtypes, stub.restype = types, ctypes.c_int
+    at = ctypes.cast(stub, ctypes.c_void_p).value
+    kinds = "".join({ctypes.c_void_p: "p", ctypes.c_float: "f"}.get(t, "n") for t in types[:-1]) + "s"
+    call = B._native_call()(at, kinds, B._through_ctypes(stub, kinds), B.BatchItem)
+    values = []
+    for k, t in enumerate(types):
+        last = k + 1 == len(types)
+        values.append(0x7000 + k if last else torch.zeros(16) if t is ctypes.c_void_p else 0.25 + k if t is ctypes.c_float else 100 + k)
+    assert call(*values) == 0
+    want = [v.data_ptr() if torch.is_tensor(v) else v for v in values]
+    assert list((ctypes.c_double * 32).in_dll(S, "seen"))[:len(types)] == want
+    with pytest.raises((TypeError, ctypes.ArgumentError)):
+        call(*values[:-1])
+    with pytest.raises(AttributeError):
+        call(0x10000, *values[1:])

@@ -1,0 +1,279 @@
+"""The norms around a block, its gate and residual scale, and their gradients against a 64-bit evaluation (bounds: block_util)."""
+import pytest
+import torch
+
+from paper_2110_15362_b200 import binding as B
+from tests.block_util import ACC, DT, HALF, TINY, Buffer, gen, normal, within
+
+pytestmark = pytest.mark.gpu
+KINDS = ["f32", "f16", "bf16", "f64"]
+SCALE, EPS = 0.375, 2.0 ** -20                      # both exact in binary32
+
+# rows, d: one row, one element, every form of the kernels (a warp or a CTA per row, whole vectors or not, rows read again)
+SIZES = [(1, 1), (1, 2048), (5, 7), (3, 64), (37, 72), (130, 256), (33, 520), (19, 1000), (9, 1025), (700, 1024), (6, 4096), (5, 4100), (4, 8192),
+         (3, 8193), (2, 16392), (3, 20001)]
+
+
+def chain(d):
+    """Additions that a sum over a row goes through at most: a thread's own (it takes every 32nd element at least), and the tree."""
+    return d / 32 + 40
+
+
+def make(rows, d, kind, groups=1, seed=0):
+    g = gen(seed)
+    return {"x": normal(g, (rows, d), kind, 1.0, 0.2), "f": normal(g, (rows, d), kind, 2.0), "gate": normal(g, (groups, d), kind, 0.3, 0.5),
+            "w_post": normal(g, (d,), kind, 0.2, 1.0), "w_pre": normal(g, (d,), kind, 0.2, 1.0), "dn": normal(g, (rows, d), kind, 0.5),
+            "dy": normal(g, (rows, d), kind, 0.5)}
+
+
+def spread(gate, rows):
+    return 1.0 if gate is None else gate.double().repeat_interleave(rows // gate.shape[0], 0)
+
+
+def dbl(t):
+    return None if t is None else t.double()
+
+
+def forward(t, parts, in_place=False):
+    rows, d = t["x"].shape
+    have = {k: t[k] if k in parts else None for k in ("f", "gate", "w_post", "w_pre")}
+    y = Buffer((rows, d), t["x"].dtype) if have["f"] is not None else None
+    n = Buffer((rows, d), t["x"].dtype) if have["w_pre"] is not None else None
+    x, f = t["x"], have["f"]
+    if in_place:                                    # x_out over x, n_out over f
+        y.t.copy_(x), n.t.copy_(f)
+        x, f = y.t, n.t
+    B.bt_block_norm_fwd(x, f, have["gate"], have["w_post"], have["w_pre"], None if y is None else y.t, None if n is None else n.t,
+                        scale=SCALE, eps=EPS)
+    torch.cuda.synchronize()
+    assert all(b is None or b.intact() for b in (y, n))
+    return None if y is None else y.t, None if n is None else n.t
+
+
+def check_forward(t, parts, kind, got):
+    x, f, gate, w_post, w_pre = (dbl(t[k]) if k in parts else None for k in ("x", "f", "gate", "w_post", "w_pre"))
+    x = t["x"].double()
+    rows, d = x.shape
+    u, ey, y = ACC[kind], 0.0, x
+    if f is not None:
+        p = f
+        if w_post is not None:
+            p = f / torch.sqrt((f * f).mean(-1, keepdim=True) + EPS) * w_post
+        branch = SCALE * spread(t["gate"] if gate is not None else None, rows) * p
+        y = x + branch
+        ey = branch.abs() * (chain(d) + 10) * u + (x.abs() + branch.abs()) * u
+        within("x_out", got[0], y, y.abs() * HALF[kind] + 1.01 * ey + TINY[kind])
+    if w_pre is not None:
+        ms = (y * y).mean(-1, keepdim=True) + EPS
+        r = 1 / torch.sqrt(ms)
+        n = y * r * w_pre
+        # the factor moves by half the relative error of the mean square: its own sum, and the elements' errors
+        er = 0.5 * (chain(d) + 8) * u + ((2 * y.abs() * ey).mean(-1, keepdim=True) / ms if f is not None else 0.0) + 4 * u
+        within("n", got[1], n, n.abs() * (HALF[kind] + 1.05 * er + 4 * u) + (ey * r * w_pre.abs() * 1.01 if f is not None else 0.0) + TINY[kind])
+
+
+PARTS = [("f", "gate", "w_post", "w_pre"), ("f", "w_post", "w_pre"), ("f", "gate", "w_pre"), ("f", "w_pre"), ("w_pre",), ("f", "gate", "w_post"), ("f",)]
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", SIZES)
+def test_forward(size, kind):
+    t = make(*size, kind)
+    check_forward(t, PARTS[0], kind, forward(t, PARTS[0]))
+    assert all(torch.equal(a, b) for a, b in zip(forward(t, PARTS[0], in_place=True), forward(t, PARTS[0])))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("parts", PARTS)
+@pytest.mark.parametrize("size", [(24, 64), (12, 1000), (6, 2048), (3, 16400)])
+def test_forward_of_some_parts(size, parts, kind):
+    t = make(*size, kind, groups=3, seed=4)
+    check_forward(t, parts, kind, forward(t, parts))
+
+
+def backward(t, parts, outputs=("x", "f", "gate", "w_post", "w_pre"), dn=True, dy=True):
+    rows, d = t["x"].shape
+    have = {k: t[k] if k in parts else None for k in ("f", "gate", "w_post", "w_pre")}
+    out = {k: Buffer(t[k].shape, t["x"].dtype) if k in outputs and (k == "x" or have[k] is not None) else None for k in ("x", "f", "gate", "w_post", "w_pre")}
+    if not dn:
+        have["w_pre"] = out["w_pre"] = None
+    ws = B.new_block_norm_workspace(rows, d, 1, t["x"].dtype)
+    ws.fill_(0xA5)
+    B.bt_block_norm_bwd(t["x"], have["f"], have["gate"], have["w_post"], have["w_pre"], t["dn"] if have["w_pre"] is not None else None,
+                        t["dy"] if dy else None, *[None if out[k] is None else out[k].t for k in ("x", "f", "gate", "w_post", "w_pre")], ws,
+                        scale=SCALE, eps=EPS)
+    torch.cuda.synchronize()
+    assert all(b is None or b.intact() for b in out.values())
+    return {k: b.t for k, b in out.items() if b is not None}
+
+
+def check_backward(t, parts, kind, got, dn=True, dy=True):
+    x = t["x"].double()
+    rows, d = x.shape
+    u, c = ACC[kind], chain(d) + 16
+    f, gate, w_post = (dbl(t[k]) if k in parts else None for k in ("f", "gate", "w_post"))
+    w_pre = t["w_pre"].double() if "w_pre" in parts and dn else None
+    gy = t["dy"].double() if dy else torch.zeros_like(x)
+    gn = t["dn"].double() if w_pre is not None else torch.zeros_like(x)
+    wn = gn * w_pre if w_pre is not None else torch.zeros_like(x)
+    r = 1 / torch.sqrt((x * x).mean(-1, keepdim=True) + EPS)
+    m = (wn * x).mean(-1, keepdim=True)
+    tt = gy + r * wn - r ** 3 * m * x
+    # every factor off by c u of its own, the mean by c u of the mean of sizes
+    et = c * u * (gy.abs() + 2 * r * wn.abs() + 4 * r ** 3 * (wn * x).abs().mean(-1, keepdim=True) * x.abs())
+    H, T = HALF[kind], TINY[kind]
+    within("dx", got["x"], tt, tt.abs() * H + et + T)
+    n_sum = rows + 64
+    if "w_pre" in got:
+        terms = gn * x * r
+        ref = terms.sum(0)
+        within("dw_pre", got["w_pre"], ref, ref.abs() * H + (c + n_sum) * u * terms.abs().sum(0) + T)
+    if f is None:
+        return
+    gs = spread(t["gate"] if gate is not None else None, rows)
+    rf = 1 / torch.sqrt((f * f).mean(-1, keepdim=True) + EPS) if w_post is not None else torch.ones(rows, 1, dtype=torch.float64, device="cuda")
+    wp = w_post if w_post is not None else torch.ones(d, dtype=torch.float64, device="cuda")
+    fh = f * rf
+    e, ee = SCALE * tt, SCALE * et
+    dp, edp = e * gs, ee * abs(gs) + 4 * u * (e * gs).abs()
+    if "f" in got:
+        if w_post is None:
+            df, b = dp, edp
+        else:
+            q = SCALE * gs * wp * f
+            mean = (tt * q).mean(-1, keepdim=True)
+            sizes = ((gy.abs() + r * wn.abs() + r ** 3 * (wn * x).abs().mean(-1, keepdim=True) * x.abs()) * q.abs()).mean(-1, keepdim=True)
+            df = rf * (dp * wp) - rf ** 3 * mean * f
+            b = rf * edp * wp.abs() + c * u * (rf * (dp * wp).abs()) + rf ** 3 * f.abs() * 6 * c * u * sizes
+        within("df", got["f"], df, df.abs() * H + 1.05 * b + T)
+    if "w_post" in got:
+        terms = dp * fh
+        ref = terms.sum(0)
+        within("dw_post", got["w_post"], ref, ref.abs() * H + (edp * fh.abs()).sum(0) * 1.05 + (c + n_sum) * u * terms.abs().sum(0) + T)
+    if "gate" in got:
+        groups = t["gate"].shape[0]
+        terms, errs = e * fh * wp, ee * (fh * wp).abs()
+        fold = lambda v: v.view(groups, rows // groups, d).sum(1)  # noqa: E731
+        ref = fold(terms)
+        within("dgate", got["gate"], ref, ref.abs() * H + 1.05 * fold(errs) + (c + n_sum) * u * fold(terms.abs()) + T)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", SIZES)
+def test_backward(size, kind):
+    t = make(*size, kind, seed=2)
+    check_backward(t, PARTS[0], kind, backward(t, PARTS[0]))
+
+
+# groups that end inside the CTAs' chunks of rows, cross them, cross several of them, one row each, one group
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f64"])
+@pytest.mark.parametrize("rows,groups", [(6000, 1), (6000, 6000), (6000, 3000), (6000, 5), (6000, 400), (6001, 1), (5999, 7), (13000, 2), (24, 8)])
+@pytest.mark.parametrize("d", [64, 72, 33, 1000, 2048])
+def test_gate_groups(rows, groups, d, kind):
+    if rows % groups:
+        groups = 1 if rows == 6001 else 857              # 5999 = 7 * 857
+    t = make(rows, d, kind, groups=groups, seed=6)
+    check_backward(t, PARTS[0], kind, backward(t, PARTS[0]))
+
+
+def test_gate_groups_in_long_rows():
+    for groups in (1, 10, 50, 150):
+        t = make(150, 16392, "f32", groups=groups, seed=9)
+        check_backward(t, PARTS[0], "f32", backward(t, PARTS[0]))
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("parts", [p for p in PARTS if "w_pre" in p])
+@pytest.mark.parametrize("size", [(24, 64), (12, 1000), (6, 2048), (3, 16400)])
+def test_backward_of_some_parts(size, parts, kind):
+    t = make(*size, kind, groups=3, seed=7)
+    check_backward(t, parts, kind, backward(t, parts))
+    check_backward(t, parts, kind, backward(t, parts, dy=False), dy=False)
+    check_backward(t, parts, kind, backward(t, parts, dn=False), dn=False)
+    whole = backward(t, parts)
+    for k in whole:
+        only = backward(t, parts, outputs=(k,))
+        assert set(only) == {k} and torch.equal(only[k], whole[k]), k
+
+
+def test_backward_against_differences():
+    rows, d = 6, 20
+    t = make(rows, d, "f64", groups=2, seed=13)
+    f0 = forward(t, PARTS[0])
+    a, b = normal(gen(14), (rows, d), "f64"), normal(gen(15), (rows, d), "f64")
+
+    def loss():
+        y, n = forward(t, PARTS[0])
+        return float((y * a).sum() + (n * b).sum())
+
+    saved = dict(t, x=f0[0], dy=a, dn=b)
+    got = backward(saved, PARTS[0])
+    step = 1e-5
+    for k in ("x", "f", "gate", "w_post", "w_pre"):
+        flat, grad = t[k].view(-1), got[k].view(-1)
+        for i in range(0, flat.numel(), 7):
+            old = flat[i].item()
+            flat[i] = old + step
+            up = loss()
+            flat[i] = old - step
+            down = loss()
+            flat[i] = old
+            # third derivatives below 1e3: 1e3 step^2 / 6; rounding 1e-13 / step
+            assert abs((up - down) / (2 * step) - float(grad[i])) < 1e-7, (k, i)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("d", [64, 1000, 2048, 16400])
+def test_rows_of_zeros_infinities_and_nans(kind, d):
+    """A row of zeros has the finite factor 1 / sqrt(eps); a NaN or an infinity stays in its row."""
+    t = make(8, d, kind, seed=17)
+    t["x"][2], t["f"][2] = 0, 0
+    check_forward(t, PARTS[0], kind, forward(t, PARTS[0]))
+    clean = forward(t, PARTS[0])
+    t["x"][5, 3], t["f"][6, 1] = float("nan"), float("inf")
+    keep = torch.tensor([0, 1, 2, 3, 4, 7], device="cuda")
+    for a, b in zip(forward(t, PARTS[0]), clean):
+        assert torch.equal(a[keep], b[keep])
+        assert torch.isnan(a[5]).any()
+    y, _ = forward(t, PARTS[0])
+    assert torch.isnan(y[6, 1])                       # inf * 0
+
+
+def test_no_rows():
+    t = make(1, 64, "f32")
+    e = t["x"][:0]
+    B.bt_block_norm_fwd(e, e, None, None, t["w_pre"], e, e)
+    dw = [torch.ones_like(t["w_pre"]) for _ in range(2)]
+    B.bt_block_norm_bwd(e, e, None, t["w_post"], t["w_pre"], e, e, e, e, None, *dw, None)
+    torch.cuda.synchronize()
+    assert not dw[0].any() and not dw[1].any()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+def test_streams_graphs_and_repeats(kind):
+    t = make(3000, 520, kind, groups=3, seed=23)
+    want = backward(t, PARTS[0])
+    out = {k: torch.empty_like(v) for k, v in want.items()}
+    ws = B.new_block_norm_workspace(3000, 520, 3, DT[kind])
+
+    def go(stream=None):
+        B.bt_block_norm_bwd(t["x"], t["f"], t["gate"], t["w_post"], t["w_pre"], t["dn"], t["dy"], *[out[k] for k in ("x", "f", "gate", "w_post", "w_pre")],
+                            ws, scale=SCALE, eps=EPS, stream=stream)
+
+    def check():
+        torch.cuda.synchronize()
+        assert all(torch.equal(out[k], want[k]) for k in want)
+        for v in out.values():
+            v.zero_()
+        torch.cuda.synchronize()
+
+    go(), check()
+    go(torch.cuda.Stream()), check()
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for g in graphs:
+        with torch.cuda.graph(g):
+            go()
+    for _ in range(3):
+        for g in graphs:
+            g.replay()
+        check()

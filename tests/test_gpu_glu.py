@@ -1,0 +1,240 @@
+"""The gated feed-forward block and its gradients against a 64-bit evaluation of the formulas (bounds: block_util)."""
+import math
+
+import pytest
+import torch
+
+from paper_2110_15362_b200 import binding as B
+from tests.block_util import ACC, DT, HALF, TINY, Buffer, gen, normal, within
+
+pytestmark = pytest.mark.gpu
+ACTS = list(B.ACT_CODE)
+KINDS = ["f32", "f16", "bf16", "f64"]
+K2 = math.sqrt(2 / math.pi)
+
+# rows, d_in, d_ff: one token, tiles cut by every axis, dimensions of whole vectors and not, one element
+SIZES = [(1, 64, 128), (1, 1, 1), (3, 8, 8), (5, 72, 136), (64, 64, 64), (65, 129, 67), (100, 200, 300), (129, 256, 264), (257, 520, 392),
+         (7, 1032, 2056), (300, 96, 1000)]
+
+
+def act64(g, act):
+    """act(g), act'(g), and what multiplies the error of g and of the functions in each (sizes of their terms)."""
+    if act == "relu":
+        on = ~(g <= 0)
+        return torch.where(on, g, 0.0), on.double()
+    if act == "silu":
+        s = torch.sigmoid(g)
+        return g * s, s * (1 + g * (1 - s))
+    if act == "gelu":
+        c = 0.5 * torch.erfc(-g * math.sqrt(0.5))
+        return g * c, c + g * torch.exp(-0.5 * g * g) / math.sqrt(2 * math.pi)
+    s = torch.sigmoid(2 * K2 * (g + 0.044715 * g ** 3))
+    return g * s, s + g * s * (1 - s) * 2 * K2 * (1 + 3 * 0.044715 * g * g)
+
+
+def act_error(g, kind):
+    """Error of act and act' as they are computed: a dozen operations, each ACC relative to terms of at most (1 + |g|) ... and of
+    exp, whose argument (at most 2|g| + 0.08|g|^3, or g^2) is itself rounded; act and act' are the sizes 1 + |g| apart."""
+    z = 2 * g.abs() + 0.08 * g.abs() ** 3 + g * g
+    return (16 + torch.clamp(z, max=60.0)) * ACC[kind] * (1 + g.abs())
+
+
+def make(rows, d, ff, kind, seed=0):
+    g = gen(seed)
+    return normal(g, (rows, d), kind), normal(g, (ff, d), kind, d ** -0.5), normal(g, (ff, d), kind, d ** -0.5)
+
+
+def forward(x, wg, wu, act, save=True):
+    rows, ff = x.shape[0], wg.shape[0]
+    out = [Buffer((rows, ff), x.dtype) for _ in range(3 if save else 1)]
+    status = torch.full((1,), -1, dtype=torch.int32, device="cuda")
+    ws = B.new_glu_workspace(rows, x.shape[1], ff, x.dtype)
+    ws.fill_(0xA5)
+    B.bt_glu_fwd(x, wg, wu, out[0].t, out[1].t if save else None, out[2].t if save else None, ws, status, activation=act)
+    torch.cuda.synchronize()
+    assert int(status) == B.BT_OK and all(b.intact() for b in out)
+    return [b.t for b in out]
+
+
+def check_forward(x, wg, wu, act, kind, got):
+    xd, gd, ud = x.double(), wg.double(), wu.double()
+    d = x.shape[1]
+    g, u = xd @ gd.T, xd @ ud.T
+    eg, eu = (d + 2) * ACC[kind] * (xd.abs() @ gd.abs().T), (d + 2) * ACC[kind] * (xd.abs() @ ud.abs().T)
+    a, da = act64(g, act)
+    # the slope of every activation here is below 1.2 in size
+    ea = 1.2 * eg + (0 if act == "relu" else act_error(g, kind))
+    eh = ea * (u.abs() + eu) + a.abs() * eu
+    within("h", got[0], a * u, (a * u).abs() * (HALF[kind] + ACC[kind]) + 1.01 * eh + TINY[kind])
+    if len(got) > 1:
+        ref = a if act == "relu" else g
+        within("g", got[1], ref, ref.abs() * HALF[kind] + 1.01 * eg + TINY[kind])
+        within("u", got[2], u, u.abs() * HALF[kind] + 1.01 * eu + TINY[kind])
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", SIZES)
+def test_forward(size, kind):
+    x, wg, wu = make(*size, kind)
+    act = ACTS[sum(size) % 4]
+    check_forward(x, wg, wu, act, kind, forward(x, wg, wu, act))
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("kind", KINDS)
+def test_activations(act, kind):
+    x, wg, wu = make(33, 64, 96, kind, seed=3)
+    x *= 4                                                          # gates of both signs, out to the flat parts
+    check_forward(x, wg, wu, act, kind, forward(x, wg, wu, act))
+    h, = forward(x, wg, wu, act, save=False)
+    assert torch.equal(h, forward(x, wg, wu, act)[0])               # what is kept for the backward pass changes nothing
+
+
+def backward(dh, g, u, x, wg, wu, act, dx=True, dw=True):
+    rows, ff, d = x.shape[0], wg.shape[0], x.shape[1]
+    out = [Buffer(x.shape, x.dtype) if dx else None, Buffer(wg.shape, x.dtype) if dw else None, Buffer(wu.shape, x.dtype) if dw else None]
+    status = torch.full((1,), -1, dtype=torch.int32, device="cuda")
+    ws = B.new_glu_workspace(rows, d, ff, x.dtype, backward=True)
+    ws.fill_(0xA5)
+    B.bt_glu_bwd(dh, g, u, x, wg, wu, *[None if b is None else b.t for b in out], ws, status, activation=act)
+    torch.cuda.synchronize()
+    assert int(status) == B.BT_OK and all(b is None or b.intact() for b in out)
+    return [None if b is None else b.t for b in out]
+
+
+def check_backward(dh, g, u, x, wg, wu, act, kind, got):
+    dhd, gd, ud, xd, wgd, wud = (t.double() for t in (dh, g, u, x, wg, wu))
+    a, da = act64(gd, act)
+    dg, du = dhd * ud * da, dhd * a
+    e = 0 if act == "relu" else act_error(gd, kind)
+    edg = (dg.abs() + (dhd * ud).abs() * e) * (HALF[kind] + 2 * ACC[kind]) + (dhd * ud).abs() * e + TINY[kind]
+    edu = (du.abs() + dhd.abs() * e) * (HALF[kind] + 2 * ACC[kind]) + dhd.abs() * e + TINY[kind]
+    rows, d, ff = x.shape[0], x.shape[1], wg.shape[0]
+    if got[0] is not None:
+        dx = dg @ wgd + du @ wud
+        b = edg @ wgd.abs() + edu @ wud.abs() + (2 * ff + 2) * ACC[kind] * (dg.abs() @ wgd.abs() + du.abs() @ wud.abs())
+        within("dx", got[0], dx, dx.abs() * HALF[kind] + 1.01 * b + TINY[kind])
+    if got[1] is not None:
+        for name, have, s, es in (("dwg", got[1], dg, edg), ("dwu", got[2], du, edu)):
+            ref = s.T @ xd
+            b = es.T @ xd.abs() + (rows + 2) * ACC[kind] * (s.abs().T @ xd.abs())
+            within(name, have, ref, ref.abs() * HALF[kind] + 1.01 * b + TINY[kind])
+
+
+def make_backward(rows, d, ff, kind, act, seed=0):
+    x, wg, wu = make(rows, d, ff, kind, seed)
+    r = gen(seed + 100)
+    g, u, dh = normal(r, (rows, ff), kind), normal(r, (rows, ff), kind), normal(r, (rows, ff), kind, 0.1)
+    return dh, g.clamp(min=0) if act == "relu" else g, u, x, wg, wu
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("size", SIZES)
+def test_backward(size, kind):
+    act = ACTS[sum(size) % 4]
+    args = make_backward(*size, kind, act)
+    check_backward(*args, act, kind, backward(*args, act))
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("kind", KINDS)
+def test_backward_of_each_activation_and_of_some_outputs(act, kind):
+    args = make_backward(70, 48, 88, kind, act, seed=5)
+    whole = backward(*args, act)
+    check_backward(*args, act, kind, whole)
+    only_x, only_w = backward(*args, act, dw=False), backward(*args, act, dx=False)
+    assert torch.equal(only_x[0], whole[0]) and all(torch.equal(a, b) for a, b in zip(only_w[1:], whole[1:]))
+
+
+@pytest.mark.parametrize("act", ACTS)
+def test_backward_against_differences(act):
+    """The gradients of L = sum(h * c), as the calls give them in binary64, against central differences of L."""
+    x, wg, wu = make(5, 16, 24, "f64", seed=7)
+    c = normal(gen(8), (5, 24), "f64")
+    _, g, u = forward(x, wg, wu, act)
+    grads = backward(c, g, u, x, wg, wu, act)
+    step = 1e-5
+    for t, grad in zip((x, wg, wu), grads):
+        for k in range(0, t.numel(), 37):
+            old = t.view(-1)[k].item()
+            t.view(-1)[k] = old + step
+            up = (forward(x, wg, wu, act, save=False)[0] * c).sum()
+            t.view(-1)[k] = old - step
+            down = (forward(x, wg, wu, act, save=False)[0] * c).sum()
+            t.view(-1)[k] = old
+            # third derivatives of these sums stay below 1e3: 1e3 step^2 / 6; rounding 1e-13 / step
+            assert abs(float((up - down) / (2 * step)) - float(grad.view(-1)[k])) < 1e-7
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_no_rows(kind):
+    x, wg, wu = make(1, 16, 24, kind)
+    empty, none = x[:0], torch.empty(0, 24, dtype=DT[kind], device="cuda")
+    ws = torch.empty(1 << 16, dtype=torch.uint8, device="cuda")
+    status = torch.full((1,), -1, dtype=torch.int32, device="cuda")
+    B.bt_glu_fwd(empty, wg, wu, none, None, None, ws, status)
+    assert int(status) == B.BT_OK
+    dwg, dwu = torch.ones_like(wg), torch.ones_like(wu)
+    status.fill_(-1)
+    B.bt_glu_bwd(none, none, none, empty, wg, wu, empty, dwg, dwu, ws, status)
+    assert int(status) == B.BT_OK and not dwg.any() and not dwu.any()
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("size", [(40, 64, 72), (200, 264, 520)])
+def test_infinities_and_nans(kind, size):
+    """A NaN in a row of x makes that row's outputs NaN and no other; a closed gate's gradients are zero whatever grad_h and u
+    hold there."""
+    rows, d, ff = size
+    x, wg, wu = make(rows, d, ff, kind, seed=11)
+    clean = forward(x, wg, wu, "relu")
+    x[3, 5] = float("nan")
+    for a, b in zip(forward(x, wg, wu, "relu"), clean):
+        assert torch.isnan(a[3]).all()
+        keep = torch.arange(rows, device="cuda") != 3
+        assert torch.equal(a[keep], b[keep])
+    dh, g, u, x, wg, wu = make_backward(rows, d, ff, kind, "relu", seed=12)
+    closed = g == 0
+    want = backward(dh, g, u, x, wg, wu, "relu")
+    dh[closed], u[closed] = float("inf"), float("nan")
+    for a, b in zip(backward(dh, g, u, x, wg, wu, "relu"), want):
+        assert torch.equal(a, b)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_streams_graphs_and_repeats(kind):
+    """The same bits on a side stream, from a replayed graph, and for two captured graphs that share a workspace in one stream."""
+    size = (150, 128, 264)
+    x, wg, wu = make(*size, kind, seed=21)
+    dh, g, u, *_ = make_backward(*size, kind, "silu", seed=21)
+    want_f, want_b = forward(x, wg, wu, "silu"), backward(dh, g, u, x, wg, wu, "silu")
+    ws = B.new_glu_workspace(*size, DT[kind], backward=True)
+    hs = [torch.empty_like(t) for t in want_f]
+    gs = [torch.empty_like(t) for t in want_b]
+
+    def both():
+        B.bt_glu_fwd(x, wg, wu, *hs, ws, activation="silu")
+        B.bt_glu_bwd(dh, g, u, x, wg, wu, *gs, ws, activation="silu")
+
+    def check():
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(hs + gs, want_f + want_b))
+        for t in hs + gs:
+            t.zero_()
+        torch.cuda.synchronize()
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        both()
+    check()
+    B.bt_glu_fwd(x, wg, wu, *hs, ws, activation="silu", stream=side)
+    B.bt_glu_bwd(dh, g, u, x, wg, wu, *gs, ws, activation="silu", stream=side)
+    check()
+    graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+    for graph in graphs:
+        with torch.cuda.graph(graph):
+            both()
+    for _ in range(3):
+        for graph in graphs:
+            graph.replay()
+        check()
