@@ -48,14 +48,19 @@ __device__ __forceinline__ A act_slope(const A g)
 struct GluCall {
     const void *x, *w_gate, *w_up;                 // [rows, d_in], [d_ff, d_in] twice
     void       *h, *g, *u;                         // forward: [rows, d_ff]; g and u may be NULL
-    const void *dg, *du;                           // backward: [rows, d_ff], made by launch_glu_slopes
+    const void *dg, *du;                           // backward: [rows, d_ff], the gradients of g and u
     void       *dx, *dw_gate, *dw_up;              // backward: any may be NULL
     uint64_t    rows, d_in, d_ff;
     int         dtype, act;
     int32_t    *dev_status;
 };
 
-// calls launch(std::integral_constant<int, DT>, std::integral_constant<int, ACT>) for a call's type and activation
+// The products on the tensor cores (bt_glu_mma.cu): types and sizes that they take; forward; backward from c.dg and c.du.
+bool        glu_mma_takes(const GluCall &c);
+cudaError_t launch_glu_mma_fwd(const GluCall &c, cudaStream_t stream);
+cudaError_t launch_glu_mma_bwd(const GluCall &c, cudaStream_t stream);
+
+// calls go(std::integral_constant<int, DT>, std::integral_constant<int, ACT>) for a call's type and activation
 template <int DT, typename F>
 cudaError_t with_act(int act, const F &go)
 {

@@ -1,0 +1,548 @@
+// The gated feed-forward block's products of 16-bit types on the tensor cores (tcgen05, sums in TMEM in binary32).
+//
+// One kernel, three uses (kUse).  A pair of CTAs (cta_group::2) computes tiles of 256 x kN outputs: each CTA holds 128 rows of
+// A and half of B's kN rows, 64 of the summed axis per stage, and the pair's sums of its own 128 rows in its TMEM.
+//
+//   kForward      A = x, B = Wg and Wu: the pair's first CTA brings kN / 2 rows of Wg, the second the same rows of Wu, so that
+//                 columns 0 .. kN/2 of the tile are g and the others u; the epilogue writes act(g) u (and g and u).
+//   kInputGrad    A = dg then du, B = Wg then Wu read along their rows (the summed axis is not the contiguous one): one sum over
+//                 both products.
+//   kWeightGrad   A = dg (or du) and B = x, both read along their rows; the tiles of both gradients in one launch.
+//
+// Per CTA: one thread loads tiles by TMA into a ring of stages, one thread of the pair's first CTA issues the products, eight
+// warps bring sums from TMEM to the output through shared memory and TMA while the next tile is summed into the other half
+// of TMEM.  Rows, columns and depths beyond a tensor are read as zeros and never written (TMA's bounds).  The summed axis and both output
+// axes may have any size; rows of every operand must begin on 16-byte boundaries (d_in and d_ff multiples of 8).
+//
+// Bound by the tensor cores.  Every wait is bounded: a role that gives up reports BT_ERR_TIMEOUT, the others follow, and the
+// CTAs leave together.
+#include <cuda.h>
+
+#include <type_traits>
+
+#include "bt_glu.cuh"
+
+namespace bt {
+namespace {
+
+enum { kForward, kInputGrad, kWeightGrad };
+
+constexpr int kDepth      = 64;                       // of the summed axis per stage: 128 bytes, the widest swizzle
+constexpr int kRows       = 128;                      // of A per CTA
+constexpr int kEpiWarps   = 8;
+constexpr int kThreads    = 32 * (2 + kEpiWarps);     // loader, issuer, epilogue
+constexpr int kStageWords = 32 * kDepth * 2;          // bytes of a warp's staged output: 32 rows of 64 elements
+
+template <int kN>
+struct Shape {
+    static constexpr int kABytes = kRows * kDepth * 2, kBBytes = kN / 2 * kDepth * 2;
+    static constexpr int kStages = kN == 256 ? 6 : 8;
+    static constexpr int kRing   = kStages * (kABytes + kBBytes);
+    static constexpr int kBytes  = kRing + kEpiWarps * kStageWords;
+    static constexpr int kSmem   = kBytes + 1024 + 256;                // room to start on 1024 bytes; barriers
+};
+
+struct MmaArgs {
+    CUtensorMap a[2], b[2], out[3];
+    uint32_t    blocks;                                // of the summed axis, of one product
+    uint32_t    tiles_i, tiles_j, tiles;               // of one output; of all
+    uint32_t    outputs;                               // forward: bit 0 h, bit 1 g, bit 2 u
+    uint64_t    size_i, size_j;                        // of an output
+    int32_t    *dev_status;
+};
+
+// ---------------------------------------------------------------------------------------------- PTX
+__device__ __forceinline__ uint32_t cluster_rank()
+{
+    uint32_t r;
+    asm("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync()
+{
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+// the address of the same word in the pair's first CTA
+__device__ __forceinline__ uint32_t in_first_cta(uint32_t addr)
+{
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr)
+{
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+}
+__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ uint64_t now_ns()
+{
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+__device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap *map, int x, int y, uint32_t bar)
+{
+    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(to),
+                 "l"(map), "r"(x), "r"(y), "r"(bar)
+                 : "memory");
+}
+__device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, uint32_t from)
+{
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(from) : "memory");
+}
+__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+
+__device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"(add ? 1u : 0u)
+        : "memory");
+}
+// both CTAs' barrier at this offset, once the products issued so far are complete
+__device__ __forceinline__ void commit_pair(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+                 "h"(static_cast<uint16_t>(3))
+                 : "memory");
+}
+__device__ __forceinline__ void tmem_load(uint32_t addr, uint32_t (&v)[32])
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]), "=r"(v[10]),
+          "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15]), "=r"(v[16]), "=r"(v[17]), "=r"(v[18]), "=r"(v[19]), "=r"(v[20]),
+          "=r"(v[21]), "=r"(v[22]), "=r"(v[23]), "=r"(v[24]), "=r"(v[25]), "=r"(v[26]), "=r"(v[27]), "=r"(v[28]), "=r"(v[29]), "=r"(v[30]),
+          "=r"(v[31])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tmem_load_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+
+// Shared-memory descriptors of operands in the 128-byte swizzle (atoms of 8 rows of 128 bytes).  Along the summed axis (rows of
+// 64 summed elements): 1024 bytes from one group of 8 rows to the next.  Along the other axis (a row holds 64 of A's or B's
+// rows for one summed element): 1024 bytes to the next 8 summed elements, 8192 to the next 64 rows.
+template <bool kAcross>
+__device__ __forceinline__ uint64_t operand(uint32_t addr)
+{
+    constexpr uint64_t kLeading = kAcross ? 64 * kDepth * 2 : 16;
+    return static_cast<uint64_t>((addr & 0x3FFFFu) >> 4) | (kLeading >> 4) << 16 | static_cast<uint64_t>(1024 >> 4) << 32 |
+           1ull << 46 |                                                 // the descriptors' version on this architecture
+           2ull << 61;                                                  // 128-byte swizzle
+}
+// bytes from the operand of one product to that of the next 16 summed elements
+template <bool kAcross>
+constexpr uint32_t kStep = kAcross ? 16 * 128 : 32;
+
+template <int DT, bool kAcrossA, bool kAcrossB, int kN>
+constexpr uint32_t kInstruction = 1u << 4 |                                                    // sums in binary32
+                                  (DT == BT_BF16 ? 1u : 0u) << 7 | (DT == BT_BF16 ? 1u : 0u) << 10 |   // operands: bfloat16 or binary16
+                                  (kAcrossA ? 1u : 0u) << 15 | (kAcrossB ? 1u : 0u) << 16 |    // which axis is contiguous
+                                  static_cast<uint32_t>(kN / 8) << 17 | static_cast<uint32_t>(256 / 16) << 24;
+
+// ---------------------------------------------------------------------------------------------- waits
+// A CTA's word that says that one of its roles gave up.
+struct Waits {
+    volatile uint32_t *gave_up;
+    int32_t           *dev_status;
+    __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const
+    {
+        if (mbar_try_wait_cluster(bar, parity)) return true;
+        const uint64_t begin = now_ns();
+        for (;;) {
+#pragma unroll 1
+            for (int k = 0; k < 64; ++k)
+                if (mbar_try_wait_cluster(bar, parity)) return true;
+            if (*gave_up) return false;
+            if (now_ns() - begin > kDefaultWaitNs) {
+                *gave_up = 1;
+                if (dev_status) *reinterpret_cast<volatile int32_t *>(dev_status) = BT_ERR_TIMEOUT;
+                return false;
+            }
+        }
+    }
+};
+
+// A ring's position: stage and parity.
+template <int kStages>
+struct Ring {
+    uint32_t stage = 0, phase = 0;
+    __device__ __forceinline__ void next()
+    {
+        if (++stage == kStages) stage = 0, phase ^= 1;
+    }
+};
+
+// ---------------------------------------------------------------------------------------------- kernel
+// tile -> its place.  Groups of 8 tile rows, walked column by column: what is in flight at once shares rows of A and of B in
+// the L2.
+struct Tile {
+    uint32_t which, i, j;
+};
+__device__ __forceinline__ Tile tile_at(const MmaArgs &p, uint32_t t)
+{
+    Tile           r;
+    const uint32_t per = p.tiles_i * p.tiles_j;
+    r.which            = t / per;
+    t -= r.which * per;
+    const uint32_t group = t / (8 * p.tiles_j), first = group * 8;
+    const uint32_t high = p.tiles_i - first < 8 ? p.tiles_i - first : 8;
+    t -= group * 8 * p.tiles_j;
+    r.i = first + t % high;
+    r.j = t / high;
+    return r;
+}
+
+template <int DT>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    if constexpr (DT == BT_BF16) {
+        const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    } else {
+        const __half2 v = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t *>(&v);
+    }
+}
+
+template <int DT, int kUse, int kAct, int kN>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
+glu_mma_kernel(const __grid_constant__ MmaArgs p)
+{
+    using S                     = Shape<kN>;
+    constexpr bool     kAcrossA = kUse == kWeightGrad, kAcrossB = kUse != kForward;
+    constexpr uint32_t kIdesc   = kInstruction<DT, kAcrossA, kAcrossB, kN>;
+    constexpr int      kStages  = S::kStages;
+    extern __shared__ unsigned char raw[];
+    const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
+    // behind the tiles: barriers (full and empty per stage, sums ready and taken per half of TMEM), TMEM's address, the word
+    const uint32_t bars = base + S::kBytes;
+    const auto full = [&](uint32_t s) { return bars + 8 * s; };
+    const auto empty = [&](uint32_t s) { return bars + 8 * (kStages + s); };
+    const auto ready = [&](uint32_t h) { return bars + 8 * (2 * kStages + h); };
+    const auto taken = [&](uint32_t h) { return bars + 8 * (2 * kStages + 2 + h); };
+    unsigned char *const generic   = raw + (base - smem_addr(raw));
+    uint32_t *const      tmem_word = reinterpret_cast<uint32_t *>(generic + S::kBytes + 8 * (2 * kStages + 4));
+    volatile uint32_t   *gave_up   = tmem_word + 1;
+
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, rank = cluster_rank();
+    const Waits    wait{gave_up, p.dev_status};
+    if (threadIdx.x == 0) {
+        uint64_t *const b = reinterpret_cast<uint64_t *>(generic + S::kBytes);
+        for (int s = 0; s < 2 * kStages; ++s) mbar_init(b + s, 1);
+        mbar_init(b + 2 * kStages, 1), mbar_init(b + 2 * kStages + 1, 1);
+        mbar_init(b + 2 * kStages + 2, 2 * kEpiWarps), mbar_init(b + 2 * kStages + 3, 2 * kEpiWarps);
+        *gave_up = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_word)), "r"(2 * kN) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tmem_fence_before();
+    __syncthreads();
+    cluster_sync();
+    tmem_fence_after();
+    const uint32_t tmem = *tmem_word;
+    in_stream_order();
+    if (p.dev_status && kUse == kForward && blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<volatile int32_t *>(p.dev_status) = BT_OK;
+
+    const uint32_t first = blockIdx.x / 2, step = gridDim.x / 2;
+    const uint32_t blocks = p.blocks * (kUse == kInputGrad ? 2 : 1);
+    if (warp == 0) {
+        // ---- loader
+        if (lane == 0) {
+            Ring<kStages> ring;
+            bool          ok = true;
+            for (uint32_t t = first; t < p.tiles && ok; t += step) {
+                const Tile tile = tile_at(p, t);
+                const int  i0 = static_cast<int>(tile.i * 256 + rank * kRows);
+                for (uint32_t k = 0; k < blocks; ++k) {
+                    if (!(ok = wait(empty(ring.stage), ring.phase ^ 1))) break;
+                    const uint32_t a = base + ring.stage * (S::kABytes + S::kBBytes), b = a + S::kABytes;
+                    const uint32_t bar = in_first_cta(full(ring.stage));
+                    // the pair's bytes are expected once, in its first CTA
+                    if (rank == 0)
+                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full(ring.stage)), "r"(2 * (S::kABytes + S::kBBytes)) : "memory");
+                    const uint32_t pair = kUse == kInputGrad ? (k >= p.blocks ? 1u : 0u) : 0u;
+                    const int      k0   = static_cast<int>((k - pair * p.blocks) * kDepth);
+                    if constexpr (kUse == kForward) {
+                        tma_load(a, &p.a[0], k0, i0, bar);
+                        tma_load(b, &p.b[rank], k0, static_cast<int>(tile.j * (kN / 2)), bar);
+                    } else {
+                        const int j0 = static_cast<int>(tile.j * kN + rank * (kN / 2));
+                        if constexpr (kUse == kInputGrad) {
+                            tma_load(a, &p.a[pair], k0, i0, bar);
+                        } else {
+#pragma unroll
+                            for (int v = 0; v < kRows / 64; ++v) tma_load(a + v * 64 * kDepth * 2, &p.a[tile.which], i0 + 64 * v, k0, bar);
+                        }
+#pragma unroll
+                        for (int v = 0; v < kN / 2 / 64; ++v) tma_load(b + v * 64 * kDepth * 2, &p.b[kUse == kInputGrad ? pair : 0], j0 + 64 * v, k0, bar);
+                    }
+                    ring.next();
+                }
+            }
+            // the last products have read their tiles: nothing arrives at this CTA's barriers any more
+            for (uint32_t s = 0; s < kStages && ok; ++s) {
+                ok = wait(empty(ring.stage), ring.phase ^ 1);
+                ring.next();
+            }
+        }
+        __syncwarp();
+    } else if (warp == 1) {
+        // ---- issuer
+        if (rank == 0 && lane == 0) {
+            Ring<kStages> ring;
+            Ring<2>       half;
+            bool          ok = true;
+            for (uint32_t t = first; t < p.tiles && ok; t += step) {
+                if (!(ok = wait(taken(half.stage), half.phase ^ 1))) break;
+                tmem_fence_after();
+                const uint32_t d = tmem + half.stage * kN;
+                for (uint32_t k = 0; k < blocks; ++k) {
+                    if (!(ok = wait(full(ring.stage), ring.phase))) break;
+                    tmem_fence_after();
+                    const uint32_t a = base + ring.stage * (S::kABytes + S::kBBytes), b = a + S::kABytes;
+                    const uint64_t da = operand<kAcrossA>(a), db = operand<kAcrossB>(b);
+#pragma unroll
+                    for (int q = 0; q < kDepth / 16; ++q)
+                        mma_pair(d, da + q * (kStep<kAcrossA> >> 4), db + q * (kStep<kAcrossB> >> 4), kIdesc, k != 0 || q != 0);
+                    commit_pair(empty(ring.stage));
+                    ring.next();
+                }
+                if (!ok) break;
+                commit_pair(ready(half.stage));
+                half.next();
+            }
+        }
+        __syncwarp();
+    } else {
+        // ---- epilogue: a quarter of TMEM's lanes (the warp's number modulo 4) and every second chunk of 64 output columns
+        const uint32_t quarter = warp % 4, turn = (warp - 2) / 4;
+        const uint32_t stage_at = base + S::kRing + (warp - 2) * kStageWords;
+        unsigned char *const stage = generic + S::kRing + (warp - 2) * kStageWords;
+        constexpr uint32_t kChunks = kUse == kForward ? kN / 2 / 64 : kN / 64;
+        constexpr uint32_t kItems  = kUse == kForward ? kChunks * 3 : kChunks;
+        Ring<2> half;
+        for (uint32_t t = first; t < p.tiles; t += step) {
+            const Tile tile = tile_at(p, t);
+            const uint32_t i0 = tile.i * 256 + rank * kRows + quarter * 32;
+            if (!wait(ready(half.stage), half.phase)) break;
+            tmem_fence_after();
+            const uint32_t from = tmem + half.stage * kN + (quarter * 32 << 16);
+            for (uint32_t item = turn; item < kItems; item += 2) {
+                const uint32_t chunk = item % kChunks, what = item / kChunks;
+                const uint32_t j0 = tile.j * (kUse == kForward ? kN / 2 : kN) + chunk * 64;
+                if (kUse == kForward && !(p.outputs >> what & 1)) continue;
+                if (j0 >= p.size_j || i0 >= p.size_i) continue;         // (the whole warp alike)
+                uint32_t packed[32];
+#pragma unroll
+                for (int part = 0; part < 2; ++part) {
+                    uint32_t v[32];
+                    if (kUse == kForward && what == 0) {
+                        uint32_t u[32];
+                        tmem_load(from + chunk * 64 + part * 32, v);
+                        tmem_load(from + kN / 2 + chunk * 64 + part * 32, u);
+                        tmem_load_wait();
+#pragma unroll
+                        for (int c = 0; c < 16; ++c)
+                            packed[part * 16 + c] = pack2<DT>(act_of<kAct>(__uint_as_float(v[2 * c])) * __uint_as_float(u[2 * c]),
+                                                              act_of<kAct>(__uint_as_float(v[2 * c + 1])) * __uint_as_float(u[2 * c + 1]));
+                    } else {
+                        tmem_load(from + (kUse == kForward && what == 2 ? kN / 2 : 0) + chunk * 64 + part * 32, v);
+                        tmem_load_wait();
+                        if (kUse == kForward && kAct == BT_ACT_RELU && what == 1) {
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) v[c] = __float_as_uint(act_of<kAct>(__uint_as_float(v[c])));
+                        }
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) packed[part * 16 + c] = pack2<DT>(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
+                    }
+                }
+                // the staged tile of before has been read; a lane writes its row's eight 16-byte pieces where the swizzle has them
+                if (lane == 0) bulk_wait_read<0>();
+                __syncwarp();
+#pragma unroll
+                for (int c = 0; c < 8; ++c)
+                    *reinterpret_cast<uint4 *>(stage + lane * 128 + ((c ^ (lane & 7)) * 16)) =
+                        make_uint4(packed[4 * c], packed[4 * c + 1], packed[4 * c + 2], packed[4 * c + 3]);
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) {
+                    tma_store(&p.out[kUse == kForward ? what : tile.which], static_cast<int>(j0), static_cast<int>(i0), stage_at);
+                    bulk_commit();
+                }
+            }
+            tmem_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_cluster(in_first_cta(taken(half.stage)));
+            half.next();
+        }
+        if (lane == 0) bulk_wait_all();
+        __syncwarp();
+    }
+    __syncthreads();
+    if (*gave_up) {                                                     // copies and products in flight land within a millisecond
+        const uint64_t begin = now_ns();
+        while (now_ns() - begin < 1000000) {
+        }
+    }
+    __syncwarp();
+    tmem_fence_before();
+    cluster_sync();
+    tmem_fence_after();
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kN) : "memory");
+}
+
+// ---------------------------------------------------------------------------------------------- host side
+using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
+                            const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+// the driver's encoder of tensor maps (host arithmetic), looked up once
+Encode encoder()
+{
+    static const Encode fn = [] {
+        void                           *p = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        if (reported(cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &p, 12000, cudaEnableDefault, &found)) != cudaSuccess ||
+            found != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<Encode>(p);
+    }();
+    return fn;
+}
+
+// a row-major matrix of 16-bit elements in boxes of 64 columns (128 bytes, swizzled) and box_rows rows
+bool map_of(CUtensorMap &m, int dtype, const void *at, uint64_t rows, uint64_t columns, uint32_t box_rows)
+{
+    const cuuint64_t size[2] = {columns, rows}, stride[1] = {columns * 2};
+    const cuuint32_t box[2] = {64, box_rows}, each[2] = {1, 1};
+    return encoder()(&m, dtype == BT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(at), size, stride,
+                     box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int DT, int kUse, int kAct, int kN>
+cudaError_t start(const MmaArgs &p, cudaStream_t stream, int sms)
+{
+    const auto        kernel = glu_mma_kernel<DT, kUse, kAct, kN>;
+    const cudaError_t e      = reported(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<kN>::kSmem));
+    if (e != cudaSuccess) return e;
+    const uint32_t pairs = static_cast<uint32_t>(sms) / 2;
+    return launch(kernel, 2 * (p.tiles < pairs ? p.tiles : pairs), kThreads, Shape<kN>::kSmem, stream, p);
+}
+
+// tiles of `columns` output columns, for `outputs` outputs of size_i x size_j; false if there are more than 31 bits of them
+bool set_tiles(MmaArgs &p, uint64_t size_i, uint64_t size_j, uint32_t columns, uint32_t outputs)
+{
+    p.size_i = size_i, p.size_j = size_j;
+    p.tiles_i            = static_cast<uint32_t>(round_up_div(size_i, 256));
+    p.tiles_j            = static_cast<uint32_t>(round_up_div(size_j, columns));
+    const uint64_t tiles = static_cast<uint64_t>(p.tiles_i) * p.tiles_j * outputs;
+    p.tiles              = static_cast<uint32_t>(tiles);
+    return tiles < 0x7FFFFFFFull;
+}
+
+// Tiles of 256 or of 128 columns: what the pairs of CTAs take one after the other, in columns.
+uint64_t rounds(uint64_t size_i, uint64_t size_j, uint64_t outputs, uint32_t columns, uint32_t width, int sms)
+{
+    return round_up_div(round_up_div(size_i, 256) * round_up_div(size_j, columns) * outputs, static_cast<uint64_t>(sms) / 2) * width;
+}
+
+template <int DT, int kN>
+cudaError_t forward_of(const GluCall &c, int sms, cudaStream_t stream)
+{
+    MmaArgs p{};
+    bool    ok = map_of(p.a[0], DT, c.x, c.rows, c.d_in, kRows) && map_of(p.b[0], DT, c.w_gate, c.d_ff, c.d_in, kN / 2) &&
+              map_of(p.b[1], DT, c.w_up, c.d_ff, c.d_in, kN / 2) && map_of(p.out[0], DT, c.h, c.rows, c.d_ff, 32);
+    if (c.g) ok = ok && map_of(p.out[1], DT, c.g, c.rows, c.d_ff, 32);
+    if (c.u) ok = ok && map_of(p.out[2], DT, c.u, c.rows, c.d_ff, 32);
+    if (!ok || !set_tiles(p, c.rows, c.d_ff, kN / 2, 1)) return cudaErrorInvalidValue;
+    p.outputs    = 1u | (c.g ? 2u : 0u) | (c.u ? 4u : 0u);
+    p.blocks     = static_cast<uint32_t>(round_up_div(c.d_in, kDepth));
+    p.dev_status = c.dev_status;
+    return with_act<DT>(c.act, [&](auto dt, auto act) { return start<decltype(dt)::value, kForward, decltype(act)::value, kN>(p, stream, sms); });
+}
+
+template <int DT, int kN>
+cudaError_t input_grad_of(const GluCall &c, int sms, cudaStream_t stream)
+{
+    MmaArgs    p{};
+    const bool ok = map_of(p.a[0], DT, c.dg, c.rows, c.d_ff, kRows) && map_of(p.a[1], DT, c.du, c.rows, c.d_ff, kRows) &&
+                    map_of(p.b[0], DT, c.w_gate, c.d_ff, c.d_in, kDepth) && map_of(p.b[1], DT, c.w_up, c.d_ff, c.d_in, kDepth) &&
+                    map_of(p.out[0], DT, c.dx, c.rows, c.d_in, 32);
+    if (!ok || !set_tiles(p, c.rows, c.d_in, kN, 1)) return cudaErrorInvalidValue;
+    p.blocks     = static_cast<uint32_t>(round_up_div(c.d_ff, kDepth));
+    p.dev_status = c.dev_status;
+    return start<DT, kInputGrad, BT_ACT_RELU, kN>(p, stream, sms);
+}
+
+template <int DT, int kN>
+cudaError_t weight_grad_of(const GluCall &c, int sms, cudaStream_t stream)
+{
+    MmaArgs    p{};
+    const bool ok = map_of(p.a[0], DT, c.dg, c.rows, c.d_ff, kDepth) && map_of(p.a[1], DT, c.du, c.rows, c.d_ff, kDepth) &&
+                    map_of(p.b[0], DT, c.x, c.rows, c.d_in, kDepth) && map_of(p.out[0], DT, c.dw_gate, c.d_ff, c.d_in, 32) &&
+                    map_of(p.out[1], DT, c.dw_up, c.d_ff, c.d_in, 32);
+    if (!ok || !set_tiles(p, c.d_ff, c.d_in, kN, 2)) return cudaErrorInvalidValue;
+    p.blocks     = static_cast<uint32_t>(round_up_div(c.rows, kDepth));
+    p.dev_status = c.dev_status;
+    return start<DT, kWeightGrad, BT_ACT_RELU, kN>(p, stream, sms);
+}
+
+template <int DT>
+cudaError_t forward(const GluCall &c, int sms, cudaStream_t stream)
+{
+    return rounds(c.rows, c.d_ff, 1, 128, 256, sms) <= rounds(c.rows, c.d_ff, 1, 64, 128, sms) ? forward_of<DT, 256>(c, sms, stream)
+                                                                                               : forward_of<DT, 128>(c, sms, stream);
+}
+template <int DT>
+cudaError_t backward(const GluCall &c, int sms, cudaStream_t stream)
+{
+    if (c.dx) {
+        const cudaError_t e = rounds(c.rows, c.d_in, 1, 256, 256, sms) <= rounds(c.rows, c.d_in, 1, 128, 128, sms) ? input_grad_of<DT, 256>(c, sms, stream)
+                                                                                                                   : input_grad_of<DT, 128>(c, sms, stream);
+        if (e != cudaSuccess) return e;
+    }
+    if (!c.dw_gate) return cudaSuccess;
+    return rounds(c.d_ff, c.d_in, 2, 256, 256, sms) <= rounds(c.d_ff, c.d_in, 2, 128, 128, sms) ? weight_grad_of<DT, 256>(c, sms, stream)
+                                                                                               : weight_grad_of<DT, 128>(c, sms, stream);
+}
+
+}  // namespace
+
+bool glu_mma_takes(const GluCall &c)
+{
+    return (c.dtype == BT_F16 || c.dtype == BT_BF16) && c.d_in % 8 == 0 && c.d_ff % 8 == 0 && encoder() != nullptr;
+}
+
+cudaError_t launch_glu_mma_fwd(const GluCall &c, cudaStream_t stream)
+{
+    const int sms = sm_count();
+    if (sms < 2) return cudaErrorInvalidDevice;
+    return c.dtype == BT_BF16 ? forward<BT_BF16>(c, sms, stream) : forward<BT_F16>(c, sms, stream);
+}
+
+cudaError_t launch_glu_mma_bwd(const GluCall &c, cudaStream_t stream)
+{
+    const int sms = sm_count();
+    if (sms < 2) return cudaErrorInvalidDevice;
+    return c.dtype == BT_BF16 ? backward<BT_BF16>(c, sms, stream) : backward<BT_F16>(c, sms, stream);
+}
+
+}  // namespace bt
