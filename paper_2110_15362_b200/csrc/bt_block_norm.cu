@@ -309,6 +309,241 @@ __device__ __forceinline__ bool whole_group(const NormArgs &a, const Chunk &c, c
     return begin >= c.first && end <= c.end;
 }
 
+// ---------------------------------------------------------------------------------------------- rows of whole vectors
+// A CTA per row, kHold 16-byte vectors of every operand per thread, and a ring of rows in shared memory that each thread fills
+// for itself with asynchronous copies, several rows ahead: what a thread reads it has copied, so the ring needs no barrier.
+// The work on consecutive rows overlaps, so that one barrier per row serves all its sums: while a row's sums meet, the next
+// row's are taken and the outputs of the one before are written.
+__device__ __forceinline__ void copy_ahead(void *to, const void *from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr(to)), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft>
+__device__ __forceinline__ void copy_wait()
+{
+    asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory");
+}
+
+// Eight sums over a warp by exchanges of halves (9 shuffles in place of 40): the lane ends with sum number lane / 4.
+template <typename A>
+__device__ __forceinline__ A warp_sums8(A (&v)[8])
+{
+    const uint32_t lane = threadIdx.x % 32;
+#pragma unroll
+    for (int half = 4; half >= 1; half /= 2) {
+        const bool up = lane & (4 * half);
+#pragma unroll
+        for (int k = 0; k < half; ++k) {
+            const A give = up ? v[k] : v[k + half], keep = up ? v[k + half] : v[k];
+            v[k] = keep + __shfl_xor_sync(0xFFFFFFFFu, give, 4 * half);
+        }
+    }
+    A s = v[0] + __shfl_xor_sync(0xFFFFFFFFu, v[0], 2);
+    return s + __shfl_xor_sync(0xFFFFFFFFu, s, 1);
+}
+// kSums of the eight sums over the CTA's warps (at most 16 of them), the same in every lane
+template <int kSums, typename A>
+__device__ __forceinline__ void cta_sums(const A (*part)[8], const uint32_t warps, A (&s)[kSums])
+{
+    const uint32_t lane = threadIdx.x % 32;
+    A              v    = 0;
+#pragma unroll
+    for (uint32_t k = 0; k < kMaxWarps / 4; ++k) {
+        const uint32_t w = k * 4 + lane / 8;
+        if (w < warps) v += part[w][lane % 8];
+    }
+    v += __shfl_xor_sync(0xFFFFFFFFu, v, 8);
+    v += __shfl_xor_sync(0xFFFFFFFFu, v, 16);
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) s[k] = __shfl_sync(0xFFFFFFFFu, v, k);
+}
+
+// rows of the ring
+template <int kHold>
+constexpr uint32_t kRingStages = kHold == 1 ? 5 : 3;
+
+// kRowGate: the gate changes from row to row of a CTA and comes through the ring like a fifth operand.
+template <int DT, int kHold, bool kRowGate>
+__global__ void __launch_bounds__(kMaxTeam, 1)
+block_norm_bwd_ring_kernel(const NormArgs a)
+{
+    in_stream_order();
+    using X                  = Access<DT, true>;
+    using Elem               = typename X::Elem;
+    using Acc                = typename X::Acc;
+    constexpr int kW         = X::kW;
+    constexpr int      kOperands = kRowGate ? 5 : 4;
+    constexpr uint32_t stages    = kRingStages<kHold>;
+    extern __shared__ uint4 ring[];                                    // [stage][operand][hold][thread]
+    __shared__ Acc part[2][kMaxWarps][8];
+    const uint32_t t = threadIdx.x, team = blockDim.x, chunk = blockIdx.x, warps = team / 32;
+    const uint32_t count = static_cast<uint32_t>(a.d / kW);
+    const Acc      scale = static_cast<Acc>(a.scale), eps = static_cast<Acc>(a.eps), of_d = Acc(1) / static_cast<Acc>(a.d);
+    const uint64_t bytes = a.rows * a.d * sizeof(Elem);
+    const Extent   all_x = extent_of(a.x_out, bytes), all_f = extent_of(a.n_out, bytes);
+    const Extent   all_g = extent_of(a.dgate, round_up_div(a.rows, a.gate_rows) * a.d * sizeof(Elem));
+    const Extent   part_g = extent_of(a.part_gate, 2ull * a.chunks * a.d * sizeof(Acc));
+    const Extent   part_w = extent_of(a.part_pre, a.chunks * a.d * sizeof(Acc)), part_p = extent_of(a.part_post, a.chunks * a.d * sizeof(Acc));
+    const Chunk    c      = chunk_of(a, chunk);
+
+    const auto slot = [&](const uint32_t stage, const int operand, const int j) -> uint4 & {
+        return ring[((stage * kOperands + operand) * kHold + j) * team + t];
+    };
+    // (a commit for every row of the ring, also behind the chunk's end: the waits count groups)
+    const auto fill = [&](const uint32_t stage, const uint64_t row) {
+        if (row < c.end) {
+            const void *const from[5] = {row_of<Elem>(a.x, row, a.d), row_of<Elem>(a.f, row, a.d), row_of<Elem>(a.dn, row, a.d),
+                                         row_of<Elem>(a.dy, row, a.d), kRowGate ? row_of<Elem>(a.gate, row / a.gate_rows, a.d) : nullptr};
+#pragma unroll
+            for (int j = 0; j < kHold; ++j)
+#pragma unroll
+                for (int o = 0; o < kOperands; ++o)
+                    if (j * team + t < count && from[o]) copy_ahead(&slot(stage, o, j), static_cast<const uint4 *>(from[o]) + j * team + t);
+        }
+        copy_commit();
+    };
+    // operands that the call leaves out are zeros
+#pragma unroll
+    for (int j = 0; j < kHold; ++j)
+        for (uint32_t s = 0; s < stages; ++s)
+#pragma unroll
+            for (int o = 0; o < kOperands; ++o) slot(s, o, j) = make_uint4(0, 0, 0, 0);
+    for (uint32_t s = 0; s + 1 < stages; ++s) fill(s, c.first + s);
+
+    Acc w_pre[kHold][kW], gw[kHold][kW];                               // gw: scale * gate * w_post; kRowGate: scale * w_post
+#pragma unroll
+    for (int j = 0; j < kHold; ++j) {
+#pragma unroll
+        for (int k = 0; k < kW; ++k) w_pre[j][k] = gw[j][k] = 1;
+        if (j * team + t < count) {
+            Acc g[kW];
+            if (a.w_pre) X::read_shared(a.w_pre, j * team + t, w_pre[j]);
+            if (a.w_post) X::read_shared(a.w_post, j * team + t, gw[j]);
+            if (!kRowGate && a.gate) {
+                X::read_shared(a.gate, j * team + t, g);
+#pragma unroll
+                for (int k = 0; k < kW; ++k) gw[j][k] *= g[k];
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kW; ++k) gw[j][k] *= scale;
+    }
+
+    // sum_pre: of dn x' r.  sum_f: of t f rf, of the rows that share a gate; times scale w_post it is the gate's gradient, times
+    // scale gate its share of w_post's (sum_post).
+    Acc sum_pre[kHold][kW] = {}, sum_f[kHold][kW] = {}, sum_post[kRowGate ? kHold : 1][kW] = {};
+    uint32_t stage_a = 0, stage_b = 0, stage_c = stages - 1;           // of the row whose sums are taken, of the one before, to fill
+    for (uint64_t row = c.first; row <= c.end; ++row) {
+        if (row < c.end) {
+            // ---- this row's sums
+            copy_wait<static_cast<int>(stages) - 2>();                 // (stages - 1 rows and one more per row so far are on their way)
+            Acc s[8] = {};
+#pragma unroll
+            for (int j = 0; j < kHold; ++j) {
+                Acc x[kW], f[kW], dn[kW], dy[kW], g[kW];
+                X::widen(slot(stage_a, 0, j), x), X::widen(slot(stage_a, 1, j), f), X::widen(slot(stage_a, 2, j), dn), X::widen(slot(stage_a, 3, j), dy);
+                if constexpr (kRowGate) X::widen(slot(stage_a, 4, j), g);
+#pragma unroll
+                for (int k = 0; k < kW; ++k) {
+                    const Acc wn = dn[k] * w_pre[j][k], q = (kRowGate ? gw[j][k] * g[k] : gw[j][k]) * f[k];
+                    s[0] += x[k] * x[k];
+                    s[1] += wn * x[k];
+                    s[2] += f[k] * f[k];
+                    s[3] += dy[k] * q;
+                    s[4] += wn * q;
+                    s[5] += x[k] * q;
+                }
+            }
+            const Acc v = warp_sums8(s);
+            if (t % 4 == 0) part[row & 1][t / 32][t % 32 / 4] = v;
+        }
+        if (row > c.first) {
+            // ---- the row before: its outputs
+            const uint64_t before = row - 1;
+            Acc            s[6];
+            cta_sums(part[before & 1], warps, s);
+            const RowFactors<Acc> q = factors_of(s, of_d, eps, a.w_post != nullptr);
+            void *dx = row_of<Elem>(a.x_out, before, a.d), *df = row_of<Elem>(a.n_out, before, a.d);
+#pragma unroll
+            for (int j = 0; j < kHold; ++j) {
+                const uint32_t i = j * team + t;
+                Acc x[kW], f[kW], dn[kW], dy[kW], g[kW];
+                X::widen(slot(stage_b, 0, j), x), X::widen(slot(stage_b, 1, j), f), X::widen(slot(stage_b, 2, j), dn), X::widen(slot(stage_b, 3, j), dy);
+                if constexpr (kRowGate) X::widen(slot(stage_b, 4, j), g);
+#pragma unroll
+                for (int k = 0; k < kW; ++k) {
+                    const Acc tv = dy[k] + q.r * (dn[k] * w_pre[j][k]) - q.rrc * x[k];
+                    sum_pre[j][k] += dn[k] * (x[k] * q.r);
+                    sum_f[j][k] += tv * (f[k] * q.rf);
+                    f[k]  = tv * (kRowGate ? gw[j][k] * g[k] : gw[j][k]) * q.rf - q.rf3m * f[k];
+                    dy[k] = tv;
+                }
+                if (i < count) {
+                    if (dx) X::store(dx, i, dy, all_x);
+                    if (df) X::store(df, i, f, all_f);
+                }
+            }
+            // the last of the group's rows in this chunk: its gate's gradient, or this chunk's share of it
+            if (a.gate && (row == c.end || (kRowGate && row % a.gate_rows == 0))) {
+                const uint64_t group = before / a.gate_rows;
+                uint64_t       to;
+                const bool     whole = whole_group(a, c, group, chunk, to);
+#pragma unroll
+                for (int j = 0; j < kHold; ++j) {
+                    const uint32_t i = j * team + t;
+                    Acc            w[kW], g[kW];
+#pragma unroll
+                    for (int k = 0; k < kW; ++k) w[k] = 1, g[k] = 0;
+                    if (i < count) {
+                        if (a.w_post) X::read_shared(a.w_post, i, w);
+                        if (kRowGate) X::widen(slot(stage_b, 4, j), g);
+                    }
+#pragma unroll
+                    for (int k = 0; k < kW; ++k) {
+                        w[k] *= scale * sum_f[j][k];
+                        if constexpr (kRowGate) sum_post[j][k] += scale * g[k] * sum_f[j][k], sum_f[j][k] = 0;
+                    }
+                    if (a.dgate && i < count) {
+                        if (whole) X::store(row_of<Elem>(a.dgate, group, a.d), i, w, all_g);
+                        else
+#pragma unroll
+                            for (int k = 0; k < kW; ++k) {
+                                Acc *const o = reinterpret_cast<Acc *>(a.part_gate) + to * a.d + i * kW + k;
+                                if (part_g.holds(o, sizeof(Acc))) *o = w[k];
+                            }
+                    }
+                }
+            }
+            stage_b = stage_b + 1 == stages ? 0 : stage_b + 1;
+        }
+        __syncthreads();                                               // the sums of this row are there; the words of the one before are free
+        fill(stage_c, row + stages - 1);
+        stage_c = stage_c + 1 == stages ? 0 : stage_c + 1;
+        stage_a = stage_a + 1 == stages ? 0 : stage_a + 1;
+    }
+#pragma unroll
+    for (int j = 0; j < kHold; ++j) {
+        const uint32_t i = j * team + t;
+        if (i >= count) continue;
+        if (!kRowGate && a.dw_post) {
+            Acc g[kW];
+#pragma unroll
+            for (int k = 0; k < kW; ++k) g[k] = 1;
+            if (a.gate) X::read_shared(a.gate, i, g);
+#pragma unroll
+            for (int k = 0; k < kW; ++k) sum_f[j][k] *= scale * g[k];
+        }
+#pragma unroll
+        for (int k = 0; k < kW; ++k) {
+            const uint64_t o = chunk * a.d + i * kW + k;
+            if (a.dw_pre && part_w.holds(reinterpret_cast<Acc *>(a.part_pre) + o, sizeof(Acc))) reinterpret_cast<Acc *>(a.part_pre)[o] = sum_pre[j][k];
+            if (a.dw_post && part_p.holds(reinterpret_cast<Acc *>(a.part_post) + o, sizeof(Acc)))
+                reinterpret_cast<Acc *>(a.part_post)[o] = kRowGate ? sum_post[kRowGate ? j : 0][k] : sum_f[j][k];
+        }
+    }
+}
+
 // kHold accesses of every operand per thread, held in registers with the column sums.
 template <int DT, bool kVector, int kHold, bool kCta>
 __global__ void __launch_bounds__(kCta ? kMaxTeam : 32 * kWarpTeams)
@@ -511,8 +746,9 @@ __global__ void block_norm_bwd_columns_kernel(const NormArgs a)
     if (a.dw_post && part_p.holds(reinterpret_cast<Acc *>(a.part_post) + o, sizeof(Acc))) reinterpret_cast<Acc *>(a.part_post)[o] = sum_post;
 }
 
-// The partial rows added up: blockIdx.y = 0 w_pre, 1 w_post, 2 + k the k-th chunk border's gate group.  A thread takes every
-// kSplit-th partial row of its column; the CTA adds the kSplit sums in order.
+// The partial rows added up: 0 w_pre, 1 w_post, 2 + k the k-th group of rows with a gate or, where there are more groups
+// than borders between chunks, the group that lies across the k-th border.  A thread takes every kSplit-th partial row of its
+// column; the CTA adds the kSplit sums in order.
 constexpr int kFinishColumns = 32, kSplit = 16;
 template <int DT>
 __global__ void __launch_bounds__(kFinishColumns *kSplit)
@@ -535,17 +771,21 @@ block_norm_finish_kernel(const NormArgs a)
         count = a.chunks;
         if (!to) return;
     } else {
-        // the group that crosses from chunk `what - 2` into the next one, if that is where it begins to cross
         if (!a.dgate) return;
-        const uint64_t border = (what - 1) * a.chunk_rows;              // the next chunk's first row
-        if (border >= a.rows || border % a.gate_rows == 0) return;
-        const uint64_t group = border / a.gate_rows, begin = group * a.gate_rows;
-        if (begin / a.chunk_rows != what - 2) return;
-        const uint64_t end = begin + a.gate_rows < a.rows ? begin + a.gate_rows : a.rows;
+        uint64_t group = what - 2;
+        if (round_up_div(a.rows, a.gate_rows) >= a.chunks) {            // by borders
+            const uint64_t border = (what - 1) * a.chunk_rows;          // the next chunk's first row
+            if (border >= a.rows || border % a.gate_rows == 0) return;
+            group = border / a.gate_rows;
+            if (group * a.gate_rows / a.chunk_rows != what - 2) return;  // (a group across several borders: at its first)
+        }
+        const uint64_t begin = group * a.gate_rows, end = begin + a.gate_rows < a.rows ? begin + a.gate_rows : a.rows;
+        const uint64_t from_chunk = begin / a.chunk_rows, to_chunk = (end - 1) / a.chunk_rows;
+        if (from_chunk == to_chunk) return;                             // written whole
         // slot 2 * chunk + 1 of the first chunk, then slot 2 * chunk of the others, one after the other every second row
-        from   = reinterpret_cast<const Acc *>(a.part_gate) + (2ull * (what - 2) + 1) * a.d;
+        from   = reinterpret_cast<const Acc *>(a.part_gate) + (2 * from_chunk + 1) * a.d;
         to     = static_cast<Elem *>(a.dgate) + group * a.d;
-        count  = (end - 1) / a.chunk_rows - (what - 2) + 1;
+        count  = to_chunk - from_chunk + 1;
         stride = 0;
     }
     Acc s = 0;
@@ -600,27 +840,55 @@ cudaError_t start_bwd(const NormArgs &a, uint32_t threads, cudaStream_t stream)
     const uint32_t teams = kCta ? 1 : kWarpTeams;
     return launch(block_norm_bwd_kernel<DT, kVector, kHold, kCta>, static_cast<unsigned>(round_up_div(a.chunks, teams)), threads, 0, stream, a);
 }
-template <int DT, bool kVector>
-cudaError_t bwd_of(const NormArgs &a, cudaStream_t stream)
+
+// threads of a CTA that holds `count` accesses, `hold` per thread
+uint32_t team_of(uint64_t count, uint32_t hold) { return static_cast<uint32_t>(round_up_div(round_up_div(count, hold), 32) * 32); }
+
+template <int kHold>
+size_t ring_bytes(uint32_t team, bool row_gate) { return static_cast<size_t>(kRingStages<kHold>) * (row_gate ? 5 : 4) * kHold * team * 16; }
+constexpr size_t kMostShared = 220 * 1024;
+
+template <int DT, int kHold, bool kRowGate>
+cudaError_t start_ring(const NormArgs &a, uint32_t team, cudaStream_t stream)
 {
-    constexpr uint64_t kW    = Access<DT, kVector>::kW;
-    const uint64_t     count = a.d / kW;
-    const auto team = [&](uint64_t hold) { return static_cast<uint32_t>(round_up_div(round_up_div(count, hold), 32) * 32); };
-    if (count <= 32) return start_bwd<DT, kVector, 1, false>(a, 32 * kWarpTeams, stream);
-    if (count <= 64) return start_bwd<DT, kVector, 2, false>(a, 32 * kWarpTeams, stream);
-    if (count <= kMaxTeam) return start_bwd<DT, kVector, 1, true>(a, team(1), stream);
-    if (kVector || count <= 2 * kMaxTeam) return start_bwd<DT, kVector, 2, true>(a, team(2), stream);
-    return start_bwd<DT, kVector, kVector ? 2 : 8, true>(a, team(8), stream);
+    const auto        kernel = block_norm_bwd_ring_kernel<DT, kHold, kRowGate>;
+    const size_t      smem   = ring_bytes<kHold>(team, kRowGate);
+    const cudaError_t e      = reported(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    if (e != cudaSuccess) return e;
+    return launch(kernel, a.chunks, team, smem, stream, a);
 }
 
-// the chunks of a backward pass: enough teams to fill the SMs twice over
+template <int DT>
+cudaError_t bwd_vectors(const NormArgs &a, cudaStream_t stream)
+{
+    const uint64_t count    = a.d / kLanes<DT>;
+    const bool     row_gate = a.gate && a.gate_rows < a.rows;
+    if (count <= kMaxTeam)
+        return row_gate ? start_ring<DT, 1, true>(a, team_of(count, 1), stream) : start_ring<DT, 1, false>(a, team_of(count, 1), stream);
+    const uint32_t team = team_of(count, 2);
+    if (!row_gate) return start_ring<DT, 2, false>(a, team, stream);
+    if (ring_bytes<2>(team, true) <= kMostShared) return start_ring<DT, 2, true>(a, team, stream);
+    return start_bwd<DT, true, 2, true>(a, team, stream);              // five operands of such rows do not fit shared memory three times
+}
+template <int DT>
+cudaError_t bwd_elements(const NormArgs &a, cudaStream_t stream)
+{
+    if (a.d <= 32) return start_bwd<DT, false, 1, false>(a, 32 * kWarpTeams, stream);
+    if (a.d <= 64) return start_bwd<DT, false, 2, false>(a, 32 * kWarpTeams, stream);
+    if (a.d <= kMaxTeam) return start_bwd<DT, false, 1, true>(a, team_of(a.d, 1), stream);
+    if (a.d <= 2 * kMaxTeam) return start_bwd<DT, false, 2, true>(a, team_of(a.d, 2), stream);
+    return start_bwd<DT, false, 8, true>(a, team_of(a.d, 8), stream);
+}
+
+// The chunks of a backward pass: as many teams as the SMs hold at a time.
 uint32_t chunks_of(uint64_t rows, uint64_t d, int es, int sms)
 {
-    const uint64_t lanes = 16 / static_cast<uint64_t>(es), count = d % lanes == 0 ? d / lanes : d;
+    const uint64_t lanes = 16 / static_cast<uint64_t>(es), count = d / lanes;
     uint64_t       most;
     if (!row_fits(d, es)) most = kLongChunks;
-    else if (count <= 64) most = static_cast<uint64_t>(sms) * 24;
-    else most = static_cast<uint64_t>(sms) * (count <= 256 ? 6 : count <= 512 ? 3 : 2);
+    else if (d % lanes == 0) most = static_cast<uint64_t>(sms) * (kMaxTeam / team_of(count, count <= kMaxTeam ? 1 : 2));
+    else if (d <= 64) most = static_cast<uint64_t>(sms) * 24;
+    else most = static_cast<uint64_t>(sms) * (d <= 256 ? 6 : d <= 512 ? 3 : 2);
     if (most > kMaxChunks) most = kMaxChunks;
     if (most > rows) most = rows;
     const uint64_t chunk_rows = round_up_div(rows, most);
@@ -647,11 +915,12 @@ cudaError_t backward(const NormArgs &a, cudaStream_t stream)
         if (!a.dgate && !a.dw_pre && !a.dw_post) return cudaSuccess;
         e = launch(block_norm_bwd_columns_kernel<DT>, static_cast<unsigned>(round_up_div(a.d, 128) * a.chunks), 128, 0, stream, a);
     } else {
-        e = a.d % kLanes<DT> == 0 ? bwd_of<DT, true>(a, stream) : bwd_of<DT, false>(a, stream);
+        e = a.d % kLanes<DT> == 0 ? bwd_vectors<DT>(a, stream) : bwd_elements<DT>(a, stream);
     }
     if (e != cudaSuccess || (!a.dgate && !a.dw_pre && !a.dw_post)) return e;
-    const uint64_t borders = a.dgate ? a.chunks - 1 : 0;
-    return launch(block_norm_finish_kernel<DT>, static_cast<unsigned>(round_up_div(a.d, kFinishColumns) * (2 + borders)), kFinishColumns * kSplit, 0,
+    const uint64_t groups = round_up_div(a.rows, a.gate_rows), borders = a.chunks - 1;
+    const uint64_t shared = a.dgate ? (groups < borders ? groups : borders) : 0;
+    return launch(block_norm_finish_kernel<DT>, static_cast<unsigned>(round_up_div(a.d, kFinishColumns) * (2 + shared)), kFinishColumns * kSplit, 0,
                   stream, a);
 }
 

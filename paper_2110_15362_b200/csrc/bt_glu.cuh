@@ -44,6 +44,17 @@ __device__ __forceinline__ A act_slope(const A g)
     }
 }
 
+// The same for values that are rounded to 16 bits: the logistic function by the fast exponential and reciprocal (a few units in
+// the 22nd bit).
+__device__ __forceinline__ float sigmoid_short(const float v) { return __fdividef(1.0f, 1.0f + __expf(-v)); }
+template <int kAct>
+__device__ __forceinline__ float act_short(const float g)
+{
+    if constexpr (kAct == BT_ACT_SILU) return g * sigmoid_short(g);
+    else if constexpr (kAct == BT_ACT_GELU_TANH) return g * sigmoid_short(1.5957691216057307f * (g + 0.044715f * g * g * g));
+    else return act_of<kAct>(g);
+}
+
 // One call of the block, forward or backward (sizes checked, none of them 0).
 struct GluCall {
     const void *x, *w_gate, *w_up;                 // [rows, d_in], [d_ff, d_in] twice
