@@ -358,12 +358,174 @@ __device__ __forceinline__ void cta_sums(const A (*part)[8], const uint32_t warp
 #pragma unroll
     for (int k = 0; k < kSums; ++k) s[k] = __shfl_sync(0xFFFFFFFFu, v, k);
 }
+// the sum over a warp's lanes and over the CTA's warps, in two steps
+template <typename A>
+__device__ __forceinline__ A cta_sum(const A *part, const uint32_t warps)
+{
+    const uint32_t lane = threadIdx.x % 32;
+    return warp_sum(lane < warps ? part[lane] : A(0));
+}
 
 // rows of the ring
 template <int kHold>
 constexpr uint32_t kRingStages = kHold == 1 ? 5 : 3;
 
-// kRowGate: the gate changes from row to row of a CTA and comes through the ring like a fifth operand.
+template <int DT>
+__device__ __forceinline__ void read_pairs(const void *row, const uint32_t i, Two<typename Num<DT>::Acc> (&v)[kPairs<DT>])
+{
+    widen_pairs<DT>(__ldg(static_cast<const uint4 *>(row) + i), v);
+}
+
+// scale * gate * w_post of a thread's columns (kRowGate: without the gate, which changes from row to row)
+template <int DT, int kHold, bool kRowGate>
+__device__ __forceinline__ void branch_factors(const NormArgs &a, const uint32_t count, Two<typename Num<DT>::Acc> (&gw)[kHold][kPairs<DT>])
+{
+    using Acc = typename Num<DT>::Acc;
+#pragma unroll
+    for (int j = 0; j < kHold; ++j) {
+        const uint32_t i = j * blockDim.x + threadIdx.x;
+#pragma unroll
+        for (int k = 0; k < kPairs<DT>; ++k) gw[j][k] = both(static_cast<Acc>(a.scale));
+        if (i >= count) continue;
+        Two<Acc> w[kPairs<DT>];
+        if (a.w_post) {
+            read_pairs<DT>(a.w_post, i, w);
+#pragma unroll
+            for (int k = 0; k < kPairs<DT>; ++k) gw[j][k] = gw[j][k] * w[k];
+        }
+        if (!kRowGate && a.gate) {
+            read_pairs<DT>(a.gate, i, w);
+#pragma unroll
+            for (int k = 0; k < kPairs<DT>; ++k) gw[j][k] = gw[j][k] * w[k];
+        }
+    }
+}
+
+// Forward.  In one turn of the loop: the sum of f^2 of a row, x' and its sum of the row before, n of the row before that.
+// kRowGate: the gate changes from row to row and comes through the ring like a third operand.
+template <int DT, int kHold, bool kRowGate>
+__global__ void __launch_bounds__(kMaxTeam, 1)
+block_norm_fwd_ring_kernel(const NormArgs a)
+{
+    in_stream_order();
+    using Elem               = typename Num<DT>::Elem;
+    using Acc                = typename Num<DT>::Acc;
+    constexpr int      kP    = kPairs<DT>;
+    constexpr int      kOperands = kRowGate ? 3 : 2;
+    constexpr uint32_t stages    = kRingStages<kHold>;
+    extern __shared__ uint4 ring[];                                    // [stage][operand][hold][thread]
+    __shared__ Acc part[2][2][kMaxWarps];                              // [turn][of f, of x'][warp]
+    const uint32_t t = threadIdx.x, team = blockDim.x, warps = team / 32;
+    const uint32_t count = static_cast<uint32_t>(a.d / kLanes<DT>);
+    const Acc      eps = static_cast<Acc>(a.eps), of_d = Acc(1) / static_cast<Acc>(a.d);
+    const Extent   all_x = extent_of(a.x_out, a.rows * a.d * sizeof(Elem)), all_n = extent_of(a.n_out, a.rows * a.d * sizeof(Elem));
+
+    const auto slot = [&](const uint32_t stage, const int operand, const int j) -> uint4 & {
+        return ring[((stage * kOperands + operand) * kHold + j) * team + t];
+    };
+    // (a commit for every turn, also behind the last row: the waits count groups)
+    const auto fill = [&](const uint32_t stage, const uint64_t row) {
+        if (row < a.rows) {
+            const void *const from[3] = {row_of<Elem>(a.x, row, a.d), row_of<Elem>(a.f, row, a.d), kRowGate ? row_of<Elem>(a.gate, row / a.gate_rows, a.d) : nullptr};
+#pragma unroll
+            for (int j = 0; j < kHold; ++j)
+#pragma unroll
+                for (int o = 0; o < kOperands; ++o)
+                    if (j * team + t < count && from[o]) copy_ahead(&slot(stage, o, j), static_cast<const uint4 *>(from[o]) + j * team + t);
+        }
+        copy_commit();
+    };
+#pragma unroll
+    for (int j = 0; j < kHold; ++j)
+        for (uint32_t s = 0; s < stages; ++s)                          // columns beyond the row, and an f left out, are zeros
+#pragma unroll
+            for (int o = 0; o < kOperands; ++o)
+                if (j * team + t >= count || (o == 1 && !a.f)) slot(s, o, j) = make_uint4(0, 0, 0, 0);
+    for (uint32_t s = 0; s + 1 < stages; ++s) fill(s, blockIdx.x + static_cast<uint64_t>(s) * gridDim.x);
+
+    Two<Acc> gw[kHold][kP], w_pre[kHold][kP], y[kHold][kP];
+    branch_factors<DT, kHold, kRowGate>(a, count, gw);
+#pragma unroll
+    for (int j = 0; j < kHold; ++j) {
+#pragma unroll
+        for (int k = 0; k < kP; ++k) w_pre[j][k] = both(Acc(1));
+        if (a.w_pre && j * team + t < count) read_pairs<DT>(a.w_pre, j * team + t, w_pre[j]);
+    }
+    const uint64_t mine = (a.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;      // rows of this CTA (the grid is not wider than the rows)
+    uint32_t       stage_a = 0, stage_b = 0, stage_c = stages - 1;
+    for (uint64_t turn = 0; turn < mine + 2; ++turn) {
+        const Acc(*const before)[kMaxWarps] = part[(turn & 1) ^ 1];
+        Acc(*const now)[kMaxWarps]          = part[turn & 1];
+        if (turn < mine) {
+            copy_wait<static_cast<int>(stages) - 2>();                 // (stages - 1 rows and one more per turn so far are on their way)
+            if (a.w_post) {
+                Two<Acc> s = both(Acc(0));
+#pragma unroll
+                for (int j = 0; j < kHold; ++j) {
+                    Two<Acc> f[kP];
+                    widen_pairs<DT>(slot(stage_a, 1, j), f);
+#pragma unroll
+                    for (int k = 0; k < kP; ++k) s = fma2(f[k], f[k], s);
+                }
+                const Acc v = warp_sum(s.low() + s.high());
+                if (t % 32 == 0) now[0][t / 32] = v;
+            }
+        }
+        if (turn >= 2 && a.n_out) {
+            // ---- n of the row two before, whose x' waits in y
+            const uint64_t row = blockIdx.x + (turn - 2) * gridDim.x;
+            const Two<Acc> r   = both(root_of(cta_sum(before[1], warps) * of_d + eps));
+            uint4 *const   out = static_cast<uint4 *>(row_of<Elem>(a.n_out, row, a.d));
+#pragma unroll
+            for (int j = 0; j < kHold; ++j) {
+                const uint32_t i = j * team + t;
+                if (i >= count) continue;
+                Two<Acc> n[kP];
+#pragma unroll
+                for (int k = 0; k < kP; ++k) n[k] = y[j][k] * r * w_pre[j][k];
+                if (all_n.holds(out + i, 16)) out[i] = narrow_pairs<DT>(n);
+            }
+        }
+        if (turn >= 1 && turn <= mine) {
+            // ---- x' of the row before
+            const uint64_t row = blockIdx.x + (turn - 1) * gridDim.x;
+            const Two<Acc> rf  = both(a.w_post ? root_of(cta_sum(before[0], warps) * of_d + eps) : Acc(1));
+            uint4 *const   out = static_cast<uint4 *>(row_of<Elem>(a.x_out, row, a.d));
+            Two<Acc>       s   = both(Acc(0));
+#pragma unroll
+            for (int j = 0; j < kHold; ++j) {
+                const uint32_t i = j * team + t;
+                Two<Acc>       f[kP];
+                widen_pairs<DT>(slot(stage_b, 0, j), y[j]);
+                widen_pairs<DT>(slot(stage_b, 1, j), f);
+                if constexpr (kRowGate) {
+                    Two<Acc> g[kP];
+                    widen_pairs<DT>(slot(stage_b, 2, j), g);
+#pragma unroll
+                    for (int k = 0; k < kP; ++k) f[k] = f[k] * g[k];
+                }
+#pragma unroll
+                for (int k = 0; k < kP; ++k) {
+                    y[j][k] = fma2(f[k] * rf, gw[j][k], y[j][k]);
+                    s       = fma2(y[j][k], y[j][k], s);
+                }
+                if (out && i < count && all_x.holds(out + i, 16)) out[i] = narrow_pairs<DT>(y[j]);
+            }
+            if (a.n_out) {
+                const Acc v = warp_sum(s.low() + s.high());
+                if (t % 32 == 0) now[1][t / 32] = v;
+            }
+            stage_b = stage_b + 1 == stages ? 0 : stage_b + 1;
+        }
+        __syncthreads();                                               // this turn's sums are there; those of the turn before are free
+        fill(stage_c, blockIdx.x + (turn + stages - 1) * gridDim.x);
+        stage_c = stage_c + 1 == stages ? 0 : stage_c + 1;
+        stage_a = stage_a + 1 == stages ? 0 : stage_a + 1;
+    }
+}
+
+// Backward, over the rows of a chunk.  In one turn of the loop: the six sums of a row, the outputs of the row before.
+// kRowGate: the gate changes from row to row and comes through the ring like a fifth operand.
 template <int DT, int kHold, bool kRowGate>
 __global__ void __launch_bounds__(kMaxTeam, 1)
 block_norm_bwd_ring_kernel(const NormArgs a)
@@ -372,13 +534,13 @@ block_norm_bwd_ring_kernel(const NormArgs a)
     using X                  = Access<DT, true>;
     using Elem               = typename X::Elem;
     using Acc                = typename X::Acc;
-    constexpr int kW         = X::kW;
+    constexpr int      kP    = kPairs<DT>;
     constexpr int      kOperands = kRowGate ? 5 : 4;
     constexpr uint32_t stages    = kRingStages<kHold>;
     extern __shared__ uint4 ring[];                                    // [stage][operand][hold][thread]
     __shared__ Acc part[2][kMaxWarps][8];
     const uint32_t t = threadIdx.x, team = blockDim.x, chunk = blockIdx.x, warps = team / 32;
-    const uint32_t count = static_cast<uint32_t>(a.d / kW);
+    const uint32_t count = static_cast<uint32_t>(a.d / kLanes<DT>);
     const Acc      scale = static_cast<Acc>(a.scale), eps = static_cast<Acc>(a.eps), of_d = Acc(1) / static_cast<Acc>(a.d);
     const uint64_t bytes = a.rows * a.d * sizeof(Elem);
     const Extent   all_x = extent_of(a.x_out, bytes), all_f = extent_of(a.n_out, bytes);
@@ -403,58 +565,61 @@ block_norm_bwd_ring_kernel(const NormArgs a)
         }
         copy_commit();
     };
-    // operands that the call leaves out are zeros
+    // columns beyond the row, and operands that the call leaves out, are zeros
 #pragma unroll
     for (int j = 0; j < kHold; ++j)
         for (uint32_t s = 0; s < stages; ++s)
 #pragma unroll
-            for (int o = 0; o < kOperands; ++o) slot(s, o, j) = make_uint4(0, 0, 0, 0);
+            for (int o = 0; o < kOperands; ++o)
+                if (j * team + t >= count || (o == 1 && !a.f) || (o == 2 && !a.dn) || (o == 3 && !a.dy)) slot(s, o, j) = make_uint4(0, 0, 0, 0);
     for (uint32_t s = 0; s + 1 < stages; ++s) fill(s, c.first + s);
 
-    Acc w_pre[kHold][kW], gw[kHold][kW];                               // gw: scale * gate * w_post; kRowGate: scale * w_post
+    Two<Acc> w_pre[kHold][kP], gw[kHold][kP];
+    branch_factors<DT, kHold, kRowGate>(a, count, gw);
 #pragma unroll
     for (int j = 0; j < kHold; ++j) {
 #pragma unroll
-        for (int k = 0; k < kW; ++k) w_pre[j][k] = gw[j][k] = 1;
-        if (j * team + t < count) {
-            Acc g[kW];
-            if (a.w_pre) X::read_shared(a.w_pre, j * team + t, w_pre[j]);
-            if (a.w_post) X::read_shared(a.w_post, j * team + t, gw[j]);
-            if (!kRowGate && a.gate) {
-                X::read_shared(a.gate, j * team + t, g);
-#pragma unroll
-                for (int k = 0; k < kW; ++k) gw[j][k] *= g[k];
-            }
-        }
-#pragma unroll
-        for (int k = 0; k < kW; ++k) gw[j][k] *= scale;
+        for (int k = 0; k < kP; ++k) w_pre[j][k] = both(Acc(1));
+        if (a.w_pre && j * team + t < count) read_pairs<DT>(a.w_pre, j * team + t, w_pre[j]);
     }
 
     // sum_pre: of dn x' r.  sum_f: of t f rf, of the rows that share a gate; times scale w_post it is the gate's gradient, times
     // scale gate its share of w_post's (sum_post).
-    Acc sum_pre[kHold][kW] = {}, sum_f[kHold][kW] = {}, sum_post[kRowGate ? kHold : 1][kW] = {};
+    Two<Acc> sum_pre[kHold][kP], sum_f[kHold][kP], sum_post[kRowGate ? kHold : 1][kP];
+#pragma unroll
+    for (int j = 0; j < kHold; ++j)
+#pragma unroll
+        for (int k = 0; k < kP; ++k) sum_pre[j][k] = sum_f[j][k] = sum_post[kRowGate ? j : 0][k] = both(Acc(0));
     uint32_t stage_a = 0, stage_b = 0, stage_c = stages - 1;           // of the row whose sums are taken, of the one before, to fill
     for (uint64_t row = c.first; row <= c.end; ++row) {
         if (row < c.end) {
             // ---- this row's sums
             copy_wait<static_cast<int>(stages) - 2>();                 // (stages - 1 rows and one more per row so far are on their way)
-            Acc s[8] = {};
+            Two<Acc> p[6];
+#pragma unroll
+            for (int k = 0; k < 6; ++k) p[k] = both(Acc(0));
 #pragma unroll
             for (int j = 0; j < kHold; ++j) {
-                Acc x[kW], f[kW], dn[kW], dy[kW], g[kW];
-                X::widen(slot(stage_a, 0, j), x), X::widen(slot(stage_a, 1, j), f), X::widen(slot(stage_a, 2, j), dn), X::widen(slot(stage_a, 3, j), dy);
-                if constexpr (kRowGate) X::widen(slot(stage_a, 4, j), g);
+                Two<Acc> x[kP], f[kP], dn[kP], dy[kP], g[kP];
+                widen_pairs<DT>(slot(stage_a, 0, j), x), widen_pairs<DT>(slot(stage_a, 1, j), f);
+                widen_pairs<DT>(slot(stage_a, 2, j), dn), widen_pairs<DT>(slot(stage_a, 3, j), dy);
+                if constexpr (kRowGate) widen_pairs<DT>(slot(stage_a, 4, j), g);
 #pragma unroll
-                for (int k = 0; k < kW; ++k) {
-                    const Acc wn = dn[k] * w_pre[j][k], q = (kRowGate ? gw[j][k] * g[k] : gw[j][k]) * f[k];
-                    s[0] += x[k] * x[k];
-                    s[1] += wn * x[k];
-                    s[2] += f[k] * f[k];
-                    s[3] += dy[k] * q;
-                    s[4] += wn * q;
-                    s[5] += x[k] * q;
+                for (int k = 0; k < kP; ++k) {
+                    const Two<Acc> wn = dn[k] * w_pre[j][k];
+                    Two<Acc>       q  = gw[j][k] * f[k];
+                    if constexpr (kRowGate) q = q * g[k];
+                    p[0] = fma2(x[k], x[k], p[0]);
+                    p[1] = fma2(wn, x[k], p[1]);
+                    p[2] = fma2(f[k], f[k], p[2]);
+                    p[3] = fma2(dy[k], q, p[3]);
+                    p[4] = fma2(wn, q, p[4]);
+                    p[5] = fma2(x[k], q, p[5]);
                 }
             }
+            Acc s[8] = {};
+#pragma unroll
+            for (int k = 0; k < 6; ++k) s[k] = p[k].low() + p[k].high();
             const Acc v = warp_sums8(s);
             if (t % 4 == 0) part[row & 1][t / 32][t % 32 / 4] = v;
         }
@@ -464,24 +629,28 @@ block_norm_bwd_ring_kernel(const NormArgs a)
             Acc            s[6];
             cta_sums(part[before & 1], warps, s);
             const RowFactors<Acc> q = factors_of(s, of_d, eps, a.w_post != nullptr);
-            void *dx = row_of<Elem>(a.x_out, before, a.d), *df = row_of<Elem>(a.n_out, before, a.d);
+            const Two<Acc> r = both(q.r), rrc = both(-q.rrc), rf = both(q.rf), rf3m = both(-q.rf3m);
+            uint4 *const dx = static_cast<uint4 *>(row_of<Elem>(a.x_out, before, a.d)), *const df = static_cast<uint4 *>(row_of<Elem>(a.n_out, before, a.d));
 #pragma unroll
             for (int j = 0; j < kHold; ++j) {
                 const uint32_t i = j * team + t;
-                Acc x[kW], f[kW], dn[kW], dy[kW], g[kW];
-                X::widen(slot(stage_b, 0, j), x), X::widen(slot(stage_b, 1, j), f), X::widen(slot(stage_b, 2, j), dn), X::widen(slot(stage_b, 3, j), dy);
-                if constexpr (kRowGate) X::widen(slot(stage_b, 4, j), g);
+                Two<Acc> x[kP], f[kP], dn[kP], dy[kP], g[kP];
+                widen_pairs<DT>(slot(stage_b, 0, j), x), widen_pairs<DT>(slot(stage_b, 1, j), f);
+                widen_pairs<DT>(slot(stage_b, 2, j), dn), widen_pairs<DT>(slot(stage_b, 3, j), dy);
+                if constexpr (kRowGate) widen_pairs<DT>(slot(stage_b, 4, j), g);
 #pragma unroll
-                for (int k = 0; k < kW; ++k) {
-                    const Acc tv = dy[k] + q.r * (dn[k] * w_pre[j][k]) - q.rrc * x[k];
-                    sum_pre[j][k] += dn[k] * (x[k] * q.r);
-                    sum_f[j][k] += tv * (f[k] * q.rf);
-                    f[k]  = tv * (kRowGate ? gw[j][k] * g[k] : gw[j][k]) * q.rf - q.rf3m * f[k];
+                for (int k = 0; k < kP; ++k) {
+                    const Two<Acc> tv = fma2(rrc, x[k], fma2(r, dn[k] * w_pre[j][k], dy[k]));
+                    sum_pre[j][k]     = fma2(dn[k], x[k] * r, sum_pre[j][k]);
+                    sum_f[j][k]       = fma2(tv, f[k] * rf, sum_f[j][k]);
+                    Two<Acc> tg       = tv * gw[j][k];
+                    if constexpr (kRowGate) tg = tg * g[k];
+                    f[k]  = fma2(tg, rf, rf3m * f[k]);
                     dy[k] = tv;
                 }
                 if (i < count) {
-                    if (dx) X::store(dx, i, dy, all_x);
-                    if (df) X::store(df, i, f, all_f);
+                    if (dx && all_x.holds(dx + i, 16)) dx[i] = narrow_pairs<DT>(dy);
+                    if (df && all_f.holds(df + i, 16)) df[i] = narrow_pairs<DT>(f);
                 }
             }
             // the last of the group's rows in this chunk: its gate's gradient, or this chunk's share of it
@@ -492,26 +661,29 @@ block_norm_bwd_ring_kernel(const NormArgs a)
 #pragma unroll
                 for (int j = 0; j < kHold; ++j) {
                     const uint32_t i = j * team + t;
-                    Acc            w[kW], g[kW];
+                    Two<Acc>       w[kP], g[kP];
 #pragma unroll
-                    for (int k = 0; k < kW; ++k) w[k] = 1, g[k] = 0;
+                    for (int k = 0; k < kP; ++k) w[k] = both(Acc(1)), g[k] = both(Acc(0));
                     if (i < count) {
-                        if (a.w_post) X::read_shared(a.w_post, i, w);
-                        if (kRowGate) X::widen(slot(stage_b, 4, j), g);
+                        if (a.w_post) read_pairs<DT>(a.w_post, i, w);
+                        if (kRowGate) widen_pairs<DT>(slot(stage_b, 4, j), g);
                     }
 #pragma unroll
-                    for (int k = 0; k < kW; ++k) {
-                        w[k] *= scale * sum_f[j][k];
-                        if constexpr (kRowGate) sum_post[j][k] += scale * g[k] * sum_f[j][k], sum_f[j][k] = 0;
+                    for (int k = 0; k < kP; ++k) {
+                        w[k] = w[k] * both(scale) * sum_f[j][k];
+                        if constexpr (kRowGate) sum_post[j][k] = fma2(both(scale) * g[k], sum_f[j][k], sum_post[j][k]), sum_f[j][k] = both(Acc(0));
                     }
                     if (a.dgate && i < count) {
-                        if (whole) X::store(row_of<Elem>(a.dgate, group, a.d), i, w, all_g);
-                        else
+                        uint4 *const out = static_cast<uint4 *>(row_of<Elem>(a.dgate, group, a.d)) + i;
+                        if (whole) {
+                            if (all_g.holds(out, 16)) *out = narrow_pairs<DT>(w);
+                        } else {
 #pragma unroll
-                            for (int k = 0; k < kW; ++k) {
-                                Acc *const o = reinterpret_cast<Acc *>(a.part_gate) + to * a.d + i * kW + k;
-                                if (part_g.holds(o, sizeof(Acc))) *o = w[k];
+                            for (int k = 0; k < 2 * kP; ++k) {
+                                Acc *const o = reinterpret_cast<Acc *>(a.part_gate) + to * a.d + i * 2 * kP + k;
+                                if (part_g.holds(o, sizeof(Acc))) *o = k % 2 ? w[k / 2].high() : w[k / 2].low();
                             }
+                        }
                     }
                 }
             }
@@ -527,19 +699,21 @@ block_norm_bwd_ring_kernel(const NormArgs a)
         const uint32_t i = j * team + t;
         if (i >= count) continue;
         if (!kRowGate && a.dw_post) {
-            Acc g[kW];
+            Two<Acc> g[kP];
 #pragma unroll
-            for (int k = 0; k < kW; ++k) g[k] = 1;
-            if (a.gate) X::read_shared(a.gate, i, g);
+            for (int k = 0; k < kP; ++k) g[k] = both(Acc(1));
+            if (a.gate) read_pairs<DT>(a.gate, i, g);
 #pragma unroll
-            for (int k = 0; k < kW; ++k) sum_f[j][k] *= scale * g[k];
+            for (int k = 0; k < kP; ++k) sum_f[j][k] = sum_f[j][k] * both(scale) * g[k];
         }
 #pragma unroll
-        for (int k = 0; k < kW; ++k) {
-            const uint64_t o = chunk * a.d + i * kW + k;
-            if (a.dw_pre && part_w.holds(reinterpret_cast<Acc *>(a.part_pre) + o, sizeof(Acc))) reinterpret_cast<Acc *>(a.part_pre)[o] = sum_pre[j][k];
+        for (int k = 0; k < 2 * kP; ++k) {
+            const uint64_t o    = chunk * a.d + i * 2 * kP + k;
+            const Two<Acc> post = kRowGate ? sum_post[kRowGate ? j : 0][k / 2] : sum_f[j][k / 2];
+            if (a.dw_pre && part_w.holds(reinterpret_cast<Acc *>(a.part_pre) + o, sizeof(Acc)))
+                reinterpret_cast<Acc *>(a.part_pre)[o] = k % 2 ? sum_pre[j][k / 2].high() : sum_pre[j][k / 2].low();
             if (a.dw_post && part_p.holds(reinterpret_cast<Acc *>(a.part_post) + o, sizeof(Acc)))
-                reinterpret_cast<Acc *>(a.part_post)[o] = kRowGate ? sum_post[kRowGate ? j : 0][k] : sum_f[j][k];
+                reinterpret_cast<Acc *>(a.part_post)[o] = k % 2 ? post.high() : post.low();
         }
     }
 }
@@ -811,27 +985,58 @@ bool row_fits(uint64_t d, int es)
     return d <= kMaxTeam * (d % lanes == 0 ? 2 * lanes : 8);
 }
 
-template <int DT, bool kVector, int kHold, bool kCta>
-cudaError_t start_fwd(const NormArgs &a, uint32_t threads, cudaStream_t stream)
+// threads of a CTA that holds `count` accesses, `hold` per thread
+uint32_t team_of(uint64_t count, uint32_t hold) { return static_cast<uint32_t>(round_up_div(round_up_div(count, hold), 32) * 32); }
+// Vectors per thread of the ring kernels: two from 64 on, which halves what the sums over a row cost per element; CTAs of an SM:
+// 512 threads' worth.
+uint32_t hold_of(uint64_t count) { return count < 64 ? 1 : 2; }
+
+template <int kHold>
+size_t ring_bytes(uint32_t team, uint32_t operands) { return static_cast<size_t>(kRingStages<kHold>) * operands * kHold * team * 16; }
+constexpr size_t kMostShared = 220 * 1024;
+
+template <typename K>
+cudaError_t start_ring(K kernel, const NormArgs &a, unsigned grid, uint32_t team, size_t smem, cudaStream_t stream)
 {
-    const int sms = sm_count();
-    if (sms == 0) return cudaErrorInvalidDevice;
+    const cudaError_t e = reported(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
+    return e != cudaSuccess ? e : launch(kernel, grid, team, smem, stream, a);
+}
+
+template <int DT, bool kVector, int kHold, bool kCta>
+cudaError_t start_fwd(const NormArgs &a, uint32_t threads, int sms, cudaStream_t stream)
+{
     const uint64_t teams = kCta ? 1 : kWarpTeams, want = round_up_div(a.rows, teams);
     const uint64_t most  = static_cast<uint64_t>(sms) * (2048 / threads);
     return launch(block_norm_fwd_kernel<DT, kVector, kHold, kCta>, static_cast<unsigned>(want < most ? want : most), threads, 0, stream, a);
 }
-template <int DT, bool kVector>
-cudaError_t fwd_of(const NormArgs &a, cudaStream_t stream)
+
+template <int DT>
+cudaError_t forward(const NormArgs &a, cudaStream_t stream)
 {
-    constexpr uint64_t kW    = Access<DT, kVector>::kW;
-    const uint64_t     count = a.d / kW;
-    if (count <= 32) return start_fwd<DT, kVector, 1, false>(a, 32 * kWarpTeams, stream);
-    if (count <= 64) return start_fwd<DT, kVector, 2, false>(a, 32 * kWarpTeams, stream);
-    if (count <= 128) return start_fwd<DT, kVector, 4, false>(a, 32 * kWarpTeams, stream);
-    const auto team = [&](uint64_t hold) { return static_cast<uint32_t>(round_up_div(round_up_div(count, hold), 32) * 32); };
-    if (count <= 2 * kMaxTeam) return start_fwd<DT, kVector, 2, true>(a, team(2), stream);
-    if (count <= 4 * kMaxTeam) return start_fwd<DT, kVector, 4, true>(a, team(4), stream);
-    return start_fwd<DT, kVector, 0, true>(a, kMaxTeam, stream);
+    const int sms = sm_count();
+    if (sms == 0) return cudaErrorInvalidDevice;
+    const uint64_t count = a.d / kLanes<DT>;
+    if (a.d % kLanes<DT> == 0 && count <= 2 * kMaxTeam) {
+        const bool     row_gate = a.gate && a.gate_rows < a.rows;
+        const uint32_t hold = hold_of(count), team = team_of(count, hold);
+        const uint64_t most = static_cast<uint64_t>(sms) * (2 * kMaxTeam / team < 32 ? 2 * kMaxTeam / team : 32);
+        const unsigned grid = static_cast<unsigned>(a.rows < most ? a.rows : most);
+        if (hold == 1)
+            return row_gate ? start_ring(block_norm_fwd_ring_kernel<DT, 1, true>, a, grid, team, ring_bytes<1>(team, 3), stream)
+                            : start_ring(block_norm_fwd_ring_kernel<DT, 1, false>, a, grid, team, ring_bytes<1>(team, 2), stream);
+        return row_gate ? start_ring(block_norm_fwd_ring_kernel<DT, 2, true>, a, grid, team, ring_bytes<2>(team, 3), stream)
+                        : start_ring(block_norm_fwd_ring_kernel<DT, 2, false>, a, grid, team, ring_bytes<2>(team, 2), stream);
+    }
+    if (a.d % kLanes<DT> == 0) {
+        if (count <= 4 * kMaxTeam) return start_fwd<DT, true, 4, true>(a, team_of(count, 4), sms, stream);
+        return start_fwd<DT, true, 0, true>(a, kMaxTeam, sms, stream);
+    }
+    if (a.d <= 32) return start_fwd<DT, false, 1, false>(a, 32 * kWarpTeams, sms, stream);
+    if (a.d <= 64) return start_fwd<DT, false, 2, false>(a, 32 * kWarpTeams, sms, stream);
+    if (a.d <= 128) return start_fwd<DT, false, 4, false>(a, 32 * kWarpTeams, sms, stream);
+    if (a.d <= 2 * kMaxTeam) return start_fwd<DT, false, 2, true>(a, team_of(a.d, 2), sms, stream);
+    if (a.d <= 4 * kMaxTeam) return start_fwd<DT, false, 4, true>(a, team_of(a.d, 4), sms, stream);
+    return start_fwd<DT, false, 0, true>(a, kMaxTeam, sms, stream);
 }
 
 template <int DT, bool kVector, int kHold, bool kCta>
@@ -841,33 +1046,17 @@ cudaError_t start_bwd(const NormArgs &a, uint32_t threads, cudaStream_t stream)
     return launch(block_norm_bwd_kernel<DT, kVector, kHold, kCta>, static_cast<unsigned>(round_up_div(a.chunks, teams)), threads, 0, stream, a);
 }
 
-// threads of a CTA that holds `count` accesses, `hold` per thread
-uint32_t team_of(uint64_t count, uint32_t hold) { return static_cast<uint32_t>(round_up_div(round_up_div(count, hold), 32) * 32); }
-
-template <int kHold>
-size_t ring_bytes(uint32_t team, bool row_gate) { return static_cast<size_t>(kRingStages<kHold>) * (row_gate ? 5 : 4) * kHold * team * 16; }
-constexpr size_t kMostShared = 220 * 1024;
-
-template <int DT, int kHold, bool kRowGate>
-cudaError_t start_ring(const NormArgs &a, uint32_t team, cudaStream_t stream)
-{
-    const auto        kernel = block_norm_bwd_ring_kernel<DT, kHold, kRowGate>;
-    const size_t      smem   = ring_bytes<kHold>(team, kRowGate);
-    const cudaError_t e      = reported(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-    if (e != cudaSuccess) return e;
-    return launch(kernel, a.chunks, team, smem, stream, a);
-}
-
 template <int DT>
 cudaError_t bwd_vectors(const NormArgs &a, cudaStream_t stream)
 {
     const uint64_t count    = a.d / kLanes<DT>;
     const bool     row_gate = a.gate && a.gate_rows < a.rows;
-    if (count <= kMaxTeam)
-        return row_gate ? start_ring<DT, 1, true>(a, team_of(count, 1), stream) : start_ring<DT, 1, false>(a, team_of(count, 1), stream);
-    const uint32_t team = team_of(count, 2);
-    if (!row_gate) return start_ring<DT, 2, false>(a, team, stream);
-    if (ring_bytes<2>(team, true) <= kMostShared) return start_ring<DT, 2, true>(a, team, stream);
+    const uint32_t hold = hold_of(count), team = team_of(count, hold);
+    if (hold == 1)
+        return row_gate ? start_ring(block_norm_bwd_ring_kernel<DT, 1, true>, a, a.chunks, team, ring_bytes<1>(team, 5), stream)
+                        : start_ring(block_norm_bwd_ring_kernel<DT, 1, false>, a, a.chunks, team, ring_bytes<1>(team, 4), stream);
+    if (!row_gate) return start_ring(block_norm_bwd_ring_kernel<DT, 2, false>, a, a.chunks, team, ring_bytes<2>(team, 4), stream);
+    if (ring_bytes<2>(team, 5) <= kMostShared) return start_ring(block_norm_bwd_ring_kernel<DT, 2, true>, a, a.chunks, team, ring_bytes<2>(team, 5), stream);
     return start_bwd<DT, true, 2, true>(a, team, stream);              // five operands of such rows do not fit shared memory three times
 }
 template <int DT>
@@ -886,19 +1075,13 @@ uint32_t chunks_of(uint64_t rows, uint64_t d, int es, int sms)
     const uint64_t lanes = 16 / static_cast<uint64_t>(es), count = d / lanes;
     uint64_t       most;
     if (!row_fits(d, es)) most = kLongChunks;
-    else if (d % lanes == 0) most = static_cast<uint64_t>(sms) * (kMaxTeam / team_of(count, count <= kMaxTeam ? 1 : 2));
+    else if (d % lanes == 0) most = static_cast<uint64_t>(sms) * (kMaxTeam / team_of(count, hold_of(count)));
     else if (d <= 64) most = static_cast<uint64_t>(sms) * 24;
     else most = static_cast<uint64_t>(sms) * (d <= 256 ? 6 : d <= 512 ? 3 : 2);
     if (most > kMaxChunks) most = kMaxChunks;
     if (most > rows) most = rows;
     const uint64_t chunk_rows = round_up_div(rows, most);
     return static_cast<uint32_t>(round_up_div(rows, chunk_rows));
-}
-
-template <int DT>
-cudaError_t forward(const NormArgs &a, cudaStream_t stream)
-{
-    return a.d % kLanes<DT> == 0 ? fwd_of<DT, true>(a, stream) : fwd_of<DT, false>(a, stream);
 }
 
 template <int DT>

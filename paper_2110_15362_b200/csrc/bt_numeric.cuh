@@ -97,6 +97,70 @@ __device__ __forceinline__ uint4 narrow_vec(const typename Num<DT>::Acc (&v)[kLa
     return w;
 }
 
+// Two sums side by side.  Binary32: a register pair, whose operations the architecture performs two at a time.
+template <typename A>
+struct Two {
+    A lo, hi;
+    __device__ static __forceinline__ Two of(A lo, A hi) { return Two{lo, hi}; }
+    __device__ __forceinline__ A low() const { return lo; }
+    __device__ __forceinline__ A high() const { return hi; }
+};
+template <>
+struct Two<float> {
+    uint64_t v;
+    __device__ static __forceinline__ Two of(float lo, float hi)
+    {
+        Two r;
+        asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+        return r;
+    }
+    __device__ __forceinline__ float low() const
+    {
+        return __uint_as_float(static_cast<uint32_t>(v));
+    }
+    __device__ __forceinline__ float high() const
+    {
+        return __uint_as_float(static_cast<uint32_t>(v >> 32));
+    }
+};
+template <typename A>
+__device__ __forceinline__ Two<A> both(A v) { return Two<A>::of(v, v); }
+__device__ __forceinline__ Two<float> operator*(Two<float> a, Two<float> b)
+{
+    Two<float> r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ Two<double> operator*(Two<double> a, Two<double> b) { return {a.lo * b.lo, a.hi * b.hi}; }
+// a b + c
+__device__ __forceinline__ Two<float> fma2(Two<float> a, Two<float> b, Two<float> c)
+{
+    Two<float> r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ Two<double> fma2(Two<double> a, Two<double> b, Two<double> c) { return {fma(a.lo, b.lo, c.lo), fma(a.hi, b.hi, c.hi)}; }
+
+// a 16-byte vector's elements, widened two by two; and back
+template <int DT>
+constexpr int kPairs = kLanes<DT> / 2;
+template <int DT>
+__device__ __forceinline__ void widen_pairs(const uint4 &w, Two<typename Num<DT>::Acc> (&v)[kPairs<DT>])
+{
+    typename Num<DT>::Acc e[kLanes<DT>];
+    widen_vec<DT>(w, e);
+#pragma unroll
+    for (int k = 0; k < kPairs<DT>; ++k) v[k] = Two<typename Num<DT>::Acc>::of(e[2 * k], e[2 * k + 1]);
+}
+template <int DT>
+__device__ __forceinline__ uint4 narrow_pairs(const Two<typename Num<DT>::Acc> (&v)[kPairs<DT>])
+{
+    typename Num<DT>::Acc e[kLanes<DT>];
+#pragma unroll
+    for (int k = 0; k < kPairs<DT>; ++k) e[2 * k] = v[k].low(), e[2 * k + 1] = v[k].high();
+    return narrow_vec<DT>(e);
+}
+
 template <typename A>
 __device__ __forceinline__ A warp_sum(A v)
 {
