@@ -28,8 +28,8 @@ struct NormArgs {
     void       *dgate, *dw_post, *dw_pre;          // backward
     float      *part_pre, *part_post, *part_gate;  // backward: partial rows (double where sums are)
     void       *stats;                             // backward, long rows: r, c, rf, mean(t q) of each row
-    uint64_t    rows, d, gate_rows, chunk_rows;    // chunk_rows: consecutive rows of one team
-    uint32_t    chunks;
+    uint64_t    rows, d, gate_rows, chunk_rows;    // chunk_rows: consecutive rows of one team, at most
+    uint32_t    chunks, group_chunks;              // group_chunks: chunks of one group of rows with a gate; 0: chunks go across groups
     double      scale, eps;
 };
 
@@ -288,18 +288,32 @@ __device__ __forceinline__ void add_sums(Acc (&s)[6], const Acc x, const Acc f, 
     s[5] += x * q;
 }
 
-// The chunk of rows of a team, and the groups of rows (with a gate row each) that it meets: a group that lies inside one chunk
-// has its gradient written at once; of one that crosses chunks every chunk leaves a partial row -- where the group begins in
-// the chunk in slot 2 * chunk + 1, where it came from the chunk before in slot 2 * chunk.
+// The chunk of rows of a team.  Where the groups of rows that share a gate row are few, no chunk goes across groups
+// (group_chunks); a chunk may then be empty.  A group that lies inside one chunk has its gate's gradient written at once; of one of
+// several chunks every chunk leaves a partial row -- where the group begins in the chunk in slot 2 * chunk + 1, where it came from
+// the chunk before in slot 2 * chunk.
 struct Chunk {
     uint64_t first, end;
 };
 __device__ __forceinline__ Chunk chunk_of(const NormArgs &a, const uint32_t chunk)
 {
-    Chunk c;
-    c.first = chunk * a.chunk_rows;
-    c.end   = c.first + a.chunk_rows < a.rows ? c.first + a.chunk_rows : a.rows;
+    Chunk    c;
+    uint64_t end = a.rows;
+    if (a.group_chunks) {
+        const uint64_t group = chunk / a.group_chunks, begin = group * a.gate_rows;
+        end     = begin + a.gate_rows < a.rows ? begin + a.gate_rows : a.rows;
+        c.first = begin + (chunk % a.group_chunks) * a.chunk_rows;
+        if (c.first > end) c.first = end;
+    } else {
+        c.first = chunk * a.chunk_rows;
+    }
+    c.end = c.first + a.chunk_rows < end ? c.first + a.chunk_rows : end;
     return c;
+}
+// the chunk that a row lies in
+__device__ __forceinline__ uint64_t chunk_at(const NormArgs &a, const uint64_t row)
+{
+    return a.group_chunks ? row / a.gate_rows * a.group_chunks + row % a.gate_rows / a.chunk_rows : row / a.chunk_rows;
 }
 // where the sum over the rows [.., row] of a chunk's last group goes: true if it is whole
 __device__ __forceinline__ bool whole_group(const NormArgs &a, const Chunk &c, const uint64_t group, const uint32_t chunk, uint64_t &slot)
@@ -378,7 +392,8 @@ __device__ __forceinline__ void read_pairs(const void *row, const uint32_t i, Tw
 
 // scale * gate * w_post of a thread's columns (kRowGate: without the gate, which changes from row to row)
 template <int DT, int kHold, bool kRowGate>
-__device__ __forceinline__ void branch_factors(const NormArgs &a, const uint32_t count, Two<typename Num<DT>::Acc> (&gw)[kHold][kPairs<DT>])
+__device__ __forceinline__ void branch_factors(const NormArgs &a, const uint64_t group, const uint32_t count,
+                                               Two<typename Num<DT>::Acc> (&gw)[kHold][kPairs<DT>])
 {
     using Acc = typename Num<DT>::Acc;
 #pragma unroll
@@ -394,7 +409,7 @@ __device__ __forceinline__ void branch_factors(const NormArgs &a, const uint32_t
             for (int k = 0; k < kPairs<DT>; ++k) gw[j][k] = gw[j][k] * w[k];
         }
         if (!kRowGate && a.gate) {
-            read_pairs<DT>(a.gate, i, w);
+            read_pairs<DT>(row_of<typename Num<DT>::Elem>(a.gate, group, a.d), i, w);
 #pragma unroll
             for (int k = 0; k < kPairs<DT>; ++k) gw[j][k] = gw[j][k] * w[k];
         }
@@ -423,15 +438,21 @@ block_norm_fwd_ring_kernel(const NormArgs a)
     const auto slot = [&](const uint32_t stage, const int operand, const int j) -> uint4 & {
         return ring[((stage * kOperands + operand) * kHold + j) * team + t];
     };
+    // the row to copy next, and where its vectors and those of the two rows that are written begin
+    const uint64_t stride = static_cast<uint64_t>(gridDim.x) * count;
+    uint64_t       next = blockIdx.x, at_next = next * count + t, at_y = at_next, at_n = at_next;
     // (a commit for every turn, also behind the last row: the waits count groups)
-    const auto fill = [&](const uint32_t stage, const uint64_t row) {
-        if (row < a.rows) {
-            const void *const from[3] = {row_of<Elem>(a.x, row, a.d), row_of<Elem>(a.f, row, a.d), kRowGate ? row_of<Elem>(a.gate, row / a.gate_rows, a.d) : nullptr};
+    const auto fill = [&](const uint32_t stage) {
+        if (next < a.rows) {
+            const uint4 *const x = static_cast<const uint4 *>(a.x) + at_next, *const f = static_cast<const uint4 *>(a.f) + at_next;
 #pragma unroll
             for (int j = 0; j < kHold; ++j)
-#pragma unroll
-                for (int o = 0; o < kOperands; ++o)
-                    if (j * team + t < count && from[o]) copy_ahead(&slot(stage, o, j), static_cast<const uint4 *>(from[o]) + j * team + t);
+                if (j * team + t < count) {
+                    copy_ahead(&slot(stage, 0, j), x + j * team);
+                    if (a.f) copy_ahead(&slot(stage, 1, j), f + j * team);
+                    if constexpr (kRowGate) copy_ahead(&slot(stage, 2, j), static_cast<const uint4 *>(a.gate) + next / a.gate_rows * count + j * team + t);
+                }
+            next += gridDim.x, at_next += stride;
         }
         copy_commit();
     };
@@ -441,10 +462,10 @@ block_norm_fwd_ring_kernel(const NormArgs a)
 #pragma unroll
             for (int o = 0; o < kOperands; ++o)
                 if (j * team + t >= count || (o == 1 && !a.f)) slot(s, o, j) = make_uint4(0, 0, 0, 0);
-    for (uint32_t s = 0; s + 1 < stages; ++s) fill(s, blockIdx.x + static_cast<uint64_t>(s) * gridDim.x);
+    for (uint32_t s = 0; s + 1 < stages; ++s) fill(s);
 
     Two<Acc> gw[kHold][kP], w_pre[kHold][kP], y[kHold][kP];
-    branch_factors<DT, kHold, kRowGate>(a, count, gw);
+    branch_factors<DT, kHold, kRowGate>(a, 0, count, gw);
 #pragma unroll
     for (int j = 0; j < kHold; ++j) {
 #pragma unroll
@@ -473,9 +494,9 @@ block_norm_fwd_ring_kernel(const NormArgs a)
         }
         if (turn >= 2 && a.n_out) {
             // ---- n of the row two before, whose x' waits in y
-            const uint64_t row = blockIdx.x + (turn - 2) * gridDim.x;
             const Two<Acc> r   = both(root_of(cta_sum(before[1], warps) * of_d + eps));
-            uint4 *const   out = static_cast<uint4 *>(row_of<Elem>(a.n_out, row, a.d));
+            uint4 *const   out = static_cast<uint4 *>(a.n_out) + at_n;
+            at_n += stride;
 #pragma unroll
             for (int j = 0; j < kHold; ++j) {
                 const uint32_t i = j * team + t;
@@ -483,14 +504,14 @@ block_norm_fwd_ring_kernel(const NormArgs a)
                 Two<Acc> n[kP];
 #pragma unroll
                 for (int k = 0; k < kP; ++k) n[k] = y[j][k] * r * w_pre[j][k];
-                if (all_n.holds(out + i, 16)) out[i] = narrow_pairs<DT>(n);
+                if (all_n.holds(out + j * team, 16)) out[j * team] = narrow_pairs<DT>(n);
             }
         }
         if (turn >= 1 && turn <= mine) {
             // ---- x' of the row before
-            const uint64_t row = blockIdx.x + (turn - 1) * gridDim.x;
             const Two<Acc> rf  = both(a.w_post ? root_of(cta_sum(before[0], warps) * of_d + eps) : Acc(1));
-            uint4 *const   out = static_cast<uint4 *>(row_of<Elem>(a.x_out, row, a.d));
+            uint4 *const   out = static_cast<uint4 *>(a.x_out) + at_y;
+            at_y += stride;
             Two<Acc>       s   = both(Acc(0));
 #pragma unroll
             for (int j = 0; j < kHold; ++j) {
@@ -509,7 +530,7 @@ block_norm_fwd_ring_kernel(const NormArgs a)
                     y[j][k] = fma2(f[k] * rf, gw[j][k], y[j][k]);
                     s       = fma2(y[j][k], y[j][k], s);
                 }
-                if (out && i < count && all_x.holds(out + i, 16)) out[i] = narrow_pairs<DT>(y[j]);
+                if (a.x_out && i < count && all_x.holds(out + j * team, 16)) out[j * team] = narrow_pairs<DT>(y[j]);
             }
             if (a.n_out) {
                 const Acc v = warp_sum(s.low() + s.high());
@@ -518,7 +539,7 @@ block_norm_fwd_ring_kernel(const NormArgs a)
             stage_b = stage_b + 1 == stages ? 0 : stage_b + 1;
         }
         __syncthreads();                                               // this turn's sums are there; those of the turn before are free
-        fill(stage_c, blockIdx.x + (turn + stages - 1) * gridDim.x);
+        fill(stage_c);
         stage_c = stage_c + 1 == stages ? 0 : stage_c + 1;
         stage_a = stage_a + 1 == stages ? 0 : stage_a + 1;
     }
@@ -547,21 +568,29 @@ block_norm_bwd_ring_kernel(const NormArgs a)
     const Extent   all_g = extent_of(a.dgate, round_up_div(a.rows, a.gate_rows) * a.d * sizeof(Elem));
     const Extent   part_g = extent_of(a.part_gate, 2ull * a.chunks * a.d * sizeof(Acc));
     const Extent   part_w = extent_of(a.part_pre, a.chunks * a.d * sizeof(Acc)), part_p = extent_of(a.part_post, a.chunks * a.d * sizeof(Acc));
-    const Chunk    c      = chunk_of(a, chunk);
+    const Chunk    c        = chunk_of(a, chunk);
+    const uint64_t of_chunk = a.group_chunks ? chunk / a.group_chunks : 0;       // the group of all its rows, unless kRowGate
 
     const auto slot = [&](const uint32_t stage, const int operand, const int j) -> uint4 & {
         return ring[((stage * kOperands + operand) * kHold + j) * team + t];
     };
+    // the row to copy next, and where its vectors and those of the row that is written begin
+    uint64_t next = c.first, at_next = next * count + t, at_out = at_next;
     // (a commit for every row of the ring, also behind the chunk's end: the waits count groups)
-    const auto fill = [&](const uint32_t stage, const uint64_t row) {
-        if (row < c.end) {
-            const void *const from[5] = {row_of<Elem>(a.x, row, a.d), row_of<Elem>(a.f, row, a.d), row_of<Elem>(a.dn, row, a.d),
-                                         row_of<Elem>(a.dy, row, a.d), kRowGate ? row_of<Elem>(a.gate, row / a.gate_rows, a.d) : nullptr};
+    const auto fill = [&](const uint32_t stage) {
+        if (next < c.end) {
+            const uint4 *const x = static_cast<const uint4 *>(a.x) + at_next, *const f = static_cast<const uint4 *>(a.f) + at_next;
+            const uint4 *const dn = static_cast<const uint4 *>(a.dn) + at_next, *const dy = static_cast<const uint4 *>(a.dy) + at_next;
 #pragma unroll
             for (int j = 0; j < kHold; ++j)
-#pragma unroll
-                for (int o = 0; o < kOperands; ++o)
-                    if (j * team + t < count && from[o]) copy_ahead(&slot(stage, o, j), static_cast<const uint4 *>(from[o]) + j * team + t);
+                if (j * team + t < count) {
+                    copy_ahead(&slot(stage, 0, j), x + j * team);
+                    if (a.f) copy_ahead(&slot(stage, 1, j), f + j * team);
+                    if (a.dn) copy_ahead(&slot(stage, 2, j), dn + j * team);
+                    if (a.dy) copy_ahead(&slot(stage, 3, j), dy + j * team);
+                    if constexpr (kRowGate) copy_ahead(&slot(stage, 4, j), static_cast<const uint4 *>(a.gate) + next / a.gate_rows * count + j * team + t);
+                }
+            ++next, at_next += count;
         }
         copy_commit();
     };
@@ -572,10 +601,10 @@ block_norm_bwd_ring_kernel(const NormArgs a)
 #pragma unroll
             for (int o = 0; o < kOperands; ++o)
                 if (j * team + t >= count || (o == 1 && !a.f) || (o == 2 && !a.dn) || (o == 3 && !a.dy)) slot(s, o, j) = make_uint4(0, 0, 0, 0);
-    for (uint32_t s = 0; s + 1 < stages; ++s) fill(s, c.first + s);
+    for (uint32_t s = 0; s + 1 < stages; ++s) fill(s);
 
     Two<Acc> w_pre[kHold][kP], gw[kHold][kP];
-    branch_factors<DT, kHold, kRowGate>(a, count, gw);
+    branch_factors<DT, kHold, kRowGate>(a, of_chunk, count, gw);
 #pragma unroll
     for (int j = 0; j < kHold; ++j) {
 #pragma unroll
@@ -630,7 +659,8 @@ block_norm_bwd_ring_kernel(const NormArgs a)
             cta_sums(part[before & 1], warps, s);
             const RowFactors<Acc> q = factors_of(s, of_d, eps, a.w_post != nullptr);
             const Two<Acc> r = both(q.r), rrc = both(-q.rrc), rf = both(q.rf), rf3m = both(-q.rf3m);
-            uint4 *const dx = static_cast<uint4 *>(row_of<Elem>(a.x_out, before, a.d)), *const df = static_cast<uint4 *>(row_of<Elem>(a.n_out, before, a.d));
+            uint4 *const dx = static_cast<uint4 *>(a.x_out) + at_out, *const df = static_cast<uint4 *>(a.n_out) + at_out;
+            at_out += count;
 #pragma unroll
             for (int j = 0; j < kHold; ++j) {
                 const uint32_t i = j * team + t;
@@ -649,8 +679,8 @@ block_norm_bwd_ring_kernel(const NormArgs a)
                     dy[k] = tv;
                 }
                 if (i < count) {
-                    if (dx && all_x.holds(dx + i, 16)) dx[i] = narrow_pairs<DT>(dy);
-                    if (df && all_f.holds(df + i, 16)) df[i] = narrow_pairs<DT>(f);
+                    if (a.x_out && all_x.holds(dx + j * team, 16)) dx[j * team] = narrow_pairs<DT>(dy);
+                    if (a.n_out && all_f.holds(df + j * team, 16)) df[j * team] = narrow_pairs<DT>(f);
                 }
             }
             // the last of the group's rows in this chunk: its gate's gradient, or this chunk's share of it
@@ -690,7 +720,7 @@ block_norm_bwd_ring_kernel(const NormArgs a)
             stage_b = stage_b + 1 == stages ? 0 : stage_b + 1;
         }
         __syncthreads();                                               // the sums of this row are there; the words of the one before are free
-        fill(stage_c, row + stages - 1);
+        fill(stage_c);
         stage_c = stage_c + 1 == stages ? 0 : stage_c + 1;
         stage_a = stage_a + 1 == stages ? 0 : stage_a + 1;
     }
@@ -702,7 +732,7 @@ block_norm_bwd_ring_kernel(const NormArgs a)
             Two<Acc> g[kP];
 #pragma unroll
             for (int k = 0; k < kP; ++k) g[k] = both(Acc(1));
-            if (a.gate) read_pairs<DT>(a.gate, i, g);
+            if (a.gate) read_pairs<DT>(row_of<Elem>(a.gate, of_chunk, a.d), i, g);
 #pragma unroll
             for (int k = 0; k < kP; ++k) sum_f[j][k] = sum_f[j][k] * both(scale) * g[k];
         }
@@ -938,7 +968,8 @@ block_norm_finish_kernel(const NormArgs a)
     const uint64_t i    = static_cast<uint64_t>(blockIdx.x % columns) * kFinishColumns + lane;
     const Acc     *from;
     Elem          *to;
-    uint64_t       count, stride = a.d, size = a.d;
+    uint64_t       count;
+    bool           across = false;                                     // from one chunk to the next, slots of a gate group
     if (what < 2) {
         from  = reinterpret_cast<const Acc *>(what == 0 ? a.part_pre : a.part_post);
         to    = static_cast<Elem *>(what == 0 ? a.dw_pre : a.dw_post);
@@ -947,31 +978,36 @@ block_norm_finish_kernel(const NormArgs a)
     } else {
         if (!a.dgate) return;
         uint64_t group = what - 2;
-        if (round_up_div(a.rows, a.gate_rows) >= a.chunks) {            // by borders
+        if (round_up_div(a.rows, a.gate_rows) >= a.chunks && !a.group_chunks) {                  // by borders
             const uint64_t border = (what - 1) * a.chunk_rows;          // the next chunk's first row
             if (border >= a.rows || border % a.gate_rows == 0) return;
             group = border / a.gate_rows;
             if (group * a.gate_rows / a.chunk_rows != what - 2) return;  // (a group across several borders: at its first)
         }
         const uint64_t begin = group * a.gate_rows, end = begin + a.gate_rows < a.rows ? begin + a.gate_rows : a.rows;
-        const uint64_t from_chunk = begin / a.chunk_rows, to_chunk = (end - 1) / a.chunk_rows;
+        const uint64_t from_chunk = chunk_at(a, begin), to_chunk = chunk_at(a, end - 1);
         if (from_chunk == to_chunk) return;                             // written whole
         // slot 2 * chunk + 1 of the first chunk, then slot 2 * chunk of the others, one after the other every second row
         from   = reinterpret_cast<const Acc *>(a.part_gate) + (2 * from_chunk + 1) * a.d;
         to     = static_cast<Elem *>(a.dgate) + group * a.d;
         count  = to_chunk - from_chunk + 1;
-        stride = 0;
+        across = true;
     }
     Acc s = 0;
-    if (i < a.d) {
-        for (uint64_t k = share; k < count; k += kSplit) s += from[(stride ? k * a.d : (k == 0 ? 0 : (2 * k - 1) * a.d)) + i];
+    if (i < a.d && share < count) {
+        const Acc     *at   = from + i + (across ? (share == 0 ? 0 : 2 * share - 1) : share) * a.d;
+        const uint64_t step = (across ? 2 : 1) * kSplit * a.d;
+        s = *at;
+        at += step - (across && share == 0 ? a.d : 0);                  // (slot 2 * chunk + 1 of the first chunk is one row nearer)
+#pragma unroll 8
+        for (uint64_t k = share + kSplit; k < count; k += kSplit, at += step) s += *at;
     }
     part[share][lane] = s;
     __syncthreads();
     if (share != 0 || i >= a.d) return;
 #pragma unroll
     for (int k = 1; k < kSplit; ++k) s += part[k][lane];
-    if (extent_of(to, size * sizeof(Elem)).holds(to + i, sizeof(Elem))) to[i] = Num<DT>::narrow(s);
+    if (extent_of(to, a.d * sizeof(Elem)).holds(to + i, sizeof(Elem))) to[i] = Num<DT>::narrow(s);
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -1050,7 +1086,7 @@ template <int DT>
 cudaError_t bwd_vectors(const NormArgs &a, cudaStream_t stream)
 {
     const uint64_t count    = a.d / kLanes<DT>;
-    const bool     row_gate = a.gate && a.gate_rows < a.rows;
+    const bool     row_gate = a.gate && !a.group_chunks;
     const uint32_t hold = hold_of(count), team = team_of(count, hold);
     if (hold == 1)
         return row_gate ? start_ring(block_norm_bwd_ring_kernel<DT, 1, true>, a, a.chunks, team, ring_bytes<1>(team, 5), stream)
@@ -1069,7 +1105,7 @@ cudaError_t bwd_elements(const NormArgs &a, cudaStream_t stream)
     return start_bwd<DT, false, 8, true>(a, team_of(a.d, 8), stream);
 }
 
-// The chunks of a backward pass: as many teams as the SMs hold at a time.
+// The most chunks of a backward pass: as many teams as the SMs hold at a time.
 uint32_t chunks_of(uint64_t rows, uint64_t d, int es, int sms)
 {
     const uint64_t lanes = 16 / static_cast<uint64_t>(es), count = d / lanes;
@@ -1079,9 +1115,24 @@ uint32_t chunks_of(uint64_t rows, uint64_t d, int es, int sms)
     else if (d <= 64) most = static_cast<uint64_t>(sms) * 24;
     else most = static_cast<uint64_t>(sms) * (d <= 256 ? 6 : d <= 512 ? 3 : 2);
     if (most > kMaxChunks) most = kMaxChunks;
-    if (most > rows) most = rows;
-    const uint64_t chunk_rows = round_up_div(rows, most);
-    return static_cast<uint32_t>(round_up_div(rows, chunk_rows));
+    if (most > rows / 4) most = rows / 4 > static_cast<uint64_t>(sms) ? rows / 4 : static_cast<uint64_t>(sms);   // partial rows cost, too
+    return static_cast<uint32_t>(most < rows ? most : rows);
+}
+// how the rows are dealt: inside the groups of rows with a gate while every group can have a chunk
+void set_chunks(NormArgs &a, uint32_t most)
+{
+    const uint64_t groups = a.gate ? round_up_div(a.rows, a.gate_rows) : 1, group_rows = a.gate && a.gate_rows < a.rows ? a.gate_rows : a.rows;
+    if (groups <= most) {
+        const uint64_t each = most / groups < group_rows ? most / groups : group_rows;
+        a.chunk_rows        = round_up_div(group_rows, each);
+        a.group_chunks      = static_cast<uint32_t>(round_up_div(group_rows, a.chunk_rows));
+        a.chunks            = static_cast<uint32_t>(groups) * a.group_chunks;
+        a.gate_rows         = group_rows;
+    } else {
+        a.chunk_rows   = round_up_div(a.rows, most);
+        a.group_chunks = 0;
+        a.chunks       = static_cast<uint32_t>(round_up_div(a.rows, a.chunk_rows));
+    }
 }
 
 template <int DT>
@@ -1102,7 +1153,7 @@ cudaError_t backward(const NormArgs &a, cudaStream_t stream)
     }
     if (e != cudaSuccess || (!a.dgate && !a.dw_pre && !a.dw_post)) return e;
     const uint64_t groups = round_up_div(a.rows, a.gate_rows), borders = a.chunks - 1;
-    const uint64_t shared = a.dgate ? (groups < borders ? groups : borders) : 0;
+    const uint64_t shared = a.dgate ? (a.group_chunks || groups < borders ? groups : borders) : 0;
     return launch(block_norm_finish_kernel<DT>, static_cast<unsigned>(round_up_div(a.d, kFinishColumns) * (2 + shared)), kFinishColumns * kSplit, 0,
                   stream, a);
 }
@@ -1110,8 +1161,7 @@ cudaError_t backward(const NormArgs &a, cudaStream_t stream)
 size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 
 struct Parts {
-    uint32_t chunks;
-    uint64_t chunk_rows;
+    uint32_t chunks;                             // at most
     size_t   pre, post, gate, stats, bytes;      // offsets
 };
 // the workspace of a backward pass; sms: 0 for the most that any GPU could ask for
@@ -1120,7 +1170,6 @@ Parts parts_of(uint64_t rows, uint64_t d, int es, int sms)
     const size_t acc = es == 8 ? 8 : 4;
     Parts        p{};
     p.chunks     = chunks_of(rows, d, es, sms);
-    p.chunk_rows = round_up_div(rows, p.chunks);
     const size_t row = d * acc;
     p.pre   = 0;
     p.post  = round_up(p.chunks * row);
@@ -1219,7 +1268,8 @@ int bt_block_norm_bwd(const void *x_out, uint64_t rows, uint64_t d, uint64_t gat
         a.part_pre = reinterpret_cast<float *>(w + p.pre), a.part_post = reinterpret_cast<float *>(w + p.post);
         a.part_gate = reinterpret_cast<float *>(w + p.gate), a.stats = w + p.stats;
     }
-    a.rows = rows, a.d = d, a.gate_rows = gate_rows, a.chunks = p.chunks, a.chunk_rows = p.chunk_rows;
+    a.rows = rows, a.d = d, a.gate_rows = gate_rows;
+    bt::set_chunks(a, p.chunks);
     a.scale = scale, a.eps = eps;
     return bt::dispatch(dtype, [&](auto dt) { return bt::backward<decltype(dt)::value>(a, s); });
 }

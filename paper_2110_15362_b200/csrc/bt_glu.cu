@@ -272,6 +272,7 @@ int bt_glu_fwd(const void *x, uint64_t rows, uint64_t d_in, uint64_t d_ff, int d
     bt::GluCall c{};
     c.x = x, c.w_gate = w_gate, c.w_up = w_up, c.h = h, c.g = g_out, c.u = u_out;
     c.rows = rows, c.d_in = d_in, c.d_ff = d_ff, c.dtype = dtype, c.act = activation, c.dev_status = dev_status;
+    if (bt::glu_rows_takes(c)) return bt::launch_glu_rows(c, s) == cudaSuccess ? BT_OK : BT_ERR_CUDA;
     if (bt::glu_mma_takes(c)) return bt::launch_glu_mma_fwd(c, s) == cudaSuccess ? BT_OK : BT_ERR_CUDA;
     return bt::dispatch(dtype, [&](auto dt) { return bt::forward_of<decltype(dt)::value>(c, s); });
 }

@@ -71,6 +71,10 @@ bool        glu_mma_takes(const GluCall &c);
 cudaError_t launch_glu_mma_fwd(const GluCall &c, cudaStream_t stream);
 cudaError_t launch_glu_mma_bwd(const GluCall &c, cudaStream_t stream);
 
+// The forward pass for few rows (bt_glu_rows.cu).
+bool        glu_rows_takes(const GluCall &c);
+cudaError_t launch_glu_rows(const GluCall &c, cudaStream_t stream);
+
 // calls go(std::integral_constant<int, DT>, std::integral_constant<int, ACT>) for a call's type and activation
 template <int DT, typename F>
 cudaError_t with_act(int act, const F &go)

@@ -80,6 +80,17 @@ def test_forward(size, kind):
     check_forward(x, wg, wu, act, kind, forward(x, wg, wu, act))
 
 
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("rows", [1, 2, 3, 4, 5, 8, 9, 16, 17, 31, 32, 33])
+@pytest.mark.parametrize("d,ff", [(8, 8), (40, 24), (2048, 264), (2056, 8), (1000, 1004)])
+def test_few_rows(rows, d, ff, kind):
+    """Every form for few rows: parts of the summed axis that end inside a piece, columns beyond the last."""
+    x, wg, wu = make(rows, d, ff, kind, seed=rows)
+    act = ACTS[rows % 4]
+    check_forward(x, wg, wu, act, kind, forward(x, wg, wu, act))
+    check_forward(x, wg, wu, act, kind, forward(x, wg, wu, act, save=False))
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("kind", KINDS)
 def test_activations(act, kind):
