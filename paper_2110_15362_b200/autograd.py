@@ -20,6 +20,9 @@ pre-allocated arena (the ``*_arena`` entry points): no host read in the forward 
 words are checked once, when the backward pass first asks for a tensor.  The cursor is reset on entering
 the context, so one context entry covers one forward / backward pass.
 
+For transformer blocks: ``glu_stash`` (gated feed-forward whose saved projections, with a ReLU gate, live under one
+bitmap), ``block_norm`` (the norms around a block with its gate and residual scale) and ``clip_grad_norm``.
+
 ``double_mask(out, like)`` is the double-mask form for normalisation layers: ``out`` (e.g. a batch-norm output)
 is zeroed wherever ``like`` (the layer's input, a post-ReLU tensor) is zero, and its stash reuses the bitmap and
 the prefix array of ``like``'s stash (``bt_mask_compress``); the backward pass masks the gradient with the same
@@ -59,7 +62,7 @@ except ImportError as e:
 
 __all__ = ["PackedActivation", "stash_saved_activations", "relu_stash", "ReLUStash", "relu6_stash", "ReLU6Stash",
            "double_mask", "DoubleMask", "maxpool2x2_stash", "MaxPool2x2Stash", "relu_maxpool2x2_stash",
-           "ReLUMaxPool2x2Stash"]
+           "ReLUMaxPool2x2Stash", "glu_stash", "GLUStash", "block_norm", "BlockNorm", "clip_grad_norm"]
 
 
 class _Record:
@@ -752,3 +755,167 @@ class ReLUMaxPool2x2Stash(torch.autograd.Function):
 def relu_maxpool2x2_stash(x: torch.Tensor, hooks: Optional[stash_saved_activations] = None) -> torch.Tensor:
     """``max_pool2d(relu(x), 2)`` with the pooling moved in front of the ReLU (see ``ReLUMaxPool2x2Stash``)."""
     return ReLUMaxPool2x2Stash.apply(x, hooks)
+
+
+def _on_current_device(call: str, *tensors: Optional[torch.Tensor]) -> None:
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != torch._C._cuda_getDevice()):
+            raise ValueError(f"{call}: the tensors must be on the current CUDA device, not on {t.device}")
+
+
+def _dense(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
+    return None if t is None else _flat_input(t)
+
+
+class GLUStash(torch.autograd.Function):
+    """h = act(x w_gate^T) * (x w_up^T) (``bt_glu_fwd`` / ``bt_glu_bwd``).  The backward pass needs both projections.  With a
+    ReLU gate and a context they are kept as stashes: the gate compressed, the other projection and the output under
+    the gate's bitmap (``bt_mask_compress``), wherever the gate is sparse enough to gain by it."""
+
+    @staticmethod
+    def forward(ctx, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activation: str = "relu",
+                hooks: Optional[stash_saved_activations] = None):
+        _on_current_device("glu_stash", x, w_gate, w_up)
+        xc, wg, wu = _flat_input(x), _flat_input(w_gate), _flat_input(w_up)
+        d_ff, d_in = wg.shape
+        h = torch.empty((*xc.shape[:-1], d_ff), dtype=xc.dtype, device=xc.device)
+        keep = any(ctx.needs_input_grad[:3])
+        g, u = (torch.empty_like(h), torch.empty_like(h)) if keep else (None, None)
+        rows = xc.numel() // max(d_in, 1)
+        status = hooks.statuses.next(xc.device) if hooks is not None else None
+        B.bt_glu_fwd(xc, wg, wu, h, g, u, B.new_glu_workspace(rows, d_in, d_ff, xc.dtype, xc.device),
+                     None if status is None else status[1].words[status[2]:status[2] + 1], activation=activation)
+        if status is not None:
+            hooks.statuses.made(status)
+        ctx.activation, ctx.packed = activation, None
+        if keep:
+            if hooks is not None and activation == "relu" and h.numel() >= hooks.min_numel:
+                ctx.packed = GLUStash._stash(h, g, u, hooks)
+            if ctx.packed is not None:
+                ctx.save_for_backward(xc, wg, wu)
+            else:
+                ctx.save_for_backward(xc, wg, wu, g, u)
+        return h
+
+    @staticmethod
+    def _stash(h: torch.Tensor, g: torch.Tensor, u: torch.Tensor, hooks: stash_saved_activations):
+        """The stashes of g and u (u's under g's bitmap), h's shared with the next layer's save; None if they would not be
+        smaller.  (A zero of h under an open gate is a stored value.)"""
+        record, values, nnz = _compress(g, hooks.scratch)
+        n, es = g.numel(), g.element_size()
+        if B.bt_compressed_bytes(n, nnz, g.dtype) > (1.0 - hooks.min_saving) * n * es:
+            return None
+        packed = [_packed(g, record, values, nnz)]
+        for t in (u, h):
+            under = torch.empty(max(nnz, 1), dtype=t.dtype, device=t.device)
+            B.bt_mask_compress(t.view(-1), record.bitmap, record.chunk_prefix, None, under, values_capacity=nnz)
+            packed.append(_packed(t, record, under[:nnz], nnz))
+        hooks.share(h, packed[2])
+        hooks.packed_bytes += packed[0].nbytes() + 2 * nnz * es       # the bitmap and the prefix array are kept once
+        hooks.dense_bytes += 3 * n * es
+        return packed[:2]
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad: torch.Tensor):
+        if ctx.packed is not None:
+            xc, wg, wu = ctx.saved_tensors
+            g, u = (p.unpack() for p in ctx.packed)
+        else:
+            xc, wg, wu, g, u = ctx.saved_tensors
+        dh = _flat_input(grad)
+        need_x, need_g, need_u = ctx.needs_input_grad[:3]
+        dx = torch.empty_like(xc) if need_x else None
+        dwg, dwu = (torch.empty_like(wg), torch.empty_like(wu)) if need_g or need_u else (None, None)
+        d_ff, d_in = wg.shape
+        rows = xc.numel() // max(d_in, 1)
+        B.bt_glu_bwd(dh, g, u, xc, wg, wu, dx, dwg, dwu, B.new_glu_workspace(rows, d_in, d_ff, xc.dtype, xc.device, backward=True),
+                     activation=ctx.activation)
+        return dx, dwg if need_g else None, dwu if need_u else None, None, None
+
+
+def glu_stash(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activation: str = "relu",
+              hooks: Optional[stash_saved_activations] = None) -> torch.Tensor:
+    """Gated feed-forward block of (..., d_in) tensors, weights (d_ff, d_in): ``act(x @ w_gate.T) * (x @ w_up.T)`` in one
+    kernel; `activation` "relu", "silu", "gelu" or "gelu_tanh".  Pass the active context as `hooks` to keep what the
+    backward pass needs as stashes (ReLU; see ``GLUStash``).  All three tensors have one element type."""
+    return GLUStash.apply(x, w_gate, w_up, activation, hooks)
+
+
+class BlockNorm(torch.autograd.Function):
+    """``bt_block_norm_fwd`` / ``bt_block_norm_bwd``; what is kept for the backward pass is x_out, f, gate and weights."""
+
+    @staticmethod
+    def forward(ctx, x, f, gate, w_post, w_pre, scale: float, eps: float):
+        _on_current_device("block_norm", x, f, gate, w_post, w_pre)
+        xc, fc, gc, post, pre = _flat_input(x), _dense(f), _dense(gate), _dense(w_post), _dense(w_pre)
+        y = torch.empty_like(xc) if fc is not None else None
+        n = torch.empty_like(xc) if pre is not None else None
+        B.bt_block_norm_fwd(xc, fc, gc, post, pre, y, n, scale=scale, eps=eps)
+        ctx.save_for_backward(xc if y is None else y, fc, gc, post, pre)
+        ctx.scale, ctx.eps = scale, eps
+        ctx.set_materialize_grads(False)
+        return y, n
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_y, grad_n):
+        y, f, gate, post, pre = ctx.saved_tensors
+        if grad_y is None and grad_n is None:
+            return (None,) * 7
+        need = ctx.needs_input_grad
+        if grad_n is None:
+            pre = None                                 # (w_pre's gradient is zero then: left out)
+        out = [torch.empty_like(t) if t is not None and w else None for t, w in ((y, need[0]), (f, need[1]), (gate, need[2]), (post, need[3]), (pre, need[4]))]
+        rows = y.numel() // max(y.shape[-1], 1)
+        B.bt_block_norm_bwd(y, f, gate, post, pre, _dense(grad_n), _dense(grad_y), *out,
+                            B.new_block_norm_workspace(rows, y.shape[-1], 1, y.dtype, y.device), scale=ctx.scale, eps=ctx.eps)
+        return (*out, None, None)
+
+
+def block_norm(x: torch.Tensor, f: Optional[torch.Tensor] = None, *, gate: Optional[torch.Tensor] = None,
+               w_post: Optional[torch.Tensor] = None, w_pre: Optional[torch.Tensor] = None, scale: float = 1.0, eps: float = 1e-6):
+    """The residual sum behind a block and the norm before the next one, (..., d) tensors:
+    ``y = x + scale * gate * rms(f) * w_post`` (without w_post: ``f`` itself), ``n = rms(y) * w_pre``.  Returns (y, n);
+    only y without w_pre, only n without f.  gate: (d,), or (groups, d) with a row for each of as many equal runs of rows."""
+    if f is None and (gate is not None or w_post is not None or w_pre is None):
+        raise ValueError("block_norm: without f there is only rms(x) * w_pre")
+    y, n = BlockNorm.apply(x, f, gate, w_post, w_pre, float(scale), float(eps))
+    return n if f is None else y if w_pre is None else (y, n)
+
+
+def clip_grad_norm(parameters, max_norm: float) -> torch.Tensor:
+    """Scales the gradients of `parameters` (tensors; those without a gradient are skipped, the same one twice counts once) in
+    place by min(1, max_norm / (norm + 1e-6)), norm being that of all of them together, and returns the norm (float32,
+    0-dimensional, on the device; nothing is read on the host).  Gradients of one element type: two launches; several: the sums
+    type by type, then the products."""
+    if not max_norm >= 0:
+        raise ValueError("clip_grad_norm: max_norm must not be negative")
+    if isinstance(parameters, torch.Tensor):
+        parameters = [parameters]
+    grads = list({id(p): p.grad for p in parameters if p.grad is not None}.values())
+    if not grads:
+        return torch.zeros((), dtype=torch.float32, device="cuda")
+    for g in grads:
+        if g.layout != torch.strided or g.dtype not in B.DTYPE_CODE:
+            raise ValueError(f"clip_grad_norm: dense floating-point gradients only, not {g.layout} {g.dtype}")
+    _on_current_device("clip_grad_norm", *grads)
+    dense = [_flat_input(g) for g in grads]                             # a gradient that the library cannot take: a copy, copied back
+    norm = torch.empty(1, dtype=torch.float32, device=grads[0].device)
+    kinds: Dict[torch.dtype, list] = {}
+    for g in dense:
+        kinds.setdefault(g.dtype, []).append(g)
+    calls = [(dtype, B.grad_items(gs), B.new_grad_workspace([g.numel() for g in gs], norm.device)) for dtype, gs in kinds.items()]
+    if len(calls) == 1:
+        dtype, items, ws = calls[0]
+        B.bt_grad_clip_batch(items, dtype, max_norm, norm, ws)
+    else:
+        sumsq = torch.empty(1, dtype=torch.float64, device=norm.device)
+        for k, (dtype, items, ws) in enumerate(calls):
+            B.bt_grad_norm_batch(items, dtype, sumsq, norm, ws, accumulate=k > 0)
+        for dtype, items, _ in calls:
+            B.bt_grad_scale_batch(items, dtype, max_norm, sumsq)
+    for g, c in zip(grads, dense):
+        if c is not g:
+            g.copy_(c)
+    return norm[0]

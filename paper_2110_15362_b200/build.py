@@ -20,7 +20,7 @@ AUTOGRAD_PATH = os.path.join(PKG_DIR, "_autograd" + (sysconfig.get_config_var("E
 AUTOGRAD_BUILT_FOR = os.path.join(PKG_DIR, "_autograd.built_for")      # the torch version that AUTOGRAD_PATH fits
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-Xcompiler", "-fPIC", "-shared"]
+              "-Xcompiler", "-fPIC", "-shared", "--threads", "0"]       # one thread of nvcc per source
 
 
 def sources():

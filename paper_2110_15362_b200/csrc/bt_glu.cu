@@ -236,8 +236,8 @@ size_t padded(uint64_t rows, uint64_t d_ff, int es) { return (rows * d_ff * stat
 
 size_t workspace_of(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, bool backward)
 {
-    (void)d_in;
-    return backward ? 2 * padded(rows, d_ff, element_size(dtype)) : 0;
+    if (rows == 0) return 0;
+    return backward ? 2 * padded(rows, d_ff, element_size(dtype)) + glu_mma_scratch(rows, d_in, d_ff, dtype) : 0;
 }
 
 }  // namespace
@@ -306,6 +306,7 @@ int bt_glu_bwd(const void *grad_h, uint64_t rows, uint64_t d_in, uint64_t d_ff, 
     bt::GluCall    c{};
     c.x = x, c.w_gate = w_gate, c.w_up = w_up, c.dg = slope.dg, c.du = slope.du, c.dx = grad_x, c.dw_gate = grad_w_gate, c.dw_up = grad_w_up;
     c.rows = rows, c.d_in = d_in, c.d_ff = d_ff, c.dtype = dtype, c.act = activation, c.dev_status = dev_status;
+    c.scratch = w + 2 * bt::padded(rows, d_ff, static_cast<int>(es));
     return bt::dispatch(dtype, [&](auto dt) {
         const cudaError_t e = bt::slopes_of<decltype(dt)::value>(slope, activation, s);
         if (e != cudaSuccess) return e;

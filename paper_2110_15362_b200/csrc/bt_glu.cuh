@@ -61,6 +61,7 @@ struct GluCall {
     void       *h, *g, *u;                         // forward: [rows, d_ff]; g and u may be NULL
     const void *dg, *du;                           // backward: [rows, d_ff], the gradients of g and u
     void       *dx, *dw_gate, *dw_up;              // backward: any may be NULL
+    void       *scratch;                           // backward: glu_mma_scratch bytes
     uint64_t    rows, d_in, d_ff;
     int         dtype, act;
     int32_t    *dev_status;
@@ -68,6 +69,7 @@ struct GluCall {
 
 // The products on the tensor cores (bt_glu_mma.cu): types and sizes that they take; forward; backward from c.dg and c.du.
 bool        glu_mma_takes(const GluCall &c);
+size_t      glu_mma_scratch(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype);    // bytes that a backward pass needs
 cudaError_t launch_glu_mma_fwd(const GluCall &c, cudaStream_t stream);
 cudaError_t launch_glu_mma_bwd(const GluCall &c, cudaStream_t stream);
 

@@ -48,6 +48,10 @@ struct MmaArgs {
     uint32_t    tiles_i, tiles_j, tiles;               // of one output; of all
     uint32_t    outputs;                               // forward: bit 0 h, bit 1 g, bit 2 u
     uint64_t    size_i, size_j;                        // of an output
+    // kInputGrad with few tiles: the summed axis of a tile is dealt to `splits` units of split_blocks each, whose sums go to
+    // `partial` in binary32 (join_kernel adds them up)
+    uint32_t    splits, split_blocks;
+    float4     *partial;
     int32_t    *dev_status;
 };
 
@@ -101,7 +105,7 @@ __device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, 
 {
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.bulk_group [%0, {%1, %2}], [%3];" ::"l"(map), "r"(x), "r"(y), "r"(from) : "memory");
 }
-__device__ __forceinline__ void bulk_wait_all() { asm volatile("cp.async.bulk.wait_group 0;" ::: "memory"); }
+__device__ __forceinline__ void prefetch_map(const CUtensorMap *map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 
 __device__ __forceinline__ void mma_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
 {
@@ -250,6 +254,7 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
         *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
+    if (warp == 0 && lane < 7) prefetch_map(lane < 2 ? &p.a[lane] : lane < 4 ? &p.b[lane - 2] : &p.out[lane - 4]);
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_word)), "r"(2 * kN) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
@@ -264,15 +269,23 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
 
     const uint32_t first = blockIdx.x / 2, step = gridDim.x / 2;
     const uint32_t blocks = p.blocks * (kUse == kInputGrad ? 2 : 1);
+    const bool     split  = kUse == kInputGrad && p.splits > 1;
+    // the part of the summed axis of unit t
+    const auto from_block = [&](const uint32_t t) { return split ? t % p.splits * p.split_blocks : 0u; };
+    const auto end_block = [&](const uint32_t t) {
+        const uint32_t end = from_block(t) + p.split_blocks;
+        return split && end < blocks ? end : blocks;
+    };
     if (warp == 0) {
         // ---- loader
         if (lane == 0) {
             Ring<kStages> ring;
             bool          ok = true;
             for (uint32_t t = first; t < p.tiles && ok; t += step) {
-                const Tile tile = tile_at(p, t);
-                const int  i0 = static_cast<int>(tile.i * 256 + rank * kRows);
-                for (uint32_t k = 0; k < blocks; ++k) {
+                const Tile     tile = tile_at(p, split ? t / p.splits : t);
+                const int      i0   = static_cast<int>(tile.i * 256 + rank * kRows);
+                const uint32_t end  = end_block(t);
+                for (uint32_t k = from_block(t); k < end; ++k) {
                     if (!(ok = wait(empty(ring.stage), ring.phase ^ 1))) break;
                     const uint32_t a = base + ring.stage * (S::kABytes + S::kBBytes), b = a + S::kABytes;
                     const uint32_t bar = in_first_cta(full(ring.stage));
@@ -315,14 +328,15 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
                 if (!(ok = wait(taken(half.stage), half.phase ^ 1))) break;
                 tmem_fence_after();
                 const uint32_t d = tmem + half.stage * kN;
-                for (uint32_t k = 0; k < blocks; ++k) {
+                const uint32_t begin = from_block(t), end = end_block(t);
+                for (uint32_t k = begin; k < end; ++k) {
                     if (!(ok = wait(full(ring.stage), ring.phase))) break;
                     tmem_fence_after();
                     const uint32_t a = base + ring.stage * (S::kABytes + S::kBBytes), b = a + S::kABytes;
                     const uint64_t da = operand<kAcrossA>(a), db = operand<kAcrossB>(b);
 #pragma unroll
                     for (int q = 0; q < kDepth / 16; ++q)
-                        mma_pair(d, da + q * (kStep<kAcrossA> >> 4), db + q * (kStep<kAcrossB> >> 4), kIdesc, k != 0 || q != 0);
+                        mma_pair(d, da + q * (kStep<kAcrossA> >> 4), db + q * (kStep<kAcrossB> >> 4), kIdesc, k != begin || q != 0);
                     commit_pair(empty(ring.stage));
                     ring.next();
                 }
@@ -341,7 +355,7 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
         constexpr uint32_t kItems  = kUse == kForward ? kChunks * 3 : kChunks;
         Ring<2> half;
         for (uint32_t t = first; t < p.tiles; t += step) {
-            const Tile tile = tile_at(p, t);
+            const Tile tile = tile_at(p, split ? t / p.splits : t);
             const uint32_t i0 = tile.i * 256 + rank * kRows + quarter * 32;
             if (!wait(ready(half.stage), half.phase)) break;
             tmem_fence_after();
@@ -351,6 +365,23 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
                 const uint32_t j0 = tile.j * (kUse == kForward ? kN / 2 : kN) + chunk * 64;
                 if (kUse == kForward && !(p.outputs >> what & 1)) continue;
                 if (j0 >= p.size_j || i0 >= p.size_i) continue;         // (the whole warp alike)
+                if (split) {
+                    // as they lie in TMEM, four columns of 32 rows at a time
+                    float4 *const out = p.partial + ((static_cast<uint64_t>(t) * 2 + rank) * kChunks + chunk) * (16 * kRows) + quarter * 32 + lane;
+                    const Extent  all = extent_of(p.partial, static_cast<uint64_t>(p.tiles) * 2 * kChunks * (16 * kRows) * sizeof(float4));
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        uint32_t v[32];
+                        tmem_load(from + chunk * 64 + part * 32, v);
+                        tmem_load_wait();
+#pragma unroll
+                        for (int c = 0; c < 8; ++c)
+                            if (all.holds(out + (part * 8 + c) * kRows, sizeof(float4)))
+                                out[(part * 8 + c) * kRows] = make_float4(__uint_as_float(v[4 * c]), __uint_as_float(v[4 * c + 1]),
+                                                                          __uint_as_float(v[4 * c + 2]), __uint_as_float(v[4 * c + 3]));
+                    }
+                    continue;
+                }
                 uint32_t packed[32];
 #pragma unroll
                 for (int part = 0; part < 2; ++part) {
@@ -394,7 +425,7 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
             if (lane == 0) mbar_arrive_cluster(in_first_cta(taken(half.stage)));
             half.next();
         }
-        if (lane == 0) bulk_wait_all();
+        if (lane == 0) bulk_wait_read<0>();
         __syncwarp();
     }
     __syncthreads();
@@ -408,6 +439,30 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
     cluster_sync();
     tmem_fence_after();
     if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kN) : "memory");
+}
+
+// The sums of a tile's units added up, rounded and written: a CTA takes eight columns of a CTA's 128 rows.
+template <int DT, int kN>
+__global__ void __launch_bounds__(kRows)
+join_kernel(const float4 *__restrict__ partial, const uint32_t splits, void *to, const uint64_t size_i, const uint64_t size_j, const MmaArgs p)
+{
+    in_stream_order();
+    constexpr uint32_t kChunks = kN / 64;
+    uint32_t           b       = blockIdx.x;
+    const uint32_t eight = b % 8, chunk = (b /= 8) % kChunks, rank = (b /= kChunks) % 2;
+    const uint32_t t     = b / 2;
+    const Tile     tile  = tile_at(p, t);
+    const uint64_t i = tile.i * 256ull + rank * kRows + threadIdx.x, j = tile.j * static_cast<uint64_t>(kN) + chunk * 64 + eight * 8;
+    if (i >= size_i || j >= size_j) return;
+    float s[8] = {};
+    for (uint32_t k = 0; k < splits; ++k) {
+        const float4 *const from = partial + ((static_cast<uint64_t>(t * splits + k) * 2 + rank) * kChunks + chunk) * (16 * kRows) + eight * 2 * kRows + threadIdx.x;
+        const float4 lo = from[0], hi = from[kRows];
+        s[0] += lo.x, s[1] += lo.y, s[2] += lo.z, s[3] += lo.w, s[4] += hi.x, s[5] += hi.y, s[6] += hi.z, s[7] += hi.w;
+    }
+    // (size_j is a multiple of 8)
+    uint4 *const out = reinterpret_cast<uint4 *>(static_cast<typename Num<DT>::Elem *>(to) + i * size_j + j);
+    if (extent_of(to, size_i * size_j * 2).holds(out, 16)) *out = narrow_vec<DT>(s);
 }
 
 // ---------------------------------------------------------------------------------------------- host side
@@ -458,12 +513,22 @@ bool set_tiles(MmaArgs &p, uint64_t size_i, uint64_t size_j, uint32_t columns, u
     return tiles < 0x7FFFFFFFull;
 }
 
-// Tiles of 256 or of 128 columns: what the pairs of CTAs take one after the other, a tile of 128 columns counted as 11 and one
-// of 256 as 16.  (Half the columns need three quarters of the loads: bf16 8192 x 4096 x 11264 runs at 800 TFLOP/s in
-// tiles of 128 columns and at 1400 in tiles of 256.)
-uint64_t rounds(uint64_t size_i, uint64_t size_j, uint64_t outputs, uint32_t columns, uint32_t cost, int sms)
+// How long `units` tiles of `blocks` blocks of 64 summed elements take, in ns.  A block of a 256 x 256 tile is 512 cycles of the
+// tensor cores and 64 KB from the L2, one of a 256 x 128 tile half of the former and three quarters of the latter: 280
+// and 208 ns where few pairs of CTAs run (a CTA reads 64 bytes a cycle), and more where the L2's 10.5 TB/s are shared by many.
+double tiles_ns(uint64_t units, uint64_t blocks, uint32_t columns, uint64_t pairs)
 {
-    return round_up_div(round_up_div(size_i, 256) * round_up_div(size_j, columns) * outputs, static_cast<uint64_t>(sms) / 2) * cost;
+    const double alone = columns == 256 ? 280 : 208, shared = columns == 256 ? 6.24 : 4.68;
+    const auto   block = [&](uint64_t active) { return alone > shared * static_cast<double>(active) ? alone : shared * static_cast<double>(active); };
+    double       ns    = static_cast<double>(units / pairs) * block(pairs);
+    if (units % pairs) ns += block(units % pairs);
+    return ns * static_cast<double>(blocks);
+}
+// Tiles of 256 or of 128 columns (columns256 output columns, or half of them)?
+bool wide_tiles(uint64_t size_i, uint64_t size_j, uint64_t outputs, uint64_t columns256, uint64_t blocks, int sms)
+{
+    const uint64_t pairs = static_cast<uint64_t>(sms) / 2, rows = round_up_div(size_i, 256) * outputs;
+    return tiles_ns(rows * round_up_div(size_j, columns256), blocks, 256, pairs) <= tiles_ns(rows * round_up_div(size_j, columns256 / 2), blocks, 128, pairs);
 }
 
 template <int DT, int kN>
@@ -481,8 +546,33 @@ cudaError_t forward_of(const GluCall &c, int sms, cudaStream_t stream)
     return with_act<DT>(c.act, [&](auto dt, auto act) { return start<decltype(dt)::value, kForward, decltype(act)::value, kN>(p, stream, sms); });
 }
 
+// How the input gradient is computed: columns of a tile and units per tile.  Units cost the store of their sums (1 us where
+// a pair of CTAs ends), a second launch (2 us) and 87 ns per 256 KB of sums that go out and in.
+struct SplitPlan {
+    uint32_t columns, splits, split_blocks;
+    uint64_t tiles;
+};
+SplitPlan input_grad_plan(uint64_t rows, uint64_t d_in, uint64_t d_ff, int sms)
+{
+    const uint64_t pairs = static_cast<uint64_t>(sms) / 2, blocks = 2 * round_up_div(d_ff, kDepth);
+    SplitPlan      best{};
+    double         least = 0;
+    for (const uint32_t columns : {256u, 128u}) {
+        const uint64_t tiles = round_up_div(rows, 256) * round_up_div(d_in, columns);
+        for (uint32_t splits = 1; splits <= 32 && (splits == 1 || blocks / splits >= 4); ++splits) {
+            const uint64_t each = round_up_div(blocks, splits);
+            if (round_up_div(blocks, each) != splits) continue;         // (a unit would be empty)
+            double cost = tiles_ns(tiles * splits, each, columns, pairs);
+            if (splits > 1) cost += 3000 + static_cast<double>(tiles * splits) * 87 * (columns / 256.0);
+            if (least == 0 || cost < least) least = cost, best = SplitPlan{columns, splits, static_cast<uint32_t>(each), tiles};
+        }
+    }
+    return best;
+}
+uint64_t partial_bytes(const SplitPlan &s) { return s.splits == 1 ? 0 : s.tiles * s.splits * 256 * s.columns * sizeof(float); }
+
 template <int DT, int kN>
-cudaError_t input_grad_of(const GluCall &c, int sms, cudaStream_t stream)
+cudaError_t input_grad_of(const GluCall &c, const SplitPlan &s, int sms, cudaStream_t stream)
 {
     MmaArgs    p{};
     const bool ok = map_of(p.a[0], DT, c.dg, c.rows, c.d_ff, kRows) && map_of(p.a[1], DT, c.du, c.rows, c.d_ff, kRows) &&
@@ -491,7 +581,12 @@ cudaError_t input_grad_of(const GluCall &c, int sms, cudaStream_t stream)
     if (!ok || !set_tiles(p, c.rows, c.d_in, kN, 1)) return cudaErrorInvalidValue;
     p.blocks     = static_cast<uint32_t>(round_up_div(c.d_ff, kDepth));
     p.dev_status = c.dev_status;
-    return start<DT, kInputGrad, BT_ACT_RELU, kN>(p, stream, sms);
+    p.splits = s.splits, p.split_blocks = s.split_blocks, p.partial = static_cast<float4 *>(c.scratch);
+    const uint32_t tiles = p.tiles;
+    p.tiles *= s.splits;
+    const cudaError_t e = start<DT, kInputGrad, BT_ACT_RELU, kN>(p, stream, sms);
+    if (e != cudaSuccess || s.splits == 1) return e;
+    return launch(join_kernel<DT, kN>, tiles * 2 * (kN / 64) * 8, kRows, 0, stream, p.partial, s.splits, c.dx, c.rows, c.d_in, p);
 }
 
 template <int DT, int kN>
@@ -510,19 +605,19 @@ cudaError_t weight_grad_of(const GluCall &c, int sms, cudaStream_t stream)
 template <int DT>
 cudaError_t forward(const GluCall &c, int sms, cudaStream_t stream)
 {
-    return rounds(c.rows, c.d_ff, 1, 128, 16, sms) <= rounds(c.rows, c.d_ff, 1, 64, 11, sms) ? forward_of<DT, 256>(c, sms, stream)
+    return wide_tiles(c.rows, c.d_ff, 1, 128, round_up_div(c.d_in, kDepth), sms) ? forward_of<DT, 256>(c, sms, stream)
                                                                                                : forward_of<DT, 128>(c, sms, stream);
 }
 template <int DT>
 cudaError_t backward(const GluCall &c, int sms, cudaStream_t stream)
 {
     if (c.dx) {
-        const cudaError_t e = rounds(c.rows, c.d_in, 1, 256, 16, sms) <= rounds(c.rows, c.d_in, 1, 128, 11, sms) ? input_grad_of<DT, 256>(c, sms, stream)
-                                                                                                                   : input_grad_of<DT, 128>(c, sms, stream);
+        const SplitPlan   s = input_grad_plan(c.rows, c.d_in, c.d_ff, sms);
+        const cudaError_t e = s.columns == 256 ? input_grad_of<DT, 256>(c, s, sms, stream) : input_grad_of<DT, 128>(c, s, sms, stream);
         if (e != cudaSuccess) return e;
     }
     if (!c.dw_gate) return cudaSuccess;
-    return rounds(c.d_ff, c.d_in, 2, 256, 16, sms) <= rounds(c.d_ff, c.d_in, 2, 128, 11, sms) ? weight_grad_of<DT, 256>(c, sms, stream)
+    return wide_tiles(c.d_ff, c.d_in, 2, 256, round_up_div(c.rows, kDepth), sms) ? weight_grad_of<DT, 256>(c, sms, stream)
                                                                                                : weight_grad_of<DT, 128>(c, sms, stream);
 }
 
@@ -531,6 +626,13 @@ cudaError_t backward(const GluCall &c, int sms, cudaStream_t stream)
 bool glu_mma_takes(const GluCall &c)
 {
     return (c.dtype == BT_F16 || c.dtype == BT_BF16) && c.d_in % 8 == 0 && c.d_ff % 8 == 0 && encoder() != nullptr;
+}
+
+size_t glu_mma_scratch(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype)
+{
+    if ((dtype != BT_F16 && dtype != BT_BF16) || d_in % 8 != 0 || d_ff % 8 != 0) return 0;
+    const int sms = sm_count();
+    return partial_bytes(input_grad_plan(rows, d_in, d_ff, sms ? sms : 148));
 }
 
 cudaError_t launch_glu_mma_fwd(const GluCall &c, cudaStream_t stream)

@@ -1,6 +1,6 @@
 """A VGG-16-shaped training step with and without the stash (random weights, random images).
 
-    python -m paper_2110_15362_b200.demo_vgg_step [--batch 32] [--size 224] [--dtype f32|bf16] [--arena-gib 8]
+    python -m paper_2110_15362_b200.demo_vgg_step [--batch 32] [--size 224] [--dtype f32|bf16] [--arena-gib 8] [--clip-norm 1.0]
 
 Builds the thirteen 3x3 convolutions and five 2x2 max-pools of VGG-16 (no batch normalisation, a small
 linear head), runs forward + backward several ways -- plain PyTorch (in-place ReLU), saved activations
@@ -46,6 +46,10 @@ def make_weights(dtype, device, seed=0):
     return ws, head
 
 
+CLIP = []          # the norm that the gradients of all weights together are clipped to, if there is one
+NORMS = []         # the gradients' norms, one per step that clipped
+
+
 def step(x, ws, head, relu, pool=lambda t: F.max_pool2d(t, 2), relu_before_pool=None, relu_pool=None):
     """`relu_before_pool`: the activation used where a pooling layer follows (default: `relu`).  `relu_pool`: one
     call that does the activation and the pooling layer behind it (replaces both there)."""
@@ -66,6 +70,8 @@ def step(x, ws, head, relu, pool=lambda t: F.max_pool2d(t, 2), relu_before_pool=
     del h, logits
     HELD.append(torch.cuda.memory_allocated())                # what the graph holds between the two passes
     loss.backward()
+    if CLIP:
+        NORMS.append(A.clip_grad_norm(ws + [head], CLIP[0]))
     for w in ws + [head]:
         w.grad = None
     return float(loss.detach())
@@ -99,7 +105,9 @@ def main(argv=None) -> int:
     ap.add_argument("--size", type=int, default=224)
     ap.add_argument("--dtype", choices=["f32", "bf16"], default="f32")
     ap.add_argument("--arena-gib", type=float, default=8.0)
+    ap.add_argument("--clip-norm", type=float, default=None, help="clip the gradients of every step to this norm")
     args = ap.parse_args(argv)
+    CLIP[:] = [] if args.clip_norm is None else [args.clip_norm]
 
     B.lib()
     dev = torch.device("cuda")
@@ -178,6 +186,8 @@ def main(argv=None) -> int:
 
         out["stashed_arena_bf16_values"] = measure(arena_narrow)
         out["stashed_arena_bf16_values"]["arena_used_mib"] = round(int(narrow_hooks.cursor.item()) / 2 ** 20, 1)
+    if NORMS:
+        out["grad_norm"] = round(float(NORMS[-1]), 6)
     print(json.dumps(out))
     return 0
 

@@ -1,0 +1,229 @@
+"""The transformer-block operators together, as a training step uses them: norm, gated feed-forward, projection, gated and
+scaled residual sum with the next norm, loss, backward pass, clipping -- against the same step in 64 bits, with and without
+stashes, on other streams; and what the autograd functions refuse."""
+import pytest
+import torch
+import torch.nn.functional as F
+
+from paper_2110_15362_b200 import binding as B
+from tests.block_util import DT, HALF, gen, normal
+
+pytestmark = pytest.mark.gpu
+ROWS, D, FF = 320, 128, 344
+
+
+@pytest.fixture(scope="module")
+def A():
+    B.lib()
+    from paper_2110_15362_b200 import autograd
+    return autograd
+
+
+def weights(kind, layers=2, d=D, ff=FF, seed=0):
+    g = gen(seed)
+    out = []
+    for _ in range(layers):
+        out.append({"pre": normal(g, (d,), kind, 0.1, 1.0), "gate_w": normal(g, (ff, d), kind, d ** -0.5), "up": normal(g, (ff, d), kind, d ** -0.5),
+                    "down": normal(g, (d, ff), kind, ff ** -0.5), "post": normal(g, (d,), kind, 0.1, 1.0), "gate": normal(g, (d,), kind, 0.2, 1.0)})
+    out.append({"pre": normal(g, (d,), kind, 0.1, 1.0)})
+    for w in out:
+        for t in w.values():
+            t.requires_grad_()
+    return out
+
+
+def step(A, x, ws, act, hooks=None):
+    n = A.block_norm(x, w_pre=ws[0]["pre"])
+    for w, after in zip(ws[:-1], ws[1:]):
+        h = A.glu_stash(n, w["gate_w"], w["up"], act, hooks)
+        x, n = A.block_norm(x, F.linear(h, w["down"]), gate=w["gate"], w_post=w["post"], w_pre=after["pre"], scale=0.5)
+    return (n.double() ** 2).mean() + (x.double() * n.double()).mean()
+
+
+def reference(x, ws, act):
+    rms = lambda v, w: v / torch.sqrt((v * v).mean(-1, keepdim=True) + 1e-6) * w  # noqa: E731
+    f = {"relu": torch.relu, "silu": F.silu, "gelu": F.gelu, "gelu_tanh": lambda g: F.gelu(g, approximate="tanh")}[act]
+    n = rms(x, ws[0]["pre"])
+    for w, after in zip(ws[:-1], ws[1:]):
+        p = (f(n @ w["gate_w"].T) * (n @ w["up"].T)) @ w["down"].T
+        x = x + 0.5 * w["gate"] * rms(p, w["post"])
+        n = rms(x, after["pre"])
+    return (n ** 2).mean() + (x * n).mean()
+
+
+def flat(ws):
+    return [t for w in ws for t in w.values()]
+
+
+def gradients(A, kind, act, hooks=None, seed=0):
+    ws = weights(kind, seed=seed)
+    x = normal(gen(seed + 50), (4, ROWS // 4, D), kind).requires_grad_()
+    loss = step(A, x, ws, act, hooks)
+    loss.backward()
+    return loss.detach(), [x.grad] + [t.grad for t in flat(ws)], x, ws
+
+
+@pytest.mark.parametrize("act", ["relu", "silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16", "f64"])
+def test_step_against_64_bits(A, kind, act):
+    loss, grads, x, ws = gradients(A, kind, act)
+    xd = x.detach().double().requires_grad_()
+    wd = [{k: t.detach().double().requires_grad_() for k, t in w.items()} for w in ws]
+    ref = reference(xd, wd, act)
+    ref.backward()
+    # about fifteen tensors are rounded one after the other between x and a gradient, each off by HALF relative at most, in
+    # norm; a closed gate can open by a rounding (a step of act' on a share of 2 HALF of the elements), hence the square root
+    tol = 15 * HALF[kind] + (HALF[kind] ** 0.5 if act == "relu" and kind != "f64" else 0) + (1e-5 if kind == "f32" else 0) + 1e-12
+    assert abs(float(loss) - float(ref.detach())) <= tol * abs(float(ref.detach()))
+    for got, want in zip(grads, [xd.grad] + [t.grad for t in flat(wd)]):
+        assert ((got.double() - want).norm() / want.norm()).item() <= tol
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16"])
+@pytest.mark.parametrize("arena", [None, 1 << 26])
+def test_stashes_change_no_gradient(A, kind, arena):
+    loss, want, *_ = gradients(A, kind, "relu")
+    hooks = A.stash_saved_activations(min_numel=1024, arena_bytes=arena)
+    with hooks:
+        got_loss, got, *_ = gradients(A, kind, "relu", hooks)
+        if arena is None:
+            assert 0 < hooks.packed_bytes < 0.75 * hooks.dense_bytes
+    assert torch.equal(loss, got_loss)
+    for a, b in zip(got, want):
+        assert torch.equal(a, b)
+
+
+def test_a_gate_that_is_open_everywhere_is_not_stashed(A):
+    x = torch.ones(64, 64, device="cuda").requires_grad_()
+    w = torch.full((96, 64), 0.01, device="cuda").requires_grad_()
+    hooks = A.stash_saved_activations(min_numel=1024)
+    with hooks:
+        h = A.glu_stash(x, w, w, "relu", hooks)
+        assert h.grad_fn.packed is None
+        h.sum().backward()
+    assert torch.isfinite(x.grad).all()
+
+
+def test_side_stream_and_strided_inputs(A):
+    _, want, *_ = gradients(A, "bf16", "silu")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        _, got, *_ = gradients(A, "bf16", "silu")
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    ws = weights("f32")
+    x = normal(gen(3), (D, 40), "f32").t().requires_grad_()          # not contiguous
+    a, b = A.glu_stash(x, ws[0]["gate_w"], ws[0]["up"], "gelu"), A.glu_stash(x.contiguous(), ws[0]["gate_w"], ws[0]["up"], "gelu")
+    assert torch.equal(a, b)
+    a.backward(normal(gen(4), (FF, 40), "f32").t())
+    assert x.grad.shape == x.shape
+
+
+def test_gradients_that_are_not_wanted(A):
+    ws = weights("f32")
+    x = normal(gen(5), (24, D), "f32")
+    with torch.no_grad():
+        h = A.glu_stash(x, ws[0]["gate_w"], ws[0]["up"], "silu")
+    assert not h.requires_grad
+    h = A.glu_stash(x, ws[0]["gate_w"], ws[0]["up"].detach(), "silu")
+    h.sum().backward()
+    assert x.grad is None and ws[0]["gate_w"].grad is not None
+    y, n = A.block_norm(x, x * 2, w_pre=ws[0]["pre"])
+    y.sum()                                                          # n unused: its gradient is None
+    n.sum().backward()
+    assert ws[0]["pre"].grad is not None
+
+
+def test_backward_from_one_output(A):
+    """A gradient of y alone leaves w_pre without one; of n alone reaches all."""
+    ws = weights("f32", seed=9)
+    x, f = (normal(gen(k), (24, D), "f32").requires_grad_() for k in (6, 7))
+    y, _ = A.block_norm(x, f, w_post=ws[0]["post"], w_pre=ws[0]["pre"])
+    y.sum().backward()
+    assert torch.allclose(x.grad, torch.ones_like(x)) and ws[0]["pre"].grad is None and ws[0]["post"].grad is not None
+    _, n = A.block_norm(x, f, w_post=ws[0]["post"], w_pre=ws[0]["pre"])
+    n.sum().backward()
+    assert ws[0]["pre"].grad is not None
+
+
+@pytest.mark.parametrize("kinds", [("f32",), ("bf16",), ("f32", "bf16"), ("f64", "f16", "bf16")])
+def test_clipping_of_parameters(A, kinds):
+    g = gen(11)
+    params = []
+    for k, n in enumerate([1000, 3, 40000, 17]):
+        p = torch.nn.Parameter(torch.zeros(n, dtype=DT[kinds[k % len(kinds)]], device="cuda"))
+        p.grad = normal(g, (n,), kinds[k % len(kinds)])
+        params.append(p)
+    strided = torch.nn.Parameter(torch.zeros(30, 20, device="cuda"))
+    strided.grad = torch.randn(20, 30, device="cuda").t()
+    params += [strided, torch.nn.Parameter(torch.zeros(5, device="cuda")), params[0]]        # one without a gradient, one twice
+    olds = [p.grad.double().clone() for p in params if p.grad is not None][:-1]
+    want = torch.stack([o.norm() for o in olds]).norm().item()
+    norm = A.clip_grad_norm(params, 1.0)
+    assert norm.dim() == 0 and abs(float(norm) - want) <= 2 ** -20 * want
+    for p, o in zip([p for p in params if p.grad is not None], olds):
+        assert ((p.grad.double() - o / (want + 1e-6)).norm() / o.norm() * want).item() < 2 ** -8
+    assert float(A.clip_grad_norm([params[-2]], 1.0)) == 0.0
+
+
+def test_refusals(A):
+    x, w = torch.zeros(4, 16, device="cuda"), torch.zeros(8, 16, device="cuda")
+    with pytest.raises(ValueError, match="current CUDA device"):
+        A.glu_stash(x.cpu(), w.cpu(), w.cpu())
+    with pytest.raises(ValueError, match="one element type"):
+        A.glu_stash(x, w.bfloat16(), w)
+    with pytest.raises(ValueError, match="activation"):
+        A.glu_stash(x, w, w, "tanh")
+    with pytest.raises(ValueError, match="without f"):
+        A.block_norm(x, gate=torch.zeros(16, device="cuda"), w_pre=torch.zeros(16, device="cuda"))
+    with pytest.raises(ValueError, match="negative"):
+        A.clip_grad_norm([x], -1.0)
+    p = torch.nn.Parameter(x)
+    p.grad = torch.zeros(4, 16, device="cuda").to_sparse()
+    with pytest.raises(ValueError, match="dense"):
+        A.clip_grad_norm([p], 1.0)
+
+
+def test_a_step_replayed_from_a_graph():
+    """Forward, backward and clipping captured once (the library's calls on kept buffers), replayed on new inputs."""
+    g = gen(31)
+    x, dh = normal(g, (70, D), "bf16"), normal(g, (70, FF), "bf16")
+    wg, wu = (normal(g, (FF, D), "bf16", D ** -0.5) for _ in range(2))
+    h, gg, u = (torch.empty(70, FF, dtype=torch.bfloat16, device="cuda") for _ in range(3))
+    grads = [torch.empty_like(x), torch.empty_like(wg), torch.empty_like(wu)]
+    n, pre, norm = torch.empty_like(x), normal(g, (D,), "bf16"), torch.empty(1, device="cuda")
+    ws = B.new_glu_workspace(70, D, FF, torch.bfloat16, backward=True)
+    gws = B.new_grad_workspace([t.numel() for t in grads])
+    items = B.grad_items(grads)
+
+    def go():
+        B.bt_block_norm_fwd(x, None, None, None, pre, None, n)
+        B.bt_glu_fwd(n, wg, wu, h, gg, u, ws, activation="relu")
+        B.bt_glu_bwd(dh, gg, u, n, wg, wu, *grads, ws, activation="relu")
+        B.bt_grad_clip_batch(items, torch.bfloat16, 0.5, norm, gws)
+
+    graph = torch.cuda.CUDAGraph()
+    go()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        go()
+    for seed in (1, 2):
+        x.copy_(normal(gen(seed), (70, D), "bf16"))
+        go()
+        want = [t.clone() for t in (h, *grads, norm)]
+        for t in (h, *grads, norm):
+            t.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((h, *grads, norm), want))
+
+
+def test_demo_clips(A, capsys):
+    import json
+
+    from paper_2110_15362_b200 import demo_vgg_step
+    demo_vgg_step.main(["--batch", "1", "--size", "32", "--arena-gib", "0.05", "--clip-norm", "0.25"])
+    out = json.loads(capsys.readouterr().out)
+    assert out["grad_norm"] > 0 and out["plain"]["loss"] == pytest.approx(out["stashed"]["loss"], rel=1e-4)
+    demo_vgg_step.CLIP.clear()

@@ -15,6 +15,7 @@ from paper_2110_15362_b200 import binding as B
 from tests import checking_libs as C
 from tests import gpu_util
 from tests import test_gpu_arena, test_gpu_batch, test_gpu_host_forms, test_gpu_mask, test_gpu_maxpool
+from tests import test_gpu_block_norm, test_gpu_glu, test_gpu_grad
 from tests import test_gpu_narrow, test_gpu_parity, test_gpu_prune, test_gpu_relu6, test_gpu_tile_deal
 
 pytestmark = pytest.mark.gpu
@@ -120,3 +121,25 @@ def test_arena_batch_that_runs_full(checked, oracle):
 
 def test_host_forms(checked, oracle):
     test_gpu_host_forms.test_host_round_trip_and_relu_pair(oracle, "bf16", 8192 * 5 + 123)
+
+
+# ---- operators of a transformer block
+@pytest.mark.parametrize("kind", KINDS)
+def test_gated_feed_forward(checked, kind):
+    for size in [(1, 72, 136), (5, 72, 136), (65, 129, 67), (257, 520, 392), (33, 64, 104)]:
+        test_gpu_glu.test_forward(size, kind)
+        test_gpu_glu.test_backward(size, kind)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_block_norms(checked, kind):
+    for size in [(5, 7), (37, 72), (33, 520), (9, 1025), (3, 8193), (3, 20001)]:
+        test_gpu_block_norm.test_forward(size, kind)
+        test_gpu_block_norm.test_backward(size, kind)
+    test_gpu_block_norm.test_gate_groups(6000, 5, 72, "bf16")
+    test_gpu_block_norm.test_gate_groups(6000, 3000, 33, "f32")
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_gradient_clipping(checked, kind):
+    test_gpu_grad.test_clip(kind, 0.5)
