@@ -155,6 +155,7 @@ struct SlopeArgs {
     const void *dh, *g, *u;
     void       *dg, *du;
     uint64_t    n;
+    bool        planes;      // binary32, n a multiple of 8: dg and du as three planes of bfloat16
     int32_t    *dev_status;
 };
 template <int DT, int kAct>
@@ -182,6 +183,31 @@ slopes_kernel(const SlopeArgs p)
     const uint64_t i   = static_cast<uint64_t>(blockIdx.x) * kThreads + threadIdx.x, vecs = p.n / kW;
     const Extent   eg = extent_of(p.dg, p.n * sizeof(Elem)), eu = extent_of(p.du, p.n * sizeof(Elem));
     if (p.dev_status && i == 0) *p.dev_status = BT_OK;
+    if constexpr (DT == BT_F32) {
+        if (p.planes) {
+            if (i >= p.n / 8) return;
+            float dg[8], du[8];
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+                float dh[4], g[4], u[4];
+                widen_vec<DT>(__ldg(static_cast<const uint4 *>(p.dh) + 2 * i + q), dh);
+                widen_vec<DT>(__ldg(static_cast<const uint4 *>(p.g) + 2 * i + q), g);
+                widen_vec<DT>(__ldg(static_cast<const uint4 *>(p.u) + 2 * i + q), u);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) slopes<DT, kAct>(dh[k], g[k], u[k], dg[4 * q + k], du[4 * q + k]);
+            }
+            const Extent pg = extent_of(p.dg, p.n * 6), pu = extent_of(p.du, p.n * 6);
+            uint4        sg[3], su[3];
+            glu_split8(dg, sg), glu_split8(du, su);
+#pragma unroll
+            for (int s = 0; s < 3; ++s) {
+                uint4 *const og = static_cast<uint4 *>(p.dg) + s * (p.n / 8) + i, *const ou = static_cast<uint4 *>(p.du) + s * (p.n / 8) + i;
+                if (pg.holds(og, 16)) *og = sg[s];
+                if (pu.holds(ou, 16)) *ou = su[s];
+            }
+            return;
+        }
+    }
     if (i < vecs) {
         Acc dh[kW], g[kW], u[kW];
         widen_vec<DT>(__ldg(static_cast<const uint4 *>(p.dh) + i), dh);
@@ -232,12 +258,18 @@ int check_sizes(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype)
     return BT_OK;
 }
 
-size_t padded(uint64_t rows, uint64_t d_ff, int es) { return (rows * d_ff * static_cast<uint64_t>(es) + 255) / 256 * 256; }
+// bytes of dg or of du
+size_t slope_bytes(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype)
+{
+    if (dtype == BT_F32 && glu_mma_takes(d_in, d_ff, dtype)) return glu_plane_bytes(rows * d_ff);
+    return (rows * d_ff * static_cast<uint64_t>(element_size(dtype)) + 255) / 256 * 256;
+}
 
 size_t workspace_of(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, bool backward)
 {
     if (rows == 0) return 0;
-    return backward ? 2 * padded(rows, d_ff, element_size(dtype)) + glu_mma_scratch(rows, d_in, d_ff, dtype) : 0;
+    if (backward) return 2 * slope_bytes(rows, d_in, d_ff, dtype) + glu_mma_scratch(rows, d_in, d_ff, dtype, true);
+    return glu_rows_takes(rows, d_in, dtype) ? 0 : glu_mma_scratch(rows, d_in, d_ff, dtype, false);
 }
 
 }  // namespace
@@ -272,8 +304,9 @@ int bt_glu_fwd(const void *x, uint64_t rows, uint64_t d_in, uint64_t d_ff, int d
     bt::GluCall c{};
     c.x = x, c.w_gate = w_gate, c.w_up = w_up, c.h = h, c.g = g_out, c.u = u_out;
     c.rows = rows, c.d_in = d_in, c.d_ff = d_ff, c.dtype = dtype, c.act = activation, c.dev_status = dev_status;
-    if (bt::glu_rows_takes(c)) return bt::launch_glu_rows(c, s) == cudaSuccess ? BT_OK : BT_ERR_CUDA;
-    if (bt::glu_mma_takes(c)) return bt::launch_glu_mma_fwd(c, s) == cudaSuccess ? BT_OK : BT_ERR_CUDA;
+    if (bt::glu_rows_takes(rows, d_in, dtype)) return bt::launch_glu_rows(c, s) == cudaSuccess ? BT_OK : BT_ERR_CUDA;
+    c.scratch = workspace;
+    if (bt::glu_mma_takes(d_in, d_ff, dtype)) return bt::launch_glu_mma_fwd(c, s) == cudaSuccess ? BT_OK : BT_ERR_CUDA;
     return bt::dispatch(dtype, [&](auto dt) { return bt::forward_of<decltype(dt)::value>(c, s); });
 }
 
@@ -302,15 +335,17 @@ int bt_glu_bwd(const void *grad_h, uint64_t rows, uint64_t d_in, uint64_t d_ff, 
     if (!workspace) return BT_ERR_NULL;
     if (workspace_bytes < bt::workspace_of(rows, d_in, d_ff, dtype, true)) return BT_ERR_WORKSPACE;
     unsigned char *w = static_cast<unsigned char *>(workspace);
-    bt::SlopeArgs  slope{grad_h, g, u, w, w + bt::padded(rows, d_ff, static_cast<int>(es)), rows * d_ff, dev_status};
+    const size_t   each = bt::slope_bytes(rows, d_in, d_ff, dtype);
+    const bool     mma  = bt::glu_mma_takes(d_in, d_ff, dtype);
+    bt::SlopeArgs  slope{grad_h, g, u, w, w + each, rows * d_ff, mma && dtype == BT_F32, dev_status};
     bt::GluCall    c{};
     c.x = x, c.w_gate = w_gate, c.w_up = w_up, c.dg = slope.dg, c.du = slope.du, c.dx = grad_x, c.dw_gate = grad_w_gate, c.dw_up = grad_w_up;
     c.rows = rows, c.d_in = d_in, c.d_ff = d_ff, c.dtype = dtype, c.act = activation, c.dev_status = dev_status;
-    c.scratch = w + 2 * bt::padded(rows, d_ff, static_cast<int>(es));
+    c.scratch = w + 2 * each;
     return bt::dispatch(dtype, [&](auto dt) {
         const cudaError_t e = bt::slopes_of<decltype(dt)::value>(slope, activation, s);
         if (e != cudaSuccess) return e;
-        return bt::glu_mma_takes(c) ? bt::launch_glu_mma_bwd(c, s) : bt::backward_of<decltype(dt)::value>(c, s);
+        return mma ? bt::launch_glu_mma_bwd(c, s) : bt::backward_of<decltype(dt)::value>(c, s);
     });
 }
 

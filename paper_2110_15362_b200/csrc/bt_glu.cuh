@@ -61,20 +61,49 @@ struct GluCall {
     void       *h, *g, *u;                         // forward: [rows, d_ff]; g and u may be NULL
     const void *dg, *du;                           // backward: [rows, d_ff], the gradients of g and u
     void       *dx, *dw_gate, *dw_up;              // backward: any may be NULL
-    void       *scratch;                           // backward: glu_mma_scratch bytes
+    void       *scratch;                           // glu_mma_scratch bytes
     uint64_t    rows, d_in, d_ff;
     int         dtype, act;
     int32_t    *dev_status;
 };
 
-// The products on the tensor cores (bt_glu_mma.cu): types and sizes that they take; forward; backward from c.dg and c.du.
-bool        glu_mma_takes(const GluCall &c);
-size_t      glu_mma_scratch(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype);    // bytes that a backward pass needs
+// Binary32 as three planes of bfloat16, which add up to it exactly: 8 bits of the significand in each, cut off.  (An infinity
+// and a NaN are their own first plane, and the others are zeros.)
+__device__ __forceinline__ void glu_split8(const float (&x)[8], uint4 (&planes)[3])
+{
+    uint32_t w[3][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        uint32_t h[3][2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            const float    v     = x[2 * k + e];
+            const uint32_t first = __float_as_uint(v) & 0xFFFF0000u;
+            const bool     fine  = (first & 0x7F800000u) != 0x7F800000u;
+            const float    r     = fine ? v - __uint_as_float(first) : 0.0f;
+            const uint32_t next  = __float_as_uint(r) & 0xFFFF0000u;
+            h[0][e] = fine ? first >> 16 : (__float_as_uint(v) >> 16 | ((__float_as_uint(v) & 0x007FFFFFu) ? 0x40u : 0u));   // (a NaN stays one)
+            h[1][e] = next >> 16;
+            h[2][e] = __float_as_uint(r - __uint_as_float(next)) >> 16;
+        }
+#pragma unroll
+        for (int s = 0; s < 3; ++s) w[s][k] = h[s][0] | h[s][1] << 16;
+    }
+#pragma unroll
+    for (int s = 0; s < 3; ++s) planes[s] = make_uint4(w[s][0], w[s][1], w[s][2], w[s][3]);
+}
+// bytes of the planes of n elements
+inline size_t glu_plane_bytes(uint64_t n) { return (n * 6 + 255) / 256 * 256; }
+
+// The products on the tensor cores (bt_glu_mma.cu): types and sizes that they take; the scratch that a pass needs; forward;
+// backward from c.dg and c.du (binary32: three planes each).
+bool        glu_mma_takes(uint64_t d_in, uint64_t d_ff, int dtype);
+size_t      glu_mma_scratch(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, bool backward);
 cudaError_t launch_glu_mma_fwd(const GluCall &c, cudaStream_t stream);
 cudaError_t launch_glu_mma_bwd(const GluCall &c, cudaStream_t stream);
 
 // The forward pass for few rows (bt_glu_rows.cu).
-bool        glu_rows_takes(const GluCall &c);
+bool        glu_rows_takes(uint64_t rows, uint64_t d_in, int dtype);
 cudaError_t launch_glu_rows(const GluCall &c, cudaStream_t stream);
 
 // calls go(std::integral_constant<int, DT>, std::integral_constant<int, ACT>) for a call's type and activation

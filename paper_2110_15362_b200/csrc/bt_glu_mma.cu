@@ -1,4 +1,4 @@
-// The gated feed-forward block's products of 16-bit types on the tensor cores (tcgen05, sums in TMEM in binary32).
+// The gated feed-forward block's products on the tensor cores (tcgen05, sums in TMEM in binary32).
 //
 // One kernel, three uses (kUse).  A pair of CTAs (cta_group::2) computes tiles of 256 x kN outputs: each CTA holds 128 rows of
 // A and half of B's kN rows, 64 of the summed axis per stage, and the pair's sums of its own 128 rows in its TMEM.
@@ -14,7 +14,15 @@
 // of TMEM.  Rows, columns and depths beyond a tensor are read as zeros and never written (TMA's bounds).  The summed axis and both output
 // axes may have any size; rows of every operand must begin on 16-byte boundaries (d_in and d_ff multiples of 8).
 //
-// Bound by the tensor cores.  Every wait is bounded: a role that gives up reports BT_ERR_TIMEOUT, the others follow, and the
+// Binary32 operands come as three planes of bfloat16 each, which add up to them exactly (8 bits of the significand per plane,
+// cut off, not rounded: split_kernel).  Of the nine products of planes the six above 2^-24 are taken.  The tensor cores cut
+// their sums off where an addition would round, by up to 2^-23 of the sum and always towards zero, so that long sums drift (4e-6
+// of a sum of 4096 products of random signs, 1.4e-5 of equal ones; measured); therefore the products of the first planes have a
+// sum of their own, the other five share a second one, which is 2^8 smaller, and both go to registers, added there with
+// rounding, every 256 summed elements (kChunk).  Errors stay at those of a sum in binary32.
+//
+// Bound by the tensor cores, and by the 64 bytes per cycle that a CTA reads from the L2 (a block of 64 summed elements of a
+// 256 x 256 tile takes 512 cycles of either).  Every wait is bounded: a role that gives up reports BT_ERR_TIMEOUT, the others follow, and the
 // CTAs leave together.
 #include <cuda.h>
 
@@ -31,7 +39,13 @@ constexpr int kDepth      = 64;                       // of the summed axis per 
 constexpr int kRows       = 128;                      // of A per CTA
 constexpr int kEpiWarps   = 8;
 constexpr int kThreads    = 32 * (2 + kEpiWarps);     // loader, issuer, epilogue
-constexpr int kStageWords = 32 * kDepth * 2;          // bytes of a warp's staged output: 32 rows of 64 elements
+constexpr int kStageWords = 32 * kDepth * 2;          // bytes of a warp's staged output: 32 rows of 128 bytes
+constexpr uint32_t kChunk = 4;                        // binary32: blocks of 64 summed elements from one addition in registers to the next
+
+template <int DT>
+constexpr uint32_t kPlanes = DT == BT_F32 ? 3 : 1;    // of an operand
+template <int DT>
+constexpr uint32_t kStaged = DT == BT_F32 ? 32 : 64;  // columns of a staged row of 128 bytes
 
 template <int kN>
 struct Shape {
@@ -95,10 +109,10 @@ __device__ __forceinline__ uint64_t now_ns()
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
     return t;
 }
-__device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap *map, int x, int y, uint32_t bar)
+__device__ __forceinline__ void tma_load(uint32_t to, const CUtensorMap *map, int x, int y, int plane, uint32_t bar)
 {
-    asm volatile("cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(to),
-                 "l"(map), "r"(x), "r"(y), "r"(bar)
+    asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(to),
+                 "l"(map), "r"(x), "r"(y), "r"(plane), "r"(bar)
                  : "memory");
 }
 __device__ __forceinline__ void tma_store(const CUtensorMap *map, int x, int y, uint32_t from)
@@ -155,7 +169,7 @@ constexpr uint32_t kStep = kAcross ? 16 * 128 : 32;
 
 template <int DT, bool kAcrossA, bool kAcrossB, int kN>
 constexpr uint32_t kInstruction = 1u << 4 |                                                    // sums in binary32
-                                  (DT == BT_BF16 ? 1u : 0u) << 7 | (DT == BT_BF16 ? 1u : 0u) << 10 |   // operands: bfloat16 or binary16
+                                  (DT == BT_F16 ? 0u : 1u) << 7 | (DT == BT_F16 ? 0u : 1u) << 10 |     // operands: binary16 or bfloat16
                                   (kAcrossA ? 1u : 0u) << 15 | (kAcrossB ? 1u : 0u) << 16 |    // which axis is contiguous
                                   static_cast<uint32_t>(kN / 8) << 17 | static_cast<uint32_t>(256 / 16) << 24;
 
@@ -228,7 +242,9 @@ template <int DT, int kUse, int kAct, int kN>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 glu_mma_kernel(const __grid_constant__ MmaArgs p)
 {
+    static_assert(DT != BT_F32 || kN == 128, "two sums per tile, twice");
     using S                     = Shape<kN>;
+    constexpr uint32_t kSums    = DT == BT_F32 ? 2 * kN : kN;            // TMEM columns of a tile
     constexpr bool     kAcrossA = kUse == kWeightGrad, kAcrossB = kUse != kForward;
     constexpr uint32_t kIdesc   = kInstruction<DT, kAcrossA, kAcrossB, kN>;
     constexpr int      kStages  = S::kStages;
@@ -256,7 +272,7 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
     }
     if (warp == 0 && lane < 7) prefetch_map(lane < 2 ? &p.a[lane] : lane < 4 ? &p.b[lane - 2] : &p.out[lane - 4]);
     if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_word)), "r"(2 * kN) : "memory");
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_word)), "r"(2 * kSums) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
     }
     tmem_fence_before();
@@ -284,8 +300,9 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
             for (uint32_t t = first; t < p.tiles && ok; t += step) {
                 const Tile     tile = tile_at(p, split ? t / p.splits : t);
                 const int      i0   = static_cast<int>(tile.i * 256 + rank * kRows);
-                const uint32_t end  = end_block(t);
-                for (uint32_t k = from_block(t); k < end; ++k) {
+                const uint32_t end  = end_block(t) * kPlanes<DT>;
+                for (uint32_t it = from_block(t) * kPlanes<DT>; it < end; ++it) {
+                    const uint32_t k = it / kPlanes<DT>, plane = it % kPlanes<DT>;
                     if (!(ok = wait(empty(ring.stage), ring.phase ^ 1))) break;
                     const uint32_t a = base + ring.stage * (S::kABytes + S::kBBytes), b = a + S::kABytes;
                     const uint32_t bar = in_first_cta(full(ring.stage));
@@ -295,18 +312,18 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
                     const uint32_t pair = kUse == kInputGrad ? (k >= p.blocks ? 1u : 0u) : 0u;
                     const int      k0   = static_cast<int>((k - pair * p.blocks) * kDepth);
                     if constexpr (kUse == kForward) {
-                        tma_load(a, &p.a[0], k0, i0, bar);
-                        tma_load(b, &p.b[rank], k0, static_cast<int>(tile.j * (kN / 2)), bar);
+                        tma_load(a, &p.a[0], k0, i0, plane, bar);
+                        tma_load(b, &p.b[rank], k0, static_cast<int>(tile.j * (kN / 2)), plane, bar);
                     } else {
                         const int j0 = static_cast<int>(tile.j * kN + rank * (kN / 2));
                         if constexpr (kUse == kInputGrad) {
-                            tma_load(a, &p.a[pair], k0, i0, bar);
+                            tma_load(a, &p.a[pair], k0, i0, plane, bar);
                         } else {
 #pragma unroll
-                            for (int v = 0; v < kRows / 64; ++v) tma_load(a + v * 64 * kDepth * 2, &p.a[tile.which], i0 + 64 * v, k0, bar);
+                            for (int v = 0; v < kRows / 64; ++v) tma_load(a + v * 64 * kDepth * 2, &p.a[tile.which], i0 + 64 * v, k0, plane, bar);
                         }
 #pragma unroll
-                        for (int v = 0; v < kN / 2 / 64; ++v) tma_load(b + v * 64 * kDepth * 2, &p.b[kUse == kInputGrad ? pair : 0], j0 + 64 * v, k0, bar);
+                        for (int v = 0; v < kN / 2 / 64; ++v) tma_load(b + v * 64 * kDepth * 2, &p.b[kUse == kInputGrad ? pair : 0], j0 + 64 * v, k0, plane, bar);
                     }
                     ring.next();
                 }
@@ -325,35 +342,141 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
             Ring<2>       half;
             bool          ok = true;
             for (uint32_t t = first; t < p.tiles && ok; t += step) {
-                if (!(ok = wait(taken(half.stage), half.phase ^ 1))) break;
-                tmem_fence_after();
-                const uint32_t d = tmem + half.stage * kN;
-                const uint32_t begin = from_block(t), end = end_block(t);
-                for (uint32_t k = begin; k < end; ++k) {
-                    if (!(ok = wait(full(ring.stage), ring.phase))) break;
+                const uint32_t end = end_block(t);
+                // binary32: a chunk of blocks at a time; else all of them
+                for (uint32_t begin = from_block(t); begin < end && ok;) {
+                    const uint32_t stop = DT == BT_F32 && begin + kChunk < end ? begin + kChunk : end;
+                    if (!(ok = wait(taken(half.stage), half.phase ^ 1))) break;
                     tmem_fence_after();
-                    const uint32_t a = base + ring.stage * (S::kABytes + S::kBBytes), b = a + S::kABytes;
-                    const uint64_t da = operand<kAcrossA>(a), db = operand<kAcrossB>(b);
+                    const uint32_t d = tmem + half.stage * kSums;
+                    for (uint32_t k = begin; k < stop && ok; ++k) {
+                        if constexpr (DT == BT_F32) {
+                            // a block's planes come one after the other; each is multiplied with those before it
+                            uint64_t       a[3], b[3];
+                            uint32_t       slot[3];
+                            const auto product = [&](const uint32_t to, const uint64_t da, const uint64_t db, const bool add) {
 #pragma unroll
-                    for (int q = 0; q < kDepth / 16; ++q)
-                        mma_pair(d, da + q * (kStep<kAcrossA> >> 4), db + q * (kStep<kAcrossB> >> 4), kIdesc, k != begin || q != 0);
-                    commit_pair(empty(ring.stage));
-                    ring.next();
+                                for (int q = 0; q < kDepth / 16; ++q)
+                                    mma_pair(to, da + q * (kStep<kAcrossA> >> 4), db + q * (kStep<kAcrossB> >> 4), kIdesc, add || q != 0);
+                            };
+#pragma unroll
+                            for (int s = 0; s < 3; ++s) {
+                                if (ok && !(ok = wait(full(ring.stage), ring.phase))) break;
+                                tmem_fence_after();
+                                const uint32_t at = base + ring.stage * (S::kABytes + S::kBBytes);
+                                slot[s] = ring.stage, a[s] = operand<kAcrossA>(at), b[s] = operand<kAcrossB>(at + S::kABytes);
+                                if (s == 0) product(d, a[0], b[0], k != begin);
+                                if (s == 1) product(d + kN, a[0], b[1], k != begin), product(d + kN, a[1], b[0], true), product(d + kN, a[1], b[1], true);
+                                if (s == 2) product(d + kN, a[0], b[2], true), product(d + kN, a[2], b[0], true);
+                                ring.next();
+                            }
+                            if (!ok) break;
+#pragma unroll
+                            for (int s = 0; s < 3; ++s) commit_pair(empty(slot[s]));
+                        } else {
+                            if (!(ok = wait(full(ring.stage), ring.phase))) break;
+                            tmem_fence_after();
+                            const uint32_t a = base + ring.stage * (S::kABytes + S::kBBytes), b = a + S::kABytes;
+                            const uint64_t da = operand<kAcrossA>(a), db = operand<kAcrossB>(b);
+#pragma unroll
+                            for (int q = 0; q < kDepth / 16; ++q)
+                                mma_pair(d, da + q * (kStep<kAcrossA> >> 4), db + q * (kStep<kAcrossB> >> 4), kIdesc, k != begin || q != 0);
+                            commit_pair(empty(ring.stage));
+                            ring.next();
+                        }
+                    }
+                    if (!ok) break;
+                    commit_pair(ready(half.stage));
+                    half.next();
+                    begin = stop;
                 }
-                if (!ok) break;
-                commit_pair(ready(half.stage));
-                half.next();
             }
         }
         __syncwarp();
     } else {
         // ---- epilogue: a quarter of TMEM's lanes (the warp's number modulo 4) and every second chunk of 64 output columns
         const uint32_t quarter = warp % 4, turn = (warp - 2) / 4;
-        const uint32_t stage_at = base + S::kRing + (warp - 2) * kStageWords;
-        unsigned char *const stage = generic + S::kRing + (warp - 2) * kStageWords;
+        // a row of 128 bytes per lane to the staged tile, in the pieces' swizzled places, and the tile out
+        const auto stage_out = [&](const uint32_t (&packed)[32], const CUtensorMap *map, const uint32_t j0, const uint32_t i0) {
+            if (lane == 0) bulk_wait_read<0>();                         // the tile of before has been read
+            __syncwarp();
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                *reinterpret_cast<uint4 *>(generic + S::kRing + (warp - 2) * kStageWords + lane * 128 + ((c ^ (lane & 7)) * 16)) =
+                    make_uint4(packed[4 * c], packed[4 * c + 1], packed[4 * c + 2], packed[4 * c + 3]);
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) {
+                tma_store(map, static_cast<int>(j0), static_cast<int>(i0), base + S::kRing + (warp - 2) * kStageWords);
+                bulk_commit();
+            }
+        };
         constexpr uint32_t kChunks = kUse == kForward ? kN / 2 / 64 : kN / 64;
         constexpr uint32_t kItems  = kUse == kForward ? kChunks * 3 : kChunks;
         Ring<2> half;
+        if constexpr (DT == BT_F32) {
+            // 64 columns of the tile per warp, in registers from chunk to chunk: forward 32 of g and 32 of u, else the `turn`th 64
+            bool ok = true;
+            for (uint32_t t = first; t < p.tiles && ok; t += step) {
+                const Tile     tile = tile_at(p, split ? t / p.splits : t);
+                const uint32_t i0   = tile.i * 256 + rank * kRows + quarter * 32, end = end_block(t);
+                uint32_t       sum[2][32];
+#pragma unroll
+                for (int c = 0; c < 32; ++c) sum[0][c] = sum[1][c] = 0;
+                for (uint32_t begin = from_block(t); begin < end; begin += kChunk) {
+                    if (!(ok = wait(ready(half.stage), half.phase))) break;
+                    tmem_fence_after();
+                    const uint32_t from = tmem + half.stage * kSums + (quarter * 32 << 16);
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        const uint32_t at = from + (kUse == kForward ? part * (kN / 2) + turn * 32 : turn * 64 + part * 32);
+                        uint32_t       v[32], w[32];
+                        tmem_load(at, v);
+                        tmem_load(at + kN, w);
+                        tmem_load_wait();
+#pragma unroll
+                        for (int c = 0; c < 32; ++c)
+                            sum[part][c] = __float_as_uint(__uint_as_float(sum[part][c]) + (__uint_as_float(v[c]) + __uint_as_float(w[c])));
+                    }
+                    tmem_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(in_first_cta(taken(half.stage)));
+                    half.next();
+                }
+                if (!ok) break;
+                if (i0 >= p.size_i) continue;
+                if constexpr (kUse == kForward) {
+                    const uint32_t j0 = tile.j * (kN / 2) + turn * 32;
+                    if (j0 >= p.size_j) continue;
+                    uint32_t act[32];
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) {
+                        const float g = act_of<kAct>(__uint_as_float(sum[0][c]));
+                        act[c]        = __float_as_uint(g * __uint_as_float(sum[1][c]));
+                        if (kAct == BT_ACT_RELU) sum[0][c] = __float_as_uint(g);
+                    }
+                    if (p.outputs & 1) stage_out(act, &p.out[0], j0, i0);
+                    if (p.outputs & 2) stage_out(sum[0], &p.out[1], j0, i0);
+                    if (p.outputs & 4) stage_out(sum[1], &p.out[2], j0, i0);
+                } else {
+                    if (split) {
+                        float4 *const out = p.partial + ((static_cast<uint64_t>(t) * 2 + rank) * (kN / 64) + turn) * (16 * kRows) + quarter * 32 + lane;
+                        const Extent  all = extent_of(p.partial, static_cast<uint64_t>(p.tiles) * 2 * (kN / 64) * (16 * kRows) * sizeof(float4));
+#pragma unroll
+                        for (int c = 0; c < 16; ++c)
+                            if (all.holds(out + c * kRows, sizeof(float4)))
+                                out[c * kRows] = make_float4(__uint_as_float(sum[c / 8][4 * c % 32]), __uint_as_float(sum[c / 8][4 * c % 32 + 1]),
+                                                             __uint_as_float(sum[c / 8][4 * c % 32 + 2]), __uint_as_float(sum[c / 8][4 * c % 32 + 3]));
+                        continue;
+                    }
+#pragma unroll
+                    for (int part = 0; part < 2; ++part) {
+                        const uint32_t j0 = tile.j * kN + turn * 64 + part * 32;
+                        if (j0 < p.size_j) stage_out(sum[part], &p.out[tile.which], j0, i0);
+                    }
+                }
+            }
+        } else
         for (uint32_t t = first; t < p.tiles; t += step) {
             const Tile tile = tile_at(p, split ? t / p.splits : t);
             const uint32_t i0 = tile.i * 256 + rank * kRows + quarter * 32;
@@ -406,19 +529,7 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
                         for (int c = 0; c < 16; ++c) packed[part * 16 + c] = pack2<DT>(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
                     }
                 }
-                // the staged tile of before has been read; a lane writes its row's eight 16-byte pieces where the swizzle has them
-                if (lane == 0) bulk_wait_read<0>();
-                __syncwarp();
-#pragma unroll
-                for (int c = 0; c < 8; ++c)
-                    *reinterpret_cast<uint4 *>(stage + lane * 128 + ((c ^ (lane & 7)) * 16)) =
-                        make_uint4(packed[4 * c], packed[4 * c + 1], packed[4 * c + 2], packed[4 * c + 3]);
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) {
-                    tma_store(&p.out[kUse == kForward ? what : tile.which], static_cast<int>(j0), static_cast<int>(i0), stage_at);
-                    bulk_commit();
-                }
+                stage_out(packed, &p.out[kUse == kForward ? what : tile.which], j0, i0);
             }
             tmem_fence_before();
             __syncwarp();
@@ -438,7 +549,7 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
     tmem_fence_before();
     cluster_sync();
     tmem_fence_after();
-    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kN) : "memory");
+    if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * kSums) : "memory");
 }
 
 // The sums of a tile's units added up, rounded and written: a CTA takes eight columns of a CTA's 128 rows.
@@ -462,10 +573,63 @@ join_kernel(const float4 *__restrict__ partial, const uint32_t splits, void *to,
     }
     // (size_j is a multiple of 8)
     uint4 *const out = reinterpret_cast<uint4 *>(static_cast<typename Num<DT>::Elem *>(to) + i * size_j + j);
-    if (extent_of(to, size_i * size_j * 2).holds(out, 16)) *out = narrow_vec<DT>(s);
+    constexpr int kL = kLanes<DT>;
+#pragma unroll
+    for (int q = 0; q < 8 / kL; ++q) {
+        float v[kL];
+#pragma unroll
+        for (int c = 0; c < kL; ++c) v[c] = s[q * kL + c];
+        if (extent_of(to, size_i * size_j * sizeof(typename Num<DT>::Elem)).holds(out + q, 16)) out[q] = narrow_vec<DT>(v);
+    }
+}
+
+// Up to three binary32 tensors, n elements each (a multiple of 8), into planes of bfloat16, one behind the other.
+struct SplitTensors {
+    const uint4   *from[3];
+    __nv_bfloat16 *to[3];
+    uint64_t       n[3];
+};
+__global__ void __launch_bounds__(256)
+split_kernel(const SplitTensors p)
+{
+    in_stream_order();
+    for (int k = 0; k < 3; ++k) {
+        const Extent all = extent_of(p.to[k], 6 * p.n[k]);
+        for (uint64_t v = static_cast<uint64_t>(blockIdx.x) * 256 + threadIdx.x; v < p.n[k] / 8; v += static_cast<uint64_t>(gridDim.x) * 256) {
+            const uint4 lo = __ldg(p.from[k] + 2 * v), hi = __ldg(p.from[k] + 2 * v + 1);
+            const float x[8] = {__uint_as_float(lo.x), __uint_as_float(lo.y), __uint_as_float(lo.z), __uint_as_float(lo.w),
+                                __uint_as_float(hi.x), __uint_as_float(hi.y), __uint_as_float(hi.z), __uint_as_float(hi.w)};
+            uint4 planes[3];
+            glu_split8(x, planes);
+#pragma unroll
+            for (int s = 0; s < 3; ++s) {
+                uint4 *const out = reinterpret_cast<uint4 *>(p.to[k] + s * p.n[k]) + v;
+                if (all.holds(out, 16)) *out = planes[s];
+            }
+        }
+    }
 }
 
 // ---------------------------------------------------------------------------------------------- host side
+// c.x and the weights (where they are wanted) replaced by their planes in c.scratch, which then points behind them
+cudaError_t split_operands(GluCall &c, bool x, bool weights, int sms, cudaStream_t stream)
+{
+    unsigned char *at = static_cast<unsigned char *>(c.scratch);
+    const uint64_t n[3] = {c.rows * c.d_in, c.d_ff * c.d_in, c.d_ff * c.d_in};
+    const void    *from[3] = {c.x, c.w_gate, c.w_up};
+    SplitTensors   p{};
+    uint64_t       most = 0;
+    for (int k = 0; k < 3; ++k) {
+        p.from[k] = static_cast<const uint4 *>(from[k]), p.to[k] = reinterpret_cast<__nv_bfloat16 *>(at);
+        p.n[k]    = (k == 0 ? x : weights) ? n[k] : 0;
+        most      = p.n[k] > most ? p.n[k] : most;
+        at += glu_plane_bytes(n[k]);
+    }
+    c.x = p.to[0], c.w_gate = p.to[1], c.w_up = p.to[2], c.scratch = at;
+    const uint64_t want = round_up_div(most / 8, 256), limit = static_cast<uint64_t>(sms) * 8;
+    return launch(split_kernel, static_cast<unsigned>(want < limit ? want : limit), 256, 0, stream, p);
+}
+
 using Encode = CUresult (*)(CUtensorMap *, CUtensorMapDataType, cuuint32_t, void *, const cuuint64_t *, const cuuint64_t *, const cuuint32_t *,
                             const cuuint32_t *, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 // the driver's encoder of tensor maps (host arithmetic), looked up once
@@ -482,13 +646,24 @@ Encode encoder()
     return fn;
 }
 
-// a row-major matrix of 16-bit elements in boxes of 64 columns (128 bytes, swizzled) and box_rows rows
+// an operand: a row-major matrix of 16-bit elements (binary32: three planes of them), in boxes of 64 columns (128 bytes,
+// swizzled) and box_rows rows
 bool map_of(CUtensorMap &m, int dtype, const void *at, uint64_t rows, uint64_t columns, uint32_t box_rows)
 {
-    const cuuint64_t size[2] = {columns, rows}, stride[1] = {columns * 2};
-    const cuuint32_t box[2] = {64, box_rows}, each[2] = {1, 1};
-    return encoder()(&m, dtype == BT_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, const_cast<void *>(at), size, stride,
+    const cuuint64_t size[3] = {columns, rows, dtype == BT_F32 ? 3u : 1u}, stride[2] = {columns * 2, rows * columns * 2};
+    const cuuint32_t box[3] = {64, box_rows, 1}, each[3] = {1, 1, 1};
+    return encoder()(&m, dtype == BT_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(at), size, stride,
                      box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+// an output, in boxes of 32 rows of 128 bytes
+bool out_map(CUtensorMap &m, int dtype, void *at, uint64_t rows, uint64_t columns)
+{
+    const uint64_t   es = dtype == BT_F32 ? 4 : 2;
+    const cuuint64_t size[2] = {columns, rows}, stride[1] = {columns * es};
+    const cuuint32_t box[2] = {static_cast<cuuint32_t>(128 / es), 32}, each[2] = {1, 1};
+    return encoder()(&m, dtype == BT_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : dtype == BT_F16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+                     2, at, size, stride, box, each, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                      CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -536,9 +711,9 @@ cudaError_t forward_of(const GluCall &c, int sms, cudaStream_t stream)
 {
     MmaArgs p{};
     bool    ok = map_of(p.a[0], DT, c.x, c.rows, c.d_in, kRows) && map_of(p.b[0], DT, c.w_gate, c.d_ff, c.d_in, kN / 2) &&
-              map_of(p.b[1], DT, c.w_up, c.d_ff, c.d_in, kN / 2) && map_of(p.out[0], DT, c.h, c.rows, c.d_ff, 32);
-    if (c.g) ok = ok && map_of(p.out[1], DT, c.g, c.rows, c.d_ff, 32);
-    if (c.u) ok = ok && map_of(p.out[2], DT, c.u, c.rows, c.d_ff, 32);
+              map_of(p.b[1], DT, c.w_up, c.d_ff, c.d_in, kN / 2) && out_map(p.out[0], DT, c.h, c.rows, c.d_ff);
+    if (c.g) ok = ok && out_map(p.out[1], DT, c.g, c.rows, c.d_ff);
+    if (c.u) ok = ok && out_map(p.out[2], DT, c.u, c.rows, c.d_ff);
     if (!ok || !set_tiles(p, c.rows, c.d_ff, kN / 2, 1)) return cudaErrorInvalidValue;
     p.outputs    = 1u | (c.g ? 2u : 0u) | (c.u ? 4u : 0u);
     p.blocks     = static_cast<uint32_t>(round_up_div(c.d_in, kDepth));
@@ -552,17 +727,19 @@ struct SplitPlan {
     uint32_t columns, splits, split_blocks;
     uint64_t tiles;
 };
-SplitPlan input_grad_plan(uint64_t rows, uint64_t d_in, uint64_t d_ff, int sms)
+SplitPlan input_grad_plan(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, int sms)
 {
     const uint64_t pairs = static_cast<uint64_t>(sms) / 2, blocks = 2 * round_up_div(d_ff, kDepth);
+    const uint64_t each_block = dtype == BT_F32 ? 6 : 1;                 // products
     SplitPlan      best{};
     double         least = 0;
     for (const uint32_t columns : {256u, 128u}) {
+        if (dtype == BT_F32 && columns == 256) continue;
         const uint64_t tiles = round_up_div(rows, 256) * round_up_div(d_in, columns);
         for (uint32_t splits = 1; splits <= 32 && (splits == 1 || blocks / splits >= 4); ++splits) {
             const uint64_t each = round_up_div(blocks, splits);
             if (round_up_div(blocks, each) != splits) continue;         // (a unit would be empty)
-            double cost = tiles_ns(tiles * splits, each, columns, pairs);
+            double cost = tiles_ns(tiles * splits, each * each_block, columns, pairs);
             if (splits > 1) cost += 3000 + static_cast<double>(tiles * splits) * 87 * (columns / 256.0);
             if (least == 0 || cost < least) least = cost, best = SplitPlan{columns, splits, static_cast<uint32_t>(each), tiles};
         }
@@ -577,7 +754,7 @@ cudaError_t input_grad_of(const GluCall &c, const SplitPlan &s, int sms, cudaStr
     MmaArgs    p{};
     const bool ok = map_of(p.a[0], DT, c.dg, c.rows, c.d_ff, kRows) && map_of(p.a[1], DT, c.du, c.rows, c.d_ff, kRows) &&
                     map_of(p.b[0], DT, c.w_gate, c.d_ff, c.d_in, kDepth) && map_of(p.b[1], DT, c.w_up, c.d_ff, c.d_in, kDepth) &&
-                    map_of(p.out[0], DT, c.dx, c.rows, c.d_in, 32);
+                    out_map(p.out[0], DT, c.dx, c.rows, c.d_in);
     if (!ok || !set_tiles(p, c.rows, c.d_in, kN, 1)) return cudaErrorInvalidValue;
     p.blocks     = static_cast<uint32_t>(round_up_div(c.d_ff, kDepth));
     p.dev_status = c.dev_status;
@@ -594,8 +771,8 @@ cudaError_t weight_grad_of(const GluCall &c, int sms, cudaStream_t stream)
 {
     MmaArgs    p{};
     const bool ok = map_of(p.a[0], DT, c.dg, c.rows, c.d_ff, kDepth) && map_of(p.a[1], DT, c.du, c.rows, c.d_ff, kDepth) &&
-                    map_of(p.b[0], DT, c.x, c.rows, c.d_in, kDepth) && map_of(p.out[0], DT, c.dw_gate, c.d_ff, c.d_in, 32) &&
-                    map_of(p.out[1], DT, c.dw_up, c.d_ff, c.d_in, 32);
+                    map_of(p.b[0], DT, c.x, c.rows, c.d_in, kDepth) && out_map(p.out[0], DT, c.dw_gate, c.d_ff, c.d_in) &&
+                    out_map(p.out[1], DT, c.dw_up, c.d_ff, c.d_in);
     if (!ok || !set_tiles(p, c.d_ff, c.d_in, kN, 2)) return cudaErrorInvalidValue;
     p.blocks     = static_cast<uint32_t>(round_up_div(c.rows, kDepth));
     p.dev_status = c.dev_status;
@@ -605,48 +782,59 @@ cudaError_t weight_grad_of(const GluCall &c, int sms, cudaStream_t stream)
 template <int DT>
 cudaError_t forward(const GluCall &c, int sms, cudaStream_t stream)
 {
-    return wide_tiles(c.rows, c.d_ff, 1, 128, round_up_div(c.d_in, kDepth), sms) ? forward_of<DT, 256>(c, sms, stream)
+    if constexpr (DT == BT_F32) return forward_of<DT, 128>(c, sms, stream);
+    else return wide_tiles(c.rows, c.d_ff, 1, 128, round_up_div(c.d_in, kDepth), sms) ? forward_of<DT, 256>(c, sms, stream)
                                                                                                : forward_of<DT, 128>(c, sms, stream);
 }
 template <int DT>
 cudaError_t backward(const GluCall &c, int sms, cudaStream_t stream)
 {
     if (c.dx) {
-        const SplitPlan   s = input_grad_plan(c.rows, c.d_in, c.d_ff, sms);
-        const cudaError_t e = s.columns == 256 ? input_grad_of<DT, 256>(c, s, sms, stream) : input_grad_of<DT, 128>(c, s, sms, stream);
+        const SplitPlan s = input_grad_plan(c.rows, c.d_in, c.d_ff, DT, sms);
+        cudaError_t     e;
+        if constexpr (DT == BT_F32) e = input_grad_of<DT, 128>(c, s, sms, stream);
+        else e = s.columns == 256 ? input_grad_of<DT, 256>(c, s, sms, stream) : input_grad_of<DT, 128>(c, s, sms, stream);
         if (e != cudaSuccess) return e;
     }
     if (!c.dw_gate) return cudaSuccess;
-    return wide_tiles(c.d_ff, c.d_in, 2, 256, round_up_div(c.rows, kDepth), sms) ? weight_grad_of<DT, 256>(c, sms, stream)
+    if constexpr (DT == BT_F32) return weight_grad_of<DT, 128>(c, sms, stream);
+    else return wide_tiles(c.d_ff, c.d_in, 2, 256, round_up_div(c.rows, kDepth), sms) ? weight_grad_of<DT, 256>(c, sms, stream)
                                                                                                : weight_grad_of<DT, 128>(c, sms, stream);
 }
 
 }  // namespace
 
-bool glu_mma_takes(const GluCall &c)
+bool glu_mma_takes(uint64_t d_in, uint64_t d_ff, int dtype)
 {
-    return (c.dtype == BT_F16 || c.dtype == BT_BF16) && c.d_in % 8 == 0 && c.d_ff % 8 == 0 && encoder() != nullptr;
+    return dtype != BT_F64 && d_in % 8 == 0 && d_ff % 8 == 0 && encoder() != nullptr;
 }
 
-size_t glu_mma_scratch(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype)
+size_t glu_mma_scratch(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, bool backward)
 {
-    if ((dtype != BT_F16 && dtype != BT_BF16) || d_in % 8 != 0 || d_ff % 8 != 0) return 0;
-    const int sms = sm_count();
-    return partial_bytes(input_grad_plan(rows, d_in, d_ff, sms ? sms : 148));
+    if (!glu_mma_takes(d_in, d_ff, dtype)) return 0;
+    const int    sms  = sm_count();
+    const size_t sums = backward ? partial_bytes(input_grad_plan(rows, d_in, d_ff, dtype, sms ? sms : 148)) : 0;
+    return dtype == BT_F32 ? glu_plane_bytes(rows * d_in) + 2 * glu_plane_bytes(d_ff * d_in) + sums : sums;
 }
 
-cudaError_t launch_glu_mma_fwd(const GluCall &c, cudaStream_t stream)
-{
-    const int sms = sm_count();
-    if (sms < 2) return cudaErrorInvalidDevice;
-    return c.dtype == BT_BF16 ? forward<BT_BF16>(c, sms, stream) : forward<BT_F16>(c, sms, stream);
-}
-
-cudaError_t launch_glu_mma_bwd(const GluCall &c, cudaStream_t stream)
+cudaError_t launch_glu_mma_fwd(const GluCall &call, cudaStream_t stream)
 {
     const int sms = sm_count();
     if (sms < 2) return cudaErrorInvalidDevice;
-    return c.dtype == BT_BF16 ? backward<BT_BF16>(c, sms, stream) : backward<BT_F16>(c, sms, stream);
+    if (call.dtype != BT_F32) return call.dtype == BT_BF16 ? forward<BT_BF16>(call, sms, stream) : forward<BT_F16>(call, sms, stream);
+    GluCall           c = call;
+    const cudaError_t e = split_operands(c, true, true, sms, stream);
+    return e != cudaSuccess ? e : forward<BT_F32>(c, sms, stream);
+}
+
+cudaError_t launch_glu_mma_bwd(const GluCall &call, cudaStream_t stream)
+{
+    const int sms = sm_count();
+    if (sms < 2) return cudaErrorInvalidDevice;
+    if (call.dtype != BT_F32) return call.dtype == BT_BF16 ? backward<BT_BF16>(call, sms, stream) : backward<BT_F16>(call, sms, stream);
+    GluCall           c = call;
+    const cudaError_t e = split_operands(c, c.dw_gate != nullptr, c.dx != nullptr, sms, stream);
+    return e != cudaSuccess ? e : backward<BT_F32>(c, sms, stream);
 }
 
 }  // namespace bt

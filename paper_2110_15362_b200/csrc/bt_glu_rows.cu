@@ -189,9 +189,9 @@ cudaError_t start_f32(const RowsArgs &p, int act, cudaStream_t stream)
 
 }  // namespace
 
-bool glu_rows_takes(const GluCall &c)
+bool glu_rows_takes(uint64_t rows, uint64_t d_in, int dtype)
 {
-    return c.dtype == BT_F32 ? c.rows <= 8 && c.d_in % 4 == 0 : (c.dtype == BT_F16 || c.dtype == BT_BF16) && c.rows <= 32 && c.d_in % 8 == 0;
+    return dtype == BT_F32 ? rows <= 8 && d_in % 4 == 0 : (dtype == BT_F16 || dtype == BT_BF16) && rows <= 32 && d_in % 8 == 0;
 }
 
 cudaError_t launch_glu_rows(const GluCall &c, cudaStream_t stream)

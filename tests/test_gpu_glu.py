@@ -157,6 +157,27 @@ def test_backward_of_each_activation_and_of_some_outputs(act, kind):
     assert torch.equal(only_x[0], whole[0]) and all(torch.equal(a, b) for a, b in zip(only_w[1:], whole[1:]))
 
 
+@pytest.mark.parametrize("sign", [False, True])
+@pytest.mark.parametrize("size", [(64, 512, 128), (300, 4096, 264), (96, 11264, 72), (2056, 264, 520)])
+def test_binary32_keeps_its_digits(size, sign):
+    """Sums of equal signs and of random ones, over every axis: the error, in norm, of a binary32 sum of 256-element pieces.
+    A piece drifts by 16 additions of at most 2^-23 of it and half that on average; 16 pieces and the planes' remainder (2^-24
+    each) add less than as much again."""
+    x, wg, wu = make(*size, "f32", seed=41)
+    dh, g, u, *_ = make_backward(*size, "f32", "relu", seed=42)
+    if sign:
+        x, wg, wu, dh, g, u = (t.abs() for t in (x, wg, wu, dh, g, u))
+    rel = lambda a, b: ((a.double() - b).norm() / b.norm()).item()  # noqa: E731
+    bound = 2 * 16 * 2.0 ** -24
+    h, gg, uu = forward(x, wg, wu, "relu")
+    gd, ud = torch.relu(x.double() @ wg.double().T), x.double() @ wu.double().T
+    assert rel(uu, ud) < bound and rel(gg, gd) < bound and rel(h, gd * ud) < 2 * bound
+    dx, dwg, dwu = backward(dh, g, u, x, wg, wu, "relu")
+    dg, du = torch.where(g > 0, dh.double() * u.double(), 0.0), dh.double() * g.double()
+    assert rel(dx, dg @ wg.double() + du @ wu.double()) < bound
+    assert rel(dwg, dg.T @ x.double()) < bound and rel(dwu, du.T @ x.double()) < bound
+
+
 @pytest.mark.parametrize("act", ACTS)
 def test_backward_against_differences(act):
     """The gradients of L = sum(h * c), as the calls give them in binary64, against central differences of L."""
