@@ -8,7 +8,6 @@ functions pass their data pointers, the element count and the current stream.
 """
 from __future__ import annotations
 
-import array
 import ctypes
 import os
 from typing import Optional
@@ -40,10 +39,10 @@ EXPORTS = ("bt_compressed_bytes", "bt_workspace_bytes", "bt_compress", "bt_decom
            "bt_block_norm_fwd", "bt_block_norm_bwd", "bt_grad_workspace_bytes", "bt_grad_norm_batch", "bt_grad_scale_batch",
            "bt_grad_clip_batch")
 
-# the calls with two floats, or with more words than any other
-WIDE_CALLS = ("bt_block_norm_fwd", "bt_block_norm_bwd")
+# what is called through _autograd, which checks the tensors as well
+CHECKED_CALLS = ("bt_glu_fwd", "bt_glu_bwd", "bt_block_norm_fwd", "bt_block_norm_bwd")
 # what is called through _pycall: everything that takes a stream and no host buffers
-CALLS = tuple(n for n in EXPORTS if not n.endswith("_bytes") and not n.endswith("_host") and n != "bt_set_max_ctas" and n not in WIDE_CALLS)
+CALLS = tuple(n for n in EXPORTS if not n.endswith("_bytes") and not n.endswith("_host") and n != "bt_set_max_ctas" and n not in CHECKED_CALLS)
 
 BT_ACT_RELU, BT_ACT_SILU, BT_ACT_GELU, BT_ACT_GELU_TANH = range(4)
 ACT_CODE = {"relu": BT_ACT_RELU, "silu": BT_ACT_SILU, "gelu": BT_ACT_GELU, "gelu_tanh": BT_ACT_GELU_TANH}
@@ -86,9 +85,9 @@ class _Calls:
     code that makes the calls itself."""
 
     def __init__(self, L: ctypes.CDLL, native_call, pointer: str):
-        self.address = {name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in CALLS + WIDE_CALLS}
-        for name, at in self.address.items():
-            fn = getattr(L, name)
+        self.address = {name: ctypes.cast(getattr(L, name), ctypes.c_void_p).value for name in CALLS + CHECKED_CALLS}
+        for name in CALLS:
+            at, fn = self.address[name], getattr(L, name)
             kinds = "".join({ctypes.c_void_p: pointer, ctypes.c_float: "f", ctypes.POINTER(BatchItem): "b"}.get(t, "n")
                             for t in fn.argtypes[:-1]) + "s"
             setattr(self, name, native_call(at, kinds, _through_ctypes(fn, kinds), BatchItem))
@@ -613,23 +612,23 @@ def bt_relu_bwd_from_bitmap(bitmap: torch.Tensor, grad_out: torch.Tensor, grad_i
 
 
 # ---- operators of a transformer block's training step
-def _of_one_kind(call: str, *tensors: Optional[torch.Tensor]) -> int:
-    """The element type's code of a call's tensors, which must be contiguous, of one type and on the current device."""
-    first = tensors[0]
-    dtype, device = first.dtype, first.device
-    for t in tensors:
-        if t is not None and (t.dtype != dtype or t.device != device or not t.is_contiguous()):
-            raise ValueError(f"{call}: the tensors must be contiguous, of one element type and on one device")
-    if dtype not in DTYPE_CODE:
-        raise ValueError(f"{call}: {dtype} is not an element type of the library")
-    if device.type == "cuda" and device.index != torch._C._cuda_getDevice():
-        raise ValueError(f"{call}: the tensors are on {device}, which is not the current device")
-    return DTYPE_CODE[dtype]
+_checked = None
 
 
-def _of_shape(call: str, name: str, t: Optional[torch.Tensor], shape) -> None:
-    if t is not None and t.shape != shape:
-        raise ValueError(f"{call}: {name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+def _native():
+    """The extension module that checks the tensors of the calls below and makes them."""
+    global _checked
+    if _checked is None:
+        try:
+            from . import _autograd
+        except ImportError as e:
+            raise ImportError(f"{_build.AUTOGRAD_PATH} is missing or does not load: build it with `python -m paper_2110_15362_b200.build`") from e
+        _checked = _autograd
+    return _checked
+
+
+def _stream_or_none(stream):
+    return None if stream is None else _stream(stream)
 
 
 def _act(call: str, activation) -> int:
@@ -652,15 +651,8 @@ def bt_glu_fwd(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, h: tor
                activation: str = "silu", stream=None, check: bool = True) -> int:
     """Gated feed-forward block: h = act(x w_gate^T) * (x w_up^T); x (..., d_in), weights (d_ff, d_in), h (..., d_ff).  g_out
     and u_out (h's shape, or None) receive what bt_glu_bwd reads."""
-    code = _of_one_kind("bt_glu_fwd", x, w_gate, w_up, h, g_out, u_out)
-    d_ff, d_in = w_gate.shape
-    wide = (*x.shape[:-1], d_ff)
-    _of_shape("bt_glu_fwd", "x", x, (*x.shape[:-1], d_in))
-    _of_shape("bt_glu_fwd", "w_up", w_up, w_gate.shape)
-    for name, t in (("h", h), ("g_out", g_out), ("u_out", u_out)):
-        _of_shape("bt_glu_fwd", name, t, wide)
-    st = _tensor_calls().bt_glu_fwd(x, h.numel() // max(d_ff, 1), d_in, d_ff, code, _act("bt_glu_fwd", activation), w_gate, w_up, h, g_out, u_out,
-                                    workspace, _nbytes(workspace), dev_status, _stream(stream))
+    st = _native().glu_fwd(_calls().address["bt_glu_fwd"], x, w_gate, w_up, h, g_out, u_out, workspace, dev_status,
+                           _act("bt_glu_fwd", activation), _stream_or_none(stream))
     return _check("bt_glu_fwd", st, check)
 
 
@@ -669,29 +661,9 @@ def bt_glu_bwd(grad_h: torch.Tensor, g: torch.Tensor, u: torch.Tensor, x: torch.
                workspace: torch.Tensor, dev_status: Optional[torch.Tensor] = None, *, activation: str = "silu", stream=None,
                check: bool = True) -> int:
     """The gradients of bt_glu_fwd from its stored g and u; grad_x or both weights' gradients may be None."""
-    code = _of_one_kind("bt_glu_bwd", grad_h, g, u, x, w_gate, w_up, grad_x, grad_w_gate, grad_w_up)
-    d_ff, d_in = w_gate.shape
-    wide = (*x.shape[:-1], d_ff)
-    _of_shape("bt_glu_bwd", "x", x, (*x.shape[:-1], d_in))
-    for name, t in (("grad_h", grad_h), ("g", g), ("u", u)):
-        _of_shape("bt_glu_bwd", name, t, wide)
-    for name, t in (("w_up", w_up), ("grad_w_gate", grad_w_gate), ("grad_w_up", grad_w_up)):
-        _of_shape("bt_glu_bwd", name, t, w_gate.shape)
-    _of_shape("bt_glu_bwd", "grad_x", grad_x, x.shape)
-    st = _tensor_calls().bt_glu_bwd(grad_h, grad_h.numel() // max(d_ff, 1), d_in, d_ff, code, _act("bt_glu_bwd", activation), g, u, x,
-                                    w_gate, w_up, grad_x, grad_w_gate, grad_w_up, workspace, _nbytes(workspace),
-                                    dev_status, _stream(stream))
+    st = _native().glu_bwd(_calls().address["bt_glu_bwd"], grad_h, g, u, x, w_gate, w_up, grad_x, grad_w_gate, grad_w_up, workspace,
+                           dev_status, _act("bt_glu_bwd", activation), _stream_or_none(stream))
     return _check("bt_glu_bwd", st, check)
-
-
-def _gate_rows(call: str, gate: Optional[torch.Tensor], rows: int, d: int) -> int:
-    """The rows that share a row of the gate (d,) or (groups, d)."""
-    if gate is None:
-        return max(rows, 1)
-    groups = gate.numel() // d
-    if gate.shape[-1] != d or groups == 0 or rows % groups != 0:
-        raise ValueError(f"{call}: the gate must have the shape (groups, {d}), {rows} rows being a multiple of the groups")
-    return max(rows // groups, 1)
 
 
 def bt_block_norm_workspace_bytes(rows: int, d: int, dtype) -> int:
@@ -708,15 +680,8 @@ def bt_block_norm_fwd(x: torch.Tensor, f: Optional[torch.Tensor], gate: Optional
                       scale: float = 1.0, eps: float = 1e-6, stream=None, check: bool = True) -> int:
     """x_out = x + scale * gate * rms(f) * w_post and n_out = rms(x_out) * w_pre of (..., d) tensors; gate (d,) or (groups, d),
     each of its rows for as many consecutive rows of x.  Parts that are None are left out."""
-    code = _of_one_kind("bt_block_norm_fwd", x, f, gate, w_post, w_pre, x_out, n_out)
-    d = x.shape[-1]
-    for name, t in (("f", f), ("x_out", x_out), ("n_out", n_out)):
-        _of_shape("bt_block_norm_fwd", name, t, x.shape)
-    for name, t in (("w_post", w_post), ("w_pre", w_pre)):
-        _of_shape("bt_block_norm_fwd", name, t, (d,))
-    rows = x.numel() // max(d, 1)
-    st = _tensor_calls().bt_block_norm_fwd(x, rows, d, _gate_rows("bt_block_norm_fwd", gate, rows, d), code, float(scale), float(eps), f, gate,
-                                           w_post, w_pre, x_out, n_out, _stream(stream))
+    st = _native().block_norm_fwd(_calls().address["bt_block_norm_fwd"], x, f, gate, w_post, w_pre, x_out, n_out, scale, eps,
+                                  _stream_or_none(stream))
     return _check("bt_block_norm_fwd", st, check)
 
 
@@ -726,41 +691,17 @@ def bt_block_norm_bwd(x_out: torch.Tensor, f: Optional[torch.Tensor], gate: Opti
                       grad_w_post: Optional[torch.Tensor], grad_w_pre: Optional[torch.Tensor], workspace: Optional[torch.Tensor], *,
                       scale: float = 1.0, eps: float = 1e-6, stream=None, check: bool = True) -> int:
     """The gradients of bt_block_norm_fwd from its x_out (without f: from x); outputs that are None are not computed."""
-    code = _of_one_kind("bt_block_norm_bwd", x_out, f, gate, w_post, w_pre, grad_n, grad_x_out, grad_x, grad_f, grad_gate, grad_w_post,
-                        grad_w_pre)
-    d = x_out.shape[-1]
-    for name, t in (("f", f), ("grad_n", grad_n), ("grad_x_out", grad_x_out), ("grad_x", grad_x), ("grad_f", grad_f)):
-        _of_shape("bt_block_norm_bwd", name, t, x_out.shape)
-    for name, t in (("w_post", w_post), ("w_pre", w_pre), ("grad_w_post", grad_w_post), ("grad_w_pre", grad_w_pre)):
-        _of_shape("bt_block_norm_bwd", name, t, (d,))
-    if grad_gate is not None and gate is not None:
-        _of_shape("bt_block_norm_bwd", "grad_gate", grad_gate, gate.shape)
-    rows = x_out.numel() // max(d, 1)
-    st = _tensor_calls().bt_block_norm_bwd(x_out, rows, d, _gate_rows("bt_block_norm_bwd", gate, rows, d), code, float(scale), float(eps), f,
-                                           gate, w_post, w_pre, grad_n, grad_x_out, grad_x, grad_f,
-                                           grad_gate, grad_w_post, grad_w_pre, workspace, 0 if workspace is None else _nbytes(workspace),
-                                           _stream(stream))
+    st = _native().block_norm_bwd(_calls().address["bt_block_norm_bwd"], x_out, f, gate, w_post, w_pre, grad_n, grad_x_out, grad_x, grad_f,
+                                  grad_gate, grad_w_post, grad_w_pre, workspace, scale, eps, _stream_or_none(stream))
     return _check("bt_block_norm_bwd", st, check)
-
-
-_ITEM_WORDS = ctypes.sizeof(BatchItem) // 8
 
 
 def grad_items(grads, outs=None) -> "ctypes.Array":
     """The host array of bt_batch_item for the gradient calls: `grads[k]` and, for the products, `outs[k]` (None: in place).
     The gradients must be contiguous, of one element type and on the current device."""
-    outs = grads if outs is None else outs
-    if len(outs) != len(grads):
-        raise ValueError("grad_items: as many outputs as gradients")
-    if grads:
-        _of_one_kind("grad_items", *grads, *outs)
-    words = [0] * (_ITEM_WORDS * len(grads))
-    words[0::_ITEM_WORDS] = [t.data_ptr() for t in grads]
-    words[1::_ITEM_WORDS] = [t.data_ptr() for t in outs]
-    words[_ITEM_WORDS - 1::_ITEM_WORDS] = [t.numel() for t in grads]
-    if [t.numel() for t in outs] != words[_ITEM_WORDS - 1::_ITEM_WORDS]:
-        raise ValueError("grad_items: an output has another size than its gradient")
-    return (BatchItem * len(grads)).from_buffer(array.array("Q", words)) if words else (BatchItem * 0)()
+    items = (BatchItem * len(grads))()
+    _native().grad_items(items, grads, grads if outs is None else outs)
+    return items
 
 
 def bt_grad_workspace_bytes(ns) -> int:

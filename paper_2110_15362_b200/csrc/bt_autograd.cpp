@@ -1,5 +1,7 @@
 // The parts of the autograd integration that run once per layer and direction, as a CPython extension on torch's C++ API:
-// the node of the ReLU that stashes its activation, the restore of a stash, and the wait for a stash's count.  No
+// the node of the ReLU that stashes its activation, the restore of a stash, the wait for a stash's count, and the binding's
+// calls of the transformer-block operators with the checks of their tensors (in Python 6 to 10 us a call, more than their
+// kernels take on a token; here under 1).  No
 // arithmetic here: every function allocates its outputs and calls the library's C ABI, through the address it is given
 // (a caller may have more than one build of the library open).
 //
@@ -12,10 +14,12 @@
 
 #include <ATen/ATen.h>
 #include <c10/cuda/CUDAStream.h>
+#include <c10/util/ScopeExit.h>
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
+#include <torch/csrc/utils/object_ptr.h>
 
 #include "bittrain.h"
 
@@ -212,10 +216,300 @@ PyObject *synchronize(PyObject *, PyObject *)
     END_HANDLE_TH_ERRORS
 }
 
+// ---------------------------------------------------------------------------------------------- transformer-block operators
+[[noreturn]] void refuse(PyObject *error, const char *format, ...)
+{
+    va_list v;
+    va_start(v, format);
+    PyErr_FormatV(error, format, v);
+    va_end(v);
+    throw python_error();
+}
+// A tensor argument: None is an undefined tensor.
+Tensor tensor_or_none(PyObject *o)
+{
+    if (o == Py_None) return Tensor();
+    if (!THPVariable_Check(o)) refuse(PyExc_TypeError, "a tensor or None is wanted, not %s", Py_TYPE(o)->tp_name);
+    return THPVariable_Unpack(o);
+}
+void *data_of(const Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
+std::string text(at::IntArrayRef shape)
+{
+    std::string s = "(";
+    for (size_t k = 0; k < shape.size(); ++k) s += (k ? ", " : "") + std::to_string(shape[k]);
+    return s + ")";
+}
+
+// What the tensors of a call have to have in common.  The first is given; undefined ones are left out.
+struct Call {
+    const char *name;
+    Tensor      first;
+    void same_kind(std::initializer_list<const Tensor *> tensors) const
+    {
+        for (const Tensor *t : tensors)
+            if (t->defined() && (t->scalar_type() != first.scalar_type() || t->device() != first.device() || !t->is_contiguous()))
+                refuse(PyExc_ValueError, "%s: the tensors must be contiguous, of one element type and on one device", name);
+    }
+    int code() const
+    {
+        switch (first.scalar_type()) {
+        case at::kFloat: case at::kHalf: case at::kBFloat16: case at::kDouble: return code_of(first.scalar_type());
+        default: refuse(PyExc_ValueError, "%s: %s is not an element type of the library", name, c10::toString(first.scalar_type()));
+        }
+    }
+    void shape(const char *what, const Tensor &t, at::IntArrayRef want) const
+    {
+        if (t.defined() && t.sizes() != want)
+            refuse(PyExc_ValueError, "%s: %s must have the shape %s, not %s", name, what, text(want).c_str(), text(t.sizes()).c_str());
+    }
+    void on_current_device() const
+    {
+        if (!first.is_cuda()) refuse(PyExc_ValueError, "%s: the tensors must be on a CUDA device, not on %s", name, first.device().str().c_str());
+        if (first.get_device() != c10::cuda::current_device())
+            refuse(PyExc_ValueError, "%s: the tensors are on %s, which is not the current device", name, first.device().str().c_str());
+    }
+    // a workspace or None, on the same device: its bytes
+    size_t scratch(const Tensor &t) const
+    {
+        if (!t.defined()) return 0;
+        if (!t.is_contiguous() || t.device() != first.device()) refuse(PyExc_ValueError, "%s: the workspace must be contiguous and on the tensors' device", name);
+        return t.nbytes();
+    }
+    int32_t *status(const Tensor &t) const
+    {
+        if (!t.defined()) return nullptr;
+        if (t.scalar_type() != at::kInt || t.numel() < 1 || t.device() != first.device())
+            refuse(PyExc_ValueError, "%s: dev_status must be an int32 tensor on the tensors' device", name);
+        return static_cast<int32_t *>(t.data_ptr());
+    }
+};
+void *stream_of(PyObject *o)
+{
+    if (o == Py_None) return stream();
+    void *const s = PyLong_AsVoidPtr(o);
+    if (PyErr_Occurred()) throw python_error();
+    return s;
+}
+uintptr_t function_at(PyObject *o)
+{
+    const uintptr_t f = reinterpret_cast<uintptr_t>(PyLong_AsVoidPtr(o));
+    if (PyErr_Occurred()) throw python_error();
+    return f;
+}
+void arity(Py_ssize_t n, Py_ssize_t want)
+{
+    if (n != want) refuse(PyExc_TypeError, "%zd arguments are wanted, not %zd", want, n);
+}
+// the shape of a (..., d_in) tensor's rows of another width
+c10::SmallVector<int64_t, 6> with_last(const Tensor &t, int64_t last)
+{
+    c10::SmallVector<int64_t, 6> s(t.sizes().begin(), t.sizes().end());
+    if (!s.empty()) s.back() = last;
+    return s;
+}
+struct GluSizes {
+    int64_t rows, d_in, d_ff;
+};
+GluSizes glu_sizes(const Call &c, const Tensor &x, const Tensor &w_gate, const Tensor &w_up)
+{
+    if (w_gate.dim() != 2 || x.dim() == 0) refuse(PyExc_ValueError, "%s: x must have the shape (..., d_in) and w_gate (d_ff, d_in)", c.name);
+    const int64_t d_ff = w_gate.size(0), d_in = w_gate.size(1);
+    c.shape("x", x, with_last(x, d_in));
+    c.shape("w_up", w_up, w_gate.sizes());
+    int64_t rows = 1;
+    for (int64_t k = 0; k + 1 < x.dim(); ++k) rows *= x.size(k);
+    return {rows, d_in, d_ff};
+}
+
+// glu_fwd(function, x, w_gate, w_up, h, g_out, u_out, workspace, dev_status, activation, stream) -> status
+PyObject *glu_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    arity(n, 11);
+    const auto   fn = reinterpret_cast<decltype(&bt_glu_fwd)>(function_at(a[0]));
+    const Tensor x = tensor_or_none(a[1]), wg = tensor_or_none(a[2]), wu = tensor_or_none(a[3]), h = tensor_or_none(a[4]), g = tensor_or_none(a[5]),
+                 u = tensor_or_none(a[6]), ws = tensor_or_none(a[7]), st = tensor_or_none(a[8]);
+    const int    act = static_cast<int>(PyLong_AsLong(a[9]));
+    if (!x.defined() || !wg.defined() || !wu.defined() || !h.defined()) refuse(PyExc_TypeError, "bt_glu_fwd: x, w_gate, w_up and h are tensors");
+    const Call c{"bt_glu_fwd", x};
+    c.same_kind({&x, &wg, &wu, &h, &g, &u});
+    const int      code = c.code();
+    const GluSizes s    = glu_sizes(c, x, wg, wu);
+    const auto     wide = with_last(x, s.d_ff);
+    c.shape("h", h, wide), c.shape("g_out", g, wide), c.shape("u_out", u, wide);
+    c.on_current_device();
+    const size_t   ws_bytes = c.scratch(ws);
+    int32_t *const status   = c.status(st);
+    void *const    on       = stream_of(a[10]);
+    int            result;
+    {
+        pybind11::gil_scoped_release no_gil;
+        result = fn(x.data_ptr(), s.rows, s.d_in, s.d_ff, code, act, wg.data_ptr(), wu.data_ptr(), h.data_ptr(), data_of(g), data_of(u), data_of(ws), ws_bytes,
+                    status, on);
+    }
+    return PyLong_FromLong(result);
+    END_HANDLE_TH_ERRORS
+}
+
+// glu_bwd(function, grad_h, g, u, x, w_gate, w_up, grad_x, grad_w_gate, grad_w_up, workspace, dev_status, activation, stream) -> status
+PyObject *glu_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    arity(n, 14);
+    const auto fn = reinterpret_cast<decltype(&bt_glu_bwd)>(function_at(a[0]));
+    Tensor     t[11];
+    for (int k = 0; k < 11; ++k) t[k] = tensor_or_none(a[k + 1]);
+    const Tensor &dh = t[0], &g = t[1], &u = t[2], &x = t[3], &wg = t[4], &wu = t[5], &dx = t[6], &dwg = t[7], &dwu = t[8], &ws = t[9], &st = t[10];
+    const int     act = static_cast<int>(PyLong_AsLong(a[12]));
+    for (int k = 0; k < 6; ++k)
+        if (!t[k].defined()) refuse(PyExc_TypeError, "bt_glu_bwd: grad_h, g, u, x, w_gate and w_up are tensors");
+    const Call c{"bt_glu_bwd", dh};
+    c.same_kind({&dh, &g, &u, &x, &wg, &wu, &dx, &dwg, &dwu});
+    const int      code = c.code();
+    const GluSizes s    = glu_sizes(c, x, wg, wu);
+    const auto     wide = with_last(x, s.d_ff);
+    c.shape("grad_h", dh, wide), c.shape("g", g, wide), c.shape("u", u, wide);
+    c.shape("grad_w_gate", dwg, wg.sizes()), c.shape("grad_w_up", dwu, wg.sizes()), c.shape("grad_x", dx, x.sizes());
+    c.on_current_device();
+    const size_t   ws_bytes = c.scratch(ws);
+    int32_t *const status   = c.status(st);
+    void *const    on       = stream_of(a[13]);
+    int            result;
+    {
+        pybind11::gil_scoped_release no_gil;
+        result = fn(dh.data_ptr(), s.rows, s.d_in, s.d_ff, code, act, g.data_ptr(), u.data_ptr(), x.data_ptr(), wg.data_ptr(), wu.data_ptr(), data_of(dx),
+                    data_of(dwg), data_of(dwu), data_of(ws), ws_bytes, status, on);
+    }
+    return PyLong_FromLong(result);
+    END_HANDLE_TH_ERRORS
+}
+
+struct NormSizes {
+    int64_t rows, d, gate_rows;
+};
+// the sizes of a norm's call, and the rows that share a row of its gate, (d,) or (groups, d)
+NormSizes norm_sizes(const Call &c, const Tensor &x, const Tensor &gate)
+{
+    if (x.dim() == 0) refuse(PyExc_ValueError, "%s: x must have the shape (..., d)", c.name);
+    NormSizes s{1, x.size(-1), 1};
+    for (int64_t k = 0; k + 1 < x.dim(); ++k) s.rows *= x.size(k);
+    s.gate_rows = s.rows > 0 ? s.rows : 1;
+    if (gate.defined()) {
+        const bool    fits   = gate.dim() >= 1 && gate.size(-1) == s.d && gate.numel() > 0;
+        const int64_t groups = fits ? gate.numel() / s.d : 0;
+        if (!fits || s.rows % groups != 0)
+            refuse(PyExc_ValueError, "%s: the gate must have the shape (groups, %lld), %lld rows being a multiple of the groups", c.name,
+                                    static_cast<long long>(s.d), static_cast<long long>(s.rows));
+        if (s.rows > 0) s.gate_rows = s.rows / groups;
+    }
+    return s;
+}
+
+// block_norm_fwd(function, x, f, gate, w_post, w_pre, x_out, n_out, scale, eps, stream) -> status
+PyObject *block_norm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    arity(n, 11);
+    const auto fn = reinterpret_cast<decltype(&bt_block_norm_fwd)>(function_at(a[0]));
+    Tensor     t[7];
+    for (int k = 0; k < 7; ++k) t[k] = tensor_or_none(a[k + 1]);
+    const Tensor &x = t[0], &f = t[1], &gate = t[2], &post = t[3], &pre = t[4], &y = t[5], &nn = t[6];
+    const float   scale = static_cast<float>(PyFloat_AsDouble(a[8])), eps = static_cast<float>(PyFloat_AsDouble(a[9]));
+    if (PyErr_Occurred()) return nullptr;
+    if (!x.defined()) refuse(PyExc_TypeError, "bt_block_norm_fwd: x is a tensor");
+    const Call c{"bt_block_norm_fwd", x};
+    c.same_kind({&x, &f, &gate, &post, &pre, &y, &nn});
+    const int       code = c.code();
+    const NormSizes s    = norm_sizes(c, x, gate);
+    c.shape("f", f, x.sizes()), c.shape("x_out", y, x.sizes()), c.shape("n_out", nn, x.sizes());
+    c.shape("w_post", post, {s.d}), c.shape("w_pre", pre, {s.d});
+    c.on_current_device();
+    void *const on = stream_of(a[10]);
+    int         result;
+    {
+        pybind11::gil_scoped_release no_gil;
+        result = fn(x.data_ptr(), s.rows, s.d, s.gate_rows, code, scale, eps, data_of(f), data_of(gate), data_of(post), data_of(pre), data_of(y), data_of(nn), on);
+    }
+    return PyLong_FromLong(result);
+    END_HANDLE_TH_ERRORS
+}
+
+// block_norm_bwd(function, x_out, f, gate, w_post, w_pre, grad_n, grad_x_out, grad_x, grad_f, grad_gate, grad_w_post, grad_w_pre,
+//                workspace, scale, eps, stream) -> status
+PyObject *block_norm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    arity(n, 17);
+    const auto fn = reinterpret_cast<decltype(&bt_block_norm_bwd)>(function_at(a[0]));
+    Tensor     t[13];
+    for (int k = 0; k < 13; ++k) t[k] = tensor_or_none(a[k + 1]);
+    const Tensor &x = t[0], &f = t[1], &gate = t[2], &post = t[3], &pre = t[4], &gn = t[5], &gy = t[6], &dx = t[7], &df = t[8], &dgate = t[9], &dpost = t[10],
+                 &dpre = t[11], &ws = t[12];
+    const float scale = static_cast<float>(PyFloat_AsDouble(a[14])), eps = static_cast<float>(PyFloat_AsDouble(a[15]));
+    if (PyErr_Occurred()) return nullptr;
+    if (!x.defined()) refuse(PyExc_TypeError, "bt_block_norm_bwd: x_out is a tensor");
+    const Call c{"bt_block_norm_bwd", x};
+    c.same_kind({&x, &f, &gate, &post, &pre, &gn, &gy, &dx, &df, &dgate, &dpost, &dpre});
+    const int       code = c.code();
+    const NormSizes s    = norm_sizes(c, x, gate);
+    for (const auto &[what, v] : {std::pair<const char *, const Tensor *>{"f", &f}, {"grad_n", &gn}, {"grad_x_out", &gy}, {"grad_x", &dx}, {"grad_f", &df}})
+        c.shape(what, *v, x.sizes());
+    for (const auto &[what, v] : {std::pair<const char *, const Tensor *>{"w_post", &post}, {"w_pre", &pre}, {"grad_w_post", &dpost}, {"grad_w_pre", &dpre}})
+        c.shape(what, *v, {s.d});
+    if (gate.defined()) c.shape("grad_gate", dgate, gate.sizes());
+    c.on_current_device();
+    const size_t ws_bytes = c.scratch(ws);
+    void *const  on       = stream_of(a[16]);
+    int          result;
+    {
+        pybind11::gil_scoped_release no_gil;
+        result = fn(x.data_ptr(), s.rows, s.d, s.gate_rows, code, scale, eps, data_of(f), data_of(gate), data_of(post), data_of(pre), data_of(gn), data_of(gy),
+                    data_of(dx), data_of(df), data_of(dgate), data_of(dpost), data_of(dpre), data_of(ws), ws_bytes, on);
+    }
+    return PyLong_FromLong(result);
+    END_HANDLE_TH_ERRORS
+}
+
+// grad_items(items, grads, outs): fills a ctypes array of bt_batch_item of as many items as there are gradients (all of its words
+// but these are zeros already) with the sequences' tensors
+PyObject *grad_items(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    arity(n, 3);
+    THPObjectPtr grads(PySequence_Fast(a[1], "grad_items: a sequence of tensors is wanted")), outs(PySequence_Fast(a[2], "grad_items: a sequence of tensors is wanted"));
+    if (!grads || !outs) throw python_error();
+    const Py_ssize_t count = PySequence_Fast_GET_SIZE(grads.get());
+    if (PySequence_Fast_GET_SIZE(outs.get()) != count) refuse(PyExc_ValueError, "grad_items: as many outputs as gradients");
+    Py_buffer buffer;
+    if (PyObject_GetBuffer(a[0], &buffer, PyBUF_WRITABLE) != 0) throw python_error();
+    const auto release = c10::make_scope_exit([&] { PyBuffer_Release(&buffer); });
+    if (buffer.len < count * static_cast<Py_ssize_t>(sizeof(bt_batch_item))) refuse(PyExc_ValueError, "grad_items: the array is too short");
+    auto *const items = static_cast<bt_batch_item *>(buffer.buf);
+    for (Py_ssize_t k = 0; k < count; ++k) {
+        const Tensor g = tensor_or_none(PySequence_Fast_GET_ITEM(grads.get(), k)), y = tensor_or_none(PySequence_Fast_GET_ITEM(outs.get(), k));
+        if (!g.defined() || !y.defined()) refuse(PyExc_TypeError, "grad_items: tensors are wanted");
+        const Call c{"grad_items", k == 0 ? g : THPVariable_Unpack(PySequence_Fast_GET_ITEM(grads.get(), 0))};
+        c.same_kind({&g, &y});
+        c.code();
+        if (g.is_cuda()) c.on_current_device();
+        if (y.numel() != g.numel()) refuse(PyExc_ValueError, "grad_items: an output has another size than its gradient");
+        items[k].dense = g.data_ptr();
+        items[k].y_out = y.data_ptr();
+        items[k].n     = static_cast<uint64_t>(g.numel());
+    }
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
 PyMethodDef methods[] = {
     {"relu_stash", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(relu_stash)), METH_FASTCALL, nullptr},
     {"restore", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(restore)), METH_FASTCALL, nullptr},
     {"synchronize", synchronize, METH_NOARGS, nullptr},
+    {"glu_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(glu_fwd)), METH_FASTCALL, nullptr},
+    {"glu_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(glu_bwd)), METH_FASTCALL, nullptr},
+    {"block_norm_fwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(block_norm_fwd)), METH_FASTCALL, nullptr},
+    {"block_norm_bwd", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(block_norm_bwd)), METH_FASTCALL, nullptr},
+    {"grad_items", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(grad_items)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr},
 };
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_autograd", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

@@ -1,12 +1,12 @@
 /* _pycall: calls of the C ABI from Python without ctypes' marshalling.
  *
  * native_call(address, kinds, otherwise, item) wraps the address of an exported function that takes pointers, integers and
- * at most two floats, and returns an int (an element of the ABI's status enumeration).  `kinds` has a letter per parameter:
+ * at most one float, and returns an int (an element of the ABI's status enumeration).  `kinds` has a letter per parameter:
  *   p   a tensor: the result of the argument's data_ptr() method, or a null pointer for None,
  *   a   the same, or an address as an integer,
  *   s   a stream: an integer, or None,
  *   n   a count, a size or a code: an integer,
- *   f   a float,
+ *   f   the function's one float: a float,
  *   b   a ctypes array of `item` (bt_batch_item): the address of its memory.
  * A call whose arguments are not all of these very kinds, or not as many, is handed to `otherwise` as it is, which converts
  * or refuses them (the binding passes ctypes' own call of the same function): a float or a tensor given for a count must
@@ -17,8 +17,8 @@
  * integer, None, a float, a buffer (its address) or a tensor, and the caller answers for their number and order.
  *
  * On x86-64 integer and pointer arguments travel in one sequence (six registers, then the stack) and float arguments in
- * another, so one prototype -- two floats and kMax integer words -- fits every such function: the callee does not look at
- * floats or words behind its own, and the caller clears the stack.  On other hosts the module is not built, and the binding calls
+ * another, so one prototype -- a float and kMax integer words -- fits every such function: the callee does not look at
+ * words behind its own, and the caller clears the stack.  On other hosts the module is not built, and the binding calls
  * through ctypes alone.
  */
 #define PY_SSIZE_T_CLEAN
@@ -32,16 +32,16 @@
 #error "the argument passing relied on here is that of x86-64"
 #endif
 
-enum { kMax = 20, kMaxFloats = 2, kMaxBuffers = 4 };
+enum { kMax = 18, kMaxBuffers = 4 };
 
 typedef uint64_t W;
-typedef int (*Function)(float, float, W, W, W, W, W, W, W, W, W, W, W, W, W, W, W, W, W, W, W, W);
+typedef int (*Function)(float, W, W, W, W, W, W, W, W, W, W, W, W, W, W, W, W, W, W);
 
 typedef struct {
     PyObject_HEAD
     vectorcallfunc vectorcall;
     Function       function;
-    char           kinds[kMax + kMaxFloats + 1];   /* a letter per parameter; empty: not given */
+    char           kinds[kMax + 2];   /* a letter per parameter; empty: not given */
     Py_ssize_t     arity;
     PyObject      *otherwise, *item;
 } NativeCall;
@@ -73,9 +73,9 @@ static PyObject *checked_vectorcall(PyObject *self, PyObject *const *args, size_
     NativeCall *const c = (NativeCall *)self;
     const Py_ssize_t  n = PyVectorcall_NARGS(nargsf);
     W                 a[kMax] = {0};
-    float             f[kMaxFloats] = {0};
+    float             f       = 0.0f;
     Py_buffer         items;
-    int               held = 0, k = 0, floats = 0, status = 0;
+    int               held = 0, k = 0, status = 0;
     if (n != c->arity || (kwnames != NULL && PyTuple_GET_SIZE(kwnames) != 0)) return PyObject_Vectorcall(c->otherwise, args, (size_t)n, kwnames);
     for (Py_ssize_t i = 0; i < n; ++i) {
         PyObject *const o = args[i];
@@ -86,7 +86,7 @@ static PyObject *checked_vectorcall(PyObject *self, PyObject *const *args, size_
             else other = 1;
             break;
         case 'f':
-            if (PyFloat_Check(o)) f[floats++] = (float)PyFloat_AS_DOUBLE(o);
+            if (PyFloat_Check(o)) f = (float)PyFloat_AS_DOUBLE(o);
             else other = 1;
             break;
         case 'b':
@@ -113,8 +113,7 @@ static PyObject *checked_vectorcall(PyObject *self, PyObject *const *args, size_
     {
         const Function fn = c->function;
         Py_BEGIN_ALLOW_THREADS
-        status = fn(f[0], f[1], a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12], a[13], a[14], a[15], a[16], a[17], a[18],
-                    a[19]);
+        status = fn(f, a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12], a[13], a[14], a[15], a[16], a[17]);
         Py_END_ALLOW_THREADS
     }
     if (held) PyBuffer_Release(&items);
@@ -125,25 +124,21 @@ static PyObject *native_call_vectorcall(PyObject *self, PyObject *const *args, s
 {
     const Py_ssize_t n = PyVectorcall_NARGS(nargsf);
     W                a[kMax] = {0};
-    float            f[kMaxFloats] = {0};
+    float            f       = 0.0f;
     Py_buffer        buffers[kMaxBuffers];
-    int              held = 0, k = 0, floats = 0, status = 0;
+    int              held = 0, k = 0, status = 0;
     if (kwnames != NULL && PyTuple_GET_SIZE(kwnames) != 0) {
         PyErr_SetString(PyExc_TypeError, "a native call takes no keyword arguments");
         return NULL;
     }
-    if (n > kMax + kMaxFloats) {
+    if (n > kMax + 1) {
         PyErr_SetString(PyExc_TypeError, "too many arguments");
         return NULL;
     }
     for (Py_ssize_t i = 0; i < n; ++i) {
         PyObject *const o = args[i];
         if (PyFloat_Check(o)) {
-            if (floats == kMaxFloats) {
-                PyErr_SetString(PyExc_TypeError, "too many floats");
-                goto fail;
-            }
-            f[floats++] = (float)PyFloat_AS_DOUBLE(o);
+            f = (float)PyFloat_AS_DOUBLE(o);
             continue;
         }
         if (k == kMax) {
@@ -177,8 +172,7 @@ static PyObject *native_call_vectorcall(PyObject *self, PyObject *const *args, s
     {
         const Function fn = ((NativeCall *)self)->function;
         Py_BEGIN_ALLOW_THREADS
-        status = fn(f[0], f[1], a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12], a[13], a[14], a[15], a[16], a[17], a[18],
-                    a[19]);
+        status = fn(f, a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], a[12], a[13], a[14], a[15], a[16], a[17]);
         Py_END_ALLOW_THREADS
     }
     while (held > 0) PyBuffer_Release(&buffers[--held]);
@@ -233,7 +227,7 @@ static PyObject *native_call(PyObject *module, PyObject *args)
             *q == 'f' ? ++floats : ++words;
             batches += *q == 'b';
         }
-        if (words > kMax || floats > kMaxFloats || batches > 1 || !*kinds || otherwise == NULL || !PyCallable_Check(otherwise) || (batches && item == NULL)) {
+        if (words > kMax || floats > 1 || batches > 1 || !*kinds || otherwise == NULL || !PyCallable_Check(otherwise) || (batches && item == NULL)) {
             PyErr_SetString(PyExc_ValueError, "not the parameters of a native call");
             return NULL;
         }

@@ -166,33 +166,21 @@ def test_items_name_their_tensors():
     assert [(it.dense or 0, it.y_out or 0, it.n) for it in items] == [(a.data_ptr(), b.data_ptr(), a.numel()) for a, b in zip(g, y)]
     assert all(it.bitmap is None and it.dev_status is None for it in items)
     assert len(B.grad_items([])) == 0
+    with pytest.raises(TypeError):
+        B.grad_items([torch.zeros(3), None])
+    with pytest.raises(TypeError):
+        B.grad_items(3)
 
 
-@pytest.mark.parametrize("name", B.WIDE_CALLS)
-def test_calls_with_two_floats_and_many_words(L, name, tmp_path):
-    """The wide calls pass what ctypes passes: distinct ordinary values for every parameter, in registers and on the stack."""
-    import subprocess
-    fn = getattr(L, name)
-    types = fn.argtypes
-    c_name = {ctypes.c_void_p: "void *", ctypes.c_uint64: "unsigned long long", ctypes.c_int: "int", ctypes.c_float: "float", ctypes.c_size_t: "unsigned long long"}
-    args = ", ".join("%s a%d" % (c_name[t], k) for k, t in enumerate(types))
-    body = "".join("seen[%d] = (double)(unsigned long long)a%d;" % (k, k) if t is not ctypes.c_float else "seen[%d] = a%d;" % (k, k) for k, t in enumerate(types))
-    (tmp_path / "s.c").write_text("double seen[32]; int %s(%s) { %s return 0; }" % (name, args, body))
-    subprocess.check_call(["gcc", "-O1", "-w", "-shared", "-fPIC", "-o", str(tmp_path / "s.so"), str(tmp_path / "s.c")])
-    S = ctypes.CDLL(str(tmp_path / "s.so"))
-    stub = getattr(S, name)
-    stub.argtypes, stub.restype = types, ctypes.c_int
-    at = ctypes.cast(stub, ctypes.c_void_p).value
-    kinds = "".join({ctypes.c_void_p: "p", ctypes.c_float: "f"}.get(t, "n") for t in types[:-1]) + "s"
-    call = B._native_call()(at, kinds, B._through_ctypes(stub, kinds), B.BatchItem)
-    values = []
-    for k, t in enumerate(types):
-        last = k + 1 == len(types)
-        values.append(0x7000 + k if last else torch.zeros(16) if t is ctypes.c_void_p else 0.25 + k if t is ctypes.c_float else 100 + k)
-    assert call(*values) == 0
-    want = [v.data_ptr() if torch.is_tensor(v) else v for v in values]
-    assert list((ctypes.c_double * 32).in_dll(S, "seen"))[:len(types)] == want
-    with pytest.raises((TypeError, ctypes.ArgumentError)):
-        call(*values[:-1])
-    with pytest.raises(AttributeError):
-        call(0x10000, *values[1:])
+def test_only_tensors_of_the_current_device_are_taken():
+    x, w, h = torch.zeros(4, 16), torch.zeros(32, 16), torch.zeros(4, 32)
+    with pytest.raises(ValueError, match="CUDA device"):
+        B.bt_glu_fwd(x, w, w, h, None, None, x)
+    with pytest.raises(ValueError, match="CUDA device"):
+        B.bt_block_norm_fwd(x, x, None, None, torch.zeros(16), torch.zeros(4, 16), torch.zeros(4, 16))
+    with pytest.raises(TypeError):
+        B.bt_glu_fwd(x.numpy(), w, w, h, None, None, x)
+    with pytest.raises(TypeError):
+        B.bt_glu_fwd(None, w, w, h, None, None, x)
+    with pytest.raises(TypeError):
+        B.bt_block_norm_fwd(x, x, None, None, torch.zeros(16), torch.zeros(4, 16), torch.zeros(4, 16), scale="1")
