@@ -70,6 +70,15 @@ struct MmaArgs {
 };
 
 // ---------------------------------------------------------------------------------------------- PTX
+// One lane of a converged warp.  The roles' loops are run by whole warps and only the instructions themselves by one lane: so the
+// compiler keeps descriptors and addresses in uniform registers, where these instructions want them.  (In a branch for lane 0
+// a block of four products took 570 cycles to issue and a stage's copies 430.)
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
 __device__ __forceinline__ uint32_t cluster_rank()
 {
     uint32_t r;
@@ -89,14 +98,14 @@ __device__ __forceinline__ uint32_t in_first_cta(uint32_t addr)
 }
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t addr)
 {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(addr) : "memory");
 }
-__device__ __forceinline__ bool mbar_try_wait_cluster(uint32_t bar, uint32_t parity)
+__device__ __forceinline__ bool mbar_try_wait_at(uint32_t bar, uint32_t parity)
 {
     uint32_t ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok)
         : "r"(bar), "r"(parity)
@@ -174,20 +183,20 @@ constexpr uint32_t kInstruction = 1u << 4 |                                     
                                   static_cast<uint32_t>(kN / 8) << 17 | static_cast<uint32_t>(256 / 16) << 24;
 
 // ---------------------------------------------------------------------------------------------- waits
-// A CTA's word that says that one of its roles gave up.
+// A CTA's word that says that one of its roles gave up.  A whole warp waits, and all its lanes get the same answer.
 struct Waits {
     volatile uint32_t *gave_up;
     int32_t           *dev_status;
     __device__ __forceinline__ bool operator()(uint32_t bar, uint32_t parity) const
     {
-        if (mbar_try_wait_cluster(bar, parity)) return true;
+        if (__all_sync(0xFFFFFFFFu, mbar_try_wait_at(bar, parity))) return true;
         const uint64_t begin = now_ns();
         for (;;) {
 #pragma unroll 1
             for (int k = 0; k < 64; ++k)
-                if (mbar_try_wait_cluster(bar, parity)) return true;
-            if (*gave_up) return false;
-            if (now_ns() - begin > kDefaultWaitNs) {
+                if (__all_sync(0xFFFFFFFFu, mbar_try_wait_at(bar, parity))) return true;
+            if (__any_sync(0xFFFFFFFFu, *gave_up != 0)) return false;
+            if (__any_sync(0xFFFFFFFFu, now_ns() - begin > kDefaultWaitNs)) {
                 *gave_up = 1;
                 if (dev_status) *reinterpret_cast<volatile int32_t *>(dev_status) = BT_ERR_TIMEOUT;
                 return false;
@@ -260,7 +269,7 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
     uint32_t *const      tmem_word = reinterpret_cast<uint32_t *>(generic + S::kBytes + 8 * (2 * kStages + 4));
     volatile uint32_t   *gave_up   = tmem_word + 1;
 
-    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, rank = cluster_rank();
+    const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, rank = cluster_rank();
     const Waits    wait{gave_up, p.dev_status};
     if (threadIdx.x == 0) {
         uint64_t *const b = reinterpret_cast<uint64_t *>(generic + S::kBytes);
@@ -294,50 +303,55 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
     };
     if (warp == 0) {
         // ---- loader
-        if (lane == 0) {
-            Ring<kStages> ring;
-            bool          ok = true;
-            for (uint32_t t = first; t < p.tiles && ok; t += step) {
-                const Tile     tile = tile_at(p, split ? t / p.splits : t);
-                const int      i0   = static_cast<int>(tile.i * 256 + rank * kRows);
-                const uint32_t end  = end_block(t) * kPlanes<DT>;
-                for (uint32_t it = from_block(t) * kPlanes<DT>; it < end; ++it) {
-                    const uint32_t k = it / kPlanes<DT>, plane = it % kPlanes<DT>;
+        Ring<kStages>  ring;
+        bool           ok          = true;
+        const uint32_t leader_bars = in_first_cta(full(0));
+        for (uint32_t t = first; t < p.tiles && ok; t += step) {
+            const Tile     tile = tile_at(p, split ? t / p.splits : t);
+            const int      i0   = static_cast<int>(tile.i * 256 + rank * kRows);
+            const uint32_t end  = end_block(t);
+            for (uint32_t k = from_block(t); k < end && ok; ++k) {
+                const uint32_t pair = kUse == kInputGrad ? (k >= p.blocks ? 1u : 0u) : 0u;
+                const int      k0   = static_cast<int>((k - pair * p.blocks) * kDepth);
+#pragma unroll
+                for (int plane = 0; plane < static_cast<int>(kPlanes<DT>); ++plane) {
                     if (!(ok = wait(empty(ring.stage), ring.phase ^ 1))) break;
                     const uint32_t a = base + ring.stage * (S::kABytes + S::kBBytes), b = a + S::kABytes;
-                    const uint32_t bar = in_first_cta(full(ring.stage));
-                    // the pair's bytes are expected once, in its first CTA
-                    if (rank == 0)
-                        asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full(ring.stage)), "r"(2 * (S::kABytes + S::kBBytes)) : "memory");
-                    const uint32_t pair = kUse == kInputGrad ? (k >= p.blocks ? 1u : 0u) : 0u;
-                    const int      k0   = static_cast<int>((k - pair * p.blocks) * kDepth);
-                    if constexpr (kUse == kForward) {
-                        tma_load(a, &p.a[0], k0, i0, plane, bar);
-                        tma_load(b, &p.b[rank], k0, static_cast<int>(tile.j * (kN / 2)), plane, bar);
-                    } else {
-                        const int j0 = static_cast<int>(tile.j * kN + rank * (kN / 2));
-                        if constexpr (kUse == kInputGrad) {
-                            tma_load(a, &p.a[pair], k0, i0, plane, bar);
+                    const uint32_t bar = leader_bars + 8 * ring.stage;
+                    if (elect_one()) {
+                        // the pair's bytes are expected once, in its first CTA
+                        if (rank == 0)
+                            asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(full(ring.stage)), "r"(2 * (S::kABytes + S::kBBytes)) : "memory");
+                        if constexpr (kUse == kForward) {
+                            tma_load(a, &p.a[0], k0, i0, plane, bar);
+                            tma_load(b, rank == 0 ? &p.b[0] : &p.b[1], k0, static_cast<int>(tile.j * (kN / 2)), plane, bar);
                         } else {
+                            const int          j0    = static_cast<int>(tile.j * kN + rank * (kN / 2));
+                            const CUtensorMap *map_a = (kUse == kInputGrad ? pair : tile.which) == 0 ? &p.a[0] : &p.a[1];
+                            const CUtensorMap *map_b = kUse == kInputGrad && pair != 0 ? &p.b[1] : &p.b[0];
+                            if constexpr (kUse == kInputGrad) {
+                                tma_load(a, map_a, k0, i0, plane, bar);
+                            } else {
 #pragma unroll
-                            for (int v = 0; v < kRows / 64; ++v) tma_load(a + v * 64 * kDepth * 2, &p.a[tile.which], i0 + 64 * v, k0, plane, bar);
+                                for (int v = 0; v < kRows / 64; ++v) tma_load(a + v * 64 * kDepth * 2, map_a, i0 + 64 * v, k0, plane, bar);
+                            }
+#pragma unroll
+                            for (int v = 0; v < kN / 2 / 64; ++v) tma_load(b + v * 64 * kDepth * 2, map_b, j0 + 64 * v, k0, plane, bar);
                         }
-#pragma unroll
-                        for (int v = 0; v < kN / 2 / 64; ++v) tma_load(b + v * 64 * kDepth * 2, &p.b[kUse == kInputGrad ? pair : 0], j0 + 64 * v, k0, plane, bar);
                     }
+                    __syncwarp();
                     ring.next();
                 }
             }
-            // the last products have read their tiles: nothing arrives at this CTA's barriers any more
-            for (uint32_t s = 0; s < kStages && ok; ++s) {
-                ok = wait(empty(ring.stage), ring.phase ^ 1);
-                ring.next();
-            }
         }
-        __syncwarp();
+        // the last products have read their tiles: nothing arrives at this CTA's barriers any more
+        for (uint32_t s = 0; s < kStages && ok; ++s) {
+            ok = wait(empty(ring.stage), ring.phase ^ 1);
+            ring.next();
+        }
     } else if (warp == 1) {
         // ---- issuer
-        if (rank == 0 && lane == 0) {
+        if (rank == 0) {
             Ring<kStages> ring;
             Ring<2>       half;
             bool          ok = true;
@@ -362,37 +376,42 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
 #pragma unroll
                             for (int s = 0; s < 3; ++s) {
                                 if (ok && !(ok = wait(full(ring.stage), ring.phase))) break;
-                                tmem_fence_after();
                                 const uint32_t at = base + ring.stage * (S::kABytes + S::kBBytes);
                                 slot[s] = ring.stage, a[s] = operand<kAcrossA>(at), b[s] = operand<kAcrossB>(at + S::kABytes);
-                                if (s == 0) product(d, a[0], b[0], k != begin);
-                                if (s == 1) product(d + kN, a[0], b[1], k != begin), product(d + kN, a[1], b[0], true), product(d + kN, a[1], b[1], true);
-                                if (s == 2) product(d + kN, a[0], b[2], true), product(d + kN, a[2], b[0], true);
+                                if (elect_one()) {
+                                    if (s == 0) product(d, a[0], b[0], k != begin);
+                                    if (s == 1) product(d + kN, a[0], b[1], k != begin), product(d + kN, a[1], b[0], true), product(d + kN, a[1], b[1], true);
+                                    if (s == 2) {
+                                        product(d + kN, a[0], b[2], true), product(d + kN, a[2], b[0], true);
+#pragma unroll
+                                        for (int r = 0; r < 3; ++r) commit_pair(empty(slot[r]));
+                                    }
+                                }
+                                __syncwarp();
                                 ring.next();
                             }
-                            if (!ok) break;
-#pragma unroll
-                            for (int s = 0; s < 3; ++s) commit_pair(empty(slot[s]));
                         } else {
                             if (!(ok = wait(full(ring.stage), ring.phase))) break;
-                            tmem_fence_after();
                             const uint32_t a = base + ring.stage * (S::kABytes + S::kBBytes), b = a + S::kABytes;
                             const uint64_t da = operand<kAcrossA>(a), db = operand<kAcrossB>(b);
+                            if (elect_one()) {
 #pragma unroll
-                            for (int q = 0; q < kDepth / 16; ++q)
-                                mma_pair(d, da + q * (kStep<kAcrossA> >> 4), db + q * (kStep<kAcrossB> >> 4), kIdesc, k != begin || q != 0);
-                            commit_pair(empty(ring.stage));
+                                for (int q = 0; q < kDepth / 16; ++q)
+                                    mma_pair(d, da + q * (kStep<kAcrossA> >> 4), db + q * (kStep<kAcrossB> >> 4), kIdesc, k != begin || q != 0);
+                                commit_pair(empty(ring.stage));
+                            }
+                            __syncwarp();
                             ring.next();
                         }
                     }
                     if (!ok) break;
-                    commit_pair(ready(half.stage));
+                    if (elect_one()) commit_pair(ready(half.stage));
+                    __syncwarp();
                     half.next();
                     begin = stop;
                 }
             }
         }
-        __syncwarp();
     } else {
         // ---- epilogue: a quarter of TMEM's lanes (the warp's number modulo 4) and every second chunk of 64 output columns
         const uint32_t quarter = warp % 4, turn = (warp - 2) / 4;
