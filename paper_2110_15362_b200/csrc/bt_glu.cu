@@ -306,7 +306,20 @@ int bt_glu_fwd(const void *x, uint64_t rows, uint64_t d_in, uint64_t d_ff, int d
     c.rows = rows, c.d_in = d_in, c.d_ff = d_ff, c.dtype = dtype, c.act = activation, c.dev_status = dev_status;
     if (bt::glu_rows_takes(rows, d_in, dtype)) return bt::launch_glu_rows(c, s) == cudaSuccess ? BT_OK : BT_ERR_CUDA;
     c.scratch = workspace;
-    if (bt::glu_mma_takes(d_in, d_ff, dtype)) return bt::launch_glu_mma_fwd(c, s) == cudaSuccess ? BT_OK : BT_ERR_CUDA;
+    if (bt::glu_mma_takes(d_in, d_ff, dtype)) {
+        const uint64_t tail = bt::glu_mma_tail(c);
+        if (tail != 0) {
+            bt::GluCall    last = c;
+            const uint64_t es = static_cast<uint64_t>(bt::element_size(dtype)), from = (rows - tail) * es;
+            const auto     at = [](void *p, uint64_t bytes) { return p ? static_cast<void *>(static_cast<unsigned char *>(p) + bytes) : nullptr; };
+            last.x    = static_cast<const unsigned char *>(x) + from * d_in;
+            last.h    = at(h, from * d_ff), last.g = at(g_out, from * d_ff), last.u = at(u_out, from * d_ff);
+            last.rows = tail;
+            c.rows    = rows - tail;
+            if (bt::launch_glu_rows(last, s) != cudaSuccess) return BT_ERR_CUDA;
+        }
+        return bt::launch_glu_mma_fwd(c, s) == cudaSuccess ? BT_OK : BT_ERR_CUDA;
+    }
     return bt::dispatch(dtype, [&](auto dt) { return bt::forward_of<decltype(dt)::value>(c, s); });
 }
 

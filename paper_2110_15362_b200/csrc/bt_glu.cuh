@@ -100,6 +100,7 @@ inline size_t glu_plane_bytes(uint64_t n) { return (n * 6 + 255) / 256 * 256; }
 bool        glu_mma_takes(uint64_t d_in, uint64_t d_ff, int dtype);
 size_t      glu_mma_scratch(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, bool backward);
 cudaError_t launch_glu_mma_fwd(const GluCall &c, cudaStream_t stream);
+uint64_t    glu_mma_tail(const GluCall &c);    // rows at the end that a forward pass leaves to launch_glu_rows
 cudaError_t launch_glu_mma_bwd(const GluCall &c, cudaStream_t stream);
 
 // The forward pass for few rows (bt_glu_rows.cu).

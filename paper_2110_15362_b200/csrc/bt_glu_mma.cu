@@ -271,27 +271,13 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
 
     const uint32_t warp = __shfl_sync(0xFFFFFFFFu, threadIdx.x / 32, 0), lane = threadIdx.x % 32, rank = cluster_rank();
     const Waits    wait{gave_up, p.dev_status};
-    if (threadIdx.x == 0) {
-        uint64_t *const b = reinterpret_cast<uint64_t *>(generic + S::kBytes);
-        for (int s = 0; s < 2 * kStages; ++s) mbar_init(b + s, 1);
-        mbar_init(b + 2 * kStages, 1), mbar_init(b + 2 * kStages + 1, 1);
-        mbar_init(b + 2 * kStages + 2, 2 * kEpiWarps), mbar_init(b + 2 * kStages + 3, 2 * kEpiWarps);
-        *gave_up = 0;
+    if (warp == 1) {                                                    // a barrier per lane
+        if (lane < 2 * kStages + 4) mbar_init(reinterpret_cast<uint64_t *>(generic + S::kBytes) + lane, lane < 2 * kStages + 2 ? 1 : 2 * kEpiWarps);
+        if (lane == 31) *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 0 && lane < 7) prefetch_map(lane < 2 ? &p.a[lane] : lane < 4 ? &p.b[lane - 2] : &p.out[lane - 4]);
-    if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_word)), "r"(2 * kSums) : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-    }
-    tmem_fence_before();
-    __syncthreads();
-    cluster_sync();
-    tmem_fence_after();
-    const uint32_t tmem = *tmem_word;
-    in_stream_order();
-    if (p.dev_status && kUse == kForward && blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<volatile int32_t *>(p.dev_status) = BT_OK;
-
+    // the first unit's place is worked out while the barriers are set up
     const uint32_t first = blockIdx.x / 2, step = gridDim.x / 2;
     const uint32_t blocks = p.blocks * (kUse == kInputGrad ? 2 : 1);
     const bool     split  = kUse == kInputGrad && p.splits > 1;
@@ -301,16 +287,43 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
         const uint32_t end = from_block(t) + p.split_blocks;
         return split && end < blocks ? end : blocks;
     };
+    struct Unit {
+        Tile     tile;
+        uint32_t begin, end;
+    };
+    const auto unit_at = [&](const uint32_t t) {
+        Unit u;
+        if (t < p.tiles) u.tile = tile_at(p, split ? t / p.splits : t), u.begin = from_block(t), u.end = end_block(t);
+        return u;
+    };
+    const Unit first_unit = unit_at(first);
+    __syncwarp();
+    cluster_sync();
+    in_stream_order();
+    if (p.dev_status && kUse == kForward && blockIdx.x == 0 && threadIdx.x == 0) *reinterpret_cast<volatile int32_t *>(p.dev_status) = BT_OK;
+
+    uint32_t tmem = 0;
+    if (warp != 0) {
+        // TMEM for the issuer and the epilogue; the loader has begun
+        if (warp == 1) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(tmem_word)), "r"(2 * kSums) : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
+        tmem_fence_before();
+        asm volatile("barrier.cta.sync 1, %0;" ::"n"(kThreads - 32) : "memory");
+        tmem_fence_after();
+        tmem = *tmem_word;
+    }
     if (warp == 0) {
         // ---- loader
         Ring<kStages>  ring;
         bool           ok          = true;
         const uint32_t leader_bars = in_first_cta(full(0));
-        for (uint32_t t = first; t < p.tiles && ok; t += step) {
-            const Tile     tile = tile_at(p, split ? t / p.splits : t);
-            const int      i0   = static_cast<int>(tile.i * 256 + rank * kRows);
-            const uint32_t end  = end_block(t);
-            for (uint32_t k = from_block(t); k < end && ok; ++k) {
+        Unit           unit        = first_unit;
+        for (uint32_t t = first; t < p.tiles && ok; t += step, unit = unit_at(t)) {
+            const Tile tile = unit.tile;
+            const int  i0   = static_cast<int>(tile.i * 256 + rank * kRows);
+            for (uint32_t k = unit.begin; k < unit.end && ok; ++k) {
                 const uint32_t pair = kUse == kInputGrad ? (k >= p.blocks ? 1u : 0u) : 0u;
                 const int      k0   = static_cast<int>((k - pair * p.blocks) * kDepth);
 #pragma unroll
@@ -355,10 +368,11 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
             Ring<kStages> ring;
             Ring<2>       half;
             bool          ok = true;
-            for (uint32_t t = first; t < p.tiles && ok; t += step) {
-                const uint32_t end = end_block(t);
+            Unit          unit = first_unit;
+            for (uint32_t t = first; t < p.tiles && ok; t += step, unit = unit_at(t)) {
+                const uint32_t end = unit.end;
                 // binary32: a chunk of blocks at a time; else all of them
-                for (uint32_t begin = from_block(t); begin < end && ok;) {
+                for (uint32_t begin = unit.begin; begin < end && ok;) {
                     const uint32_t stop = DT == BT_F32 && begin + kChunk < end ? begin + kChunk : end;
                     if (!(ok = wait(taken(half.stage), half.phase ^ 1))) break;
                     tmem_fence_after();
@@ -415,18 +429,20 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
     } else {
         // ---- epilogue: a quarter of TMEM's lanes (the warp's number modulo 4) and every second chunk of 64 output columns
         const uint32_t quarter = warp % 4, turn = (warp - 2) / 4;
-        // a row of 128 bytes per lane to the staged tile, in the pieces' swizzled places, and the tile out
-        const auto stage_out = [&](const uint32_t (&packed)[32], const CUtensorMap *map, const uint32_t j0, const uint32_t i0) {
+        // a row of 128 bytes per lane to the staged tile, in the pieces' swizzled places, and the tile out.  (Two staged tiles per
+        // warp cost a stage of the ring: 768 x 1000 x 2728 the same, 1024 x 2048 x 8192 4 % slower.)
+        const uint32_t at        = S::kRing + (warp - 2) * kStageWords;
+        const auto     stage_out = [&](const uint32_t (&packed)[32], const CUtensorMap *map, const uint32_t j0, const uint32_t i0) {
             if (lane == 0) bulk_wait_read<0>();                         // the tile of before has been read
             __syncwarp();
 #pragma unroll
             for (int c = 0; c < 8; ++c)
-                *reinterpret_cast<uint4 *>(generic + S::kRing + (warp - 2) * kStageWords + lane * 128 + ((c ^ (lane & 7)) * 16)) =
+                *reinterpret_cast<uint4 *>(generic + at + lane * 128 + ((c ^ (lane & 7)) * 16)) =
                     make_uint4(packed[4 * c], packed[4 * c + 1], packed[4 * c + 2], packed[4 * c + 3]);
             fence_proxy_async();
             __syncwarp();
             if (lane == 0) {
-                tma_store(map, static_cast<int>(j0), static_cast<int>(i0), base + S::kRing + (warp - 2) * kStageWords);
+                tma_store(map, static_cast<int>(j0), static_cast<int>(i0), base + at);
                 bulk_commit();
             }
         };
@@ -436,13 +452,14 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
         if constexpr (DT == BT_F32) {
             // 64 columns of the tile per warp, in registers from chunk to chunk: forward 32 of g and 32 of u, else the `turn`th 64
             bool ok = true;
-            for (uint32_t t = first; t < p.tiles && ok; t += step) {
-                const Tile     tile = tile_at(p, split ? t / p.splits : t);
-                const uint32_t i0   = tile.i * 256 + rank * kRows + quarter * 32, end = end_block(t);
+            Unit unit = first_unit;
+            for (uint32_t t = first; t < p.tiles && ok; t += step, unit = unit_at(t)) {
+                const Tile     tile = unit.tile;
+                const uint32_t i0   = tile.i * 256 + rank * kRows + quarter * 32, end = unit.end;
                 uint32_t       sum[2][32];
 #pragma unroll
                 for (int c = 0; c < 32; ++c) sum[0][c] = sum[1][c] = 0;
-                for (uint32_t begin = from_block(t); begin < end; begin += kChunk) {
+                for (uint32_t begin = unit.begin; begin < end; begin += kChunk) {
                     if (!(ok = wait(ready(half.stage), half.phase))) break;
                     tmem_fence_after();
                     const uint32_t from = tmem + half.stage * kSums + (quarter * 32 << 16);
@@ -495,9 +512,10 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
                     }
                 }
             }
-        } else
-        for (uint32_t t = first; t < p.tiles; t += step) {
-            const Tile tile = tile_at(p, split ? t / p.splits : t);
+        }
+        Unit unit = first_unit;
+        for (uint32_t t = first; DT != BT_F32 && t < p.tiles; t += step, unit = unit_at(t)) {
+            const Tile     tile = unit.tile;
             const uint32_t i0 = tile.i * 256 + rank * kRows + quarter * 32;
             if (!wait(ready(half.stage), half.phase)) break;
             tmem_fence_after();
@@ -707,12 +725,11 @@ bool set_tiles(MmaArgs &p, uint64_t size_i, uint64_t size_j, uint32_t columns, u
     return tiles < 0x7FFFFFFFull;
 }
 
-// How long `units` tiles of `blocks` blocks of 64 summed elements take, in ns.  A block of a 256 x 256 tile is 512 cycles of the
-// tensor cores and 64 KB from the L2, one of a 256 x 128 tile half of the former and three quarters of the latter: 280
-// and 208 ns where few pairs of CTAs run (a CTA reads 64 bytes a cycle), and more where the L2's 10.5 TB/s are shared by many.
+// How long `units` tiles of `blocks` blocks of 64 summed elements take, in ns: the tensor cores' time where few pairs of CTAs
+// run, more where the L2 is shared by many (measured: a block of a 256 x 256 tile 280 to 400 ns, of a 256 x 128 tile 150 to 207).
 double tiles_ns(uint64_t units, uint64_t blocks, uint32_t columns, uint64_t pairs)
 {
-    const double alone = columns == 256 ? 280 : 208, shared = columns == 256 ? 6.24 : 4.68;
+    const double alone = columns == 256 ? 280 : 150, shared = columns == 256 ? 5.4 : 2.8;
     const auto   block = [&](uint64_t active) { return alone > shared * static_cast<double>(active) ? alone : shared * static_cast<double>(active); };
     double       ns    = static_cast<double>(units / pairs) * block(pairs);
     if (units % pairs) ns += block(units % pairs);
@@ -740,8 +757,8 @@ cudaError_t forward_of(const GluCall &c, int sms, cudaStream_t stream)
     return with_act<DT>(c.act, [&](auto dt, auto act) { return start<decltype(dt)::value, kForward, decltype(act)::value, kN>(p, stream, sms); });
 }
 
-// How the input gradient is computed: columns of a tile and units per tile.  Units cost the store of their sums (1 us where
-// a pair of CTAs ends), a second launch (2 us) and 87 ns per 256 KB of sums that go out and in.
+// How the input gradient is computed: columns of a tile and units per tile.  Units cost a second launch and the store of the
+// last sums (3 us), and 30 ns per 128 KB of sums that go out and in.
 struct SplitPlan {
     uint32_t columns, splits, split_blocks;
     uint64_t tiles;
@@ -759,7 +776,7 @@ SplitPlan input_grad_plan(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype
             const uint64_t each = round_up_div(blocks, splits);
             if (round_up_div(blocks, each) != splits) continue;         // (a unit would be empty)
             double cost = tiles_ns(tiles * splits, each * each_block, columns, pairs);
-            if (splits > 1) cost += 3000 + static_cast<double>(tiles * splits) * 87 * (columns / 256.0);
+            if (splits > 1) cost += 3000 + static_cast<double>(tiles * splits) * 30 * (columns / 128.0);
             if (least == 0 || cost < least) least = cost, best = SplitPlan{columns, splits, static_cast<uint32_t>(each), tiles};
         }
     }
@@ -834,6 +851,25 @@ size_t glu_mma_scratch(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, b
     const int    sms  = sm_count();
     const size_t sums = backward ? partial_bytes(input_grad_plan(rows, d_in, d_ff, dtype, sms ? sms : 148)) : 0;
     return dtype == BT_F32 ? glu_plane_bytes(rows * d_in) + 2 * glu_plane_bytes(d_ff * d_in) + sums : sums;
+}
+
+// A last tile of a few rows costs a round of whole tiles where the tiles before it fill the pairs of CTAs; the kernel for few rows
+// then does it in the time of a launch and of the weights, which the L2 holds (fp16 777 x 1000 x 2728: 22 us in tiles, 17
+// with the nine last rows on their own).
+uint64_t glu_mma_tail(const GluCall &c)
+{
+    const uint64_t tail = c.rows % 256, main = c.rows - tail;
+    const int      sms  = sm_count();
+    if (c.dtype == BT_F32 || main == 0 || tail == 0 || tail > 16 || sms < 2) return 0;
+    const uint64_t pairs = static_cast<uint64_t>(sms) / 2, blocks = round_up_div(c.d_in, kDepth);
+    const auto     best = [&](uint64_t rows) {
+        const double wide = tiles_ns(round_up_div(rows, 256) * round_up_div(c.d_ff, 128), blocks, 256, pairs);
+        const double slim = tiles_ns(round_up_div(rows, 256) * round_up_div(c.d_ff, 64), blocks, 128, pairs);
+        return wide < slim ? wide : slim;
+    };
+    // (rows that do not begin on 32 bytes: five sectors in place of four, measured 1.3 times the time)
+    const double slower = c.d_in % 16 ? 1.3 : 1.0;
+    return (best(c.rows) - best(main)) * slower > 2500 + static_cast<double>(4 * c.d_ff * c.d_in) / 8000 ? tail : 0;
 }
 
 cudaError_t launch_glu_mma_fwd(const GluCall &call, cudaStream_t stream)

@@ -91,6 +91,13 @@ def test_few_rows(rows, d, ff, kind):
     check_forward(x, wg, wu, act, kind, forward(x, wg, wu, act, save=False))
 
 
+@pytest.mark.parametrize("kind", ["f16", "bf16"])
+@pytest.mark.parametrize("size", [(777, 1000, 2728), (785, 1000, 2728), (1025, 264, 4744), (769, 2048, 3000)])
+def test_a_few_rows_behind_whole_tiles(size, kind):
+    x, wg, wu = make(*size, kind, seed=2)
+    check_forward(x, wg, wu, "relu", kind, forward(x, wg, wu, "relu"))
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("kind", KINDS)
 def test_activations(act, kind):
