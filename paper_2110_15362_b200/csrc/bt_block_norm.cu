@@ -323,10 +323,9 @@ __device__ __forceinline__ bool whole_group(const NormArgs &a, const Chunk &c, c
     return begin >= c.first && end <= c.end;
 }
 
-// ---------------------------------------------------------------------------------------------- rows of whole vectors
-// A CTA per row, kHold 16-byte vectors of every operand per thread, and a ring of rows in shared memory that each thread fills
-// for itself with asynchronous copies, several rows ahead: what a thread reads it has copied, so the ring needs no barrier.
-// The work on consecutive rows overlaps, so that one barrier per row serves all its sums: while a row's sums meet, the next
+// ---------------------------------------------------------------------------------------------- rows through a ring
+// A CTA per row, and a ring of rows in shared memory, filled by asynchronous copies several rows ahead (RowRing).  The work on
+// consecutive rows overlaps, so that one barrier per row serves all its sums: while a row's sums meet, the next
 // row's are taken and the outputs of the one before are written.
 __device__ __forceinline__ void copy_ahead(void *to, const void *from)
 {
@@ -380,111 +379,231 @@ __device__ __forceinline__ A cta_sum(const A *part, const uint32_t warps)
     return warp_sum(lane < warps ? part[lane] : A(0));
 }
 
-// rows of the ring
-template <int kHold>
-constexpr uint32_t kRingStages = kHold == 1 ? 5 : 3;
+// rows of the ring (rows that are copied by all: one more, see RowRing)
+template <int kHold, bool kVector>
+constexpr uint32_t kRingStages = !kVector ? 4 : kHold == 1 ? 5 : 3;
 
-template <int DT>
-__device__ __forceinline__ void read_pairs(const void *row, const uint32_t i, Two<typename Num<DT>::Acc> (&v)[kPairs<DT>])
-{
-    widen_pairs<DT>(__ldg(static_cast<const uint4 *>(row) + i), v);
-}
+// What a thread holds of a row, two columns at a time: kHold times kP pairs.  kVector: kHold vectors of 16 bytes, `team` vectors
+// apart; else kHold times eight single columns, `team` columns apart (rows that do not all begin on a 16-byte boundary).
+template <int DT, int kHold, bool kVector>
+struct Columns {
+    using Elem               = typename Num<DT>::Elem;
+    using Acc                = typename Num<DT>::Acc;
+    using Pair               = Two<Acc>;
+    static constexpr int kP  = kVector ? kPairs<DT> : 4;
+    static constexpr int kES = static_cast<int>(sizeof(Elem));
+    uint32_t t, team, d;
+
+    // the column of half `h` of pair k of hold j
+    __device__ __forceinline__ uint32_t column(const int j, const int k, const int h) const
+    {
+        return kVector ? (j * team + t) * (2 * kP) + 2 * k + h : ((j * kP + k) * 2 + h) * team + t;
+    }
+    __device__ __forceinline__ bool has(const int j, const int k, const int h) const { return column(j, k, h) < d; }
+    __device__ __forceinline__ void fill(Pair (&v)[kP], const Acc with) const
+    {
+#pragma unroll
+        for (int k = 0; k < kP; ++k) v[k] = both(with);
+    }
+    // a row of global memory that no output of the call overlaps; columns beyond it keep what v holds
+    __device__ __forceinline__ void read(const Elem *row, const int j, Pair (&v)[kP]) const
+    {
+        if constexpr (kVector) {
+            if (has(j, 0, 0)) widen_pairs<DT>(__ldg(reinterpret_cast<const uint4 *>(row) + j * team + t), v);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kP; ++k)
+                v[k] = Pair::of(has(j, k, 0) ? static_cast<Acc>(Num<DT>::widen(row[column(j, k, 0)])) : v[k].low(),
+                                has(j, k, 1) ? static_cast<Acc>(Num<DT>::widen(row[column(j, k, 1)])) : v[k].high());
+        }
+    }
+    __device__ __forceinline__ void write(Elem *row, const int j, const Pair (&v)[kP], const Extent &all) const
+    {
+        if constexpr (kVector) {
+            uint4 *const o = reinterpret_cast<uint4 *>(row) + j * team + t;
+            if (has(j, 0, 0) && all.holds(o, 16)) *o = narrow_pairs<DT>(v);
+        } else {
+#pragma unroll
+            for (int k = 0; k < kP; ++k) {
+                Elem *const lo = row + column(j, k, 0), *const hi = row + column(j, k, 1);
+                if (has(j, k, 0) && all.holds(lo, kES)) *lo = Num<DT>::narrow(v[k].low());
+                if (has(j, k, 1) && all.holds(hi, kES)) *hi = Num<DT>::narrow(v[k].high());
+            }
+        }
+    }
+    // partial sums, in the sums' type
+    __device__ __forceinline__ void write_sums(Acc *row, const int j, const Pair (&v)[kP], const Extent &all) const
+    {
+#pragma unroll
+        for (int k = 0; k < kP; ++k) {
+            Acc *const lo = row + column(j, k, 0), *const hi = row + column(j, k, 1);
+            if (has(j, k, 0) && all.holds(lo, sizeof(Acc))) *lo = v[k].low();
+            if (has(j, k, 1) && all.holds(hi, sizeof(Acc))) *hi = v[k].high();
+        }
+    }
+};
+
+// The ring of rows in shared memory: `stages` rows of kOperands operands.
+// kVector: every thread copies the very vectors that it reads, and needs no barrier for them.  Else a row's bytes are copied from the
+// 16-byte boundary before it to the one behind it, by the CTA together: what a thread reads others have copied, so
+// that a row is waited for in front of the barrier before its use.
+template <int DT, int kHold, bool kVector, int kOperands>
+struct RowRing {
+    using C                          = Columns<DT, kHold, kVector>;
+    using Elem                       = typename C::Elem;
+    using Pair                       = typename C::Pair;
+    static constexpr uint32_t stages = kRingStages<kHold, kVector>;
+    // copies of later rows that may be under way when a turn begins (kVector), or when the barrier before it is reached
+    static constexpr int kBehind = static_cast<int>(stages) - (kVector ? 2 : 3);
+    const C        &c;
+    unsigned char  *at;
+    uint32_t        slot_bytes;
+
+    __device__ __forceinline__ RowRing(const C &columns, void *shared, const uint32_t bytes) : c(columns), at(static_cast<unsigned char *>(shared)), slot_bytes(bytes) {}
+    __device__ __forceinline__ uint4 &vector(const uint32_t stage, const int o, const int j) const
+    {
+        return reinterpret_cast<uint4 *>(at)[((stage * kOperands + o) * kHold + j) * c.team + c.t];
+    }
+    // columns beyond the row, and operands that the call leaves out, are zeros (kVector: in the ring, once)
+    __device__ __forceinline__ void clear(const bool (&present)[kOperands]) const
+    {
+        if constexpr (kVector)
+            for (uint32_t s = 0; s < stages; ++s)
+#pragma unroll
+                for (int j = 0; j < kHold; ++j)
+#pragma unroll
+                    for (int o = 0; o < kOperands; ++o)
+                        if (!c.has(j, 0, 0) || !present[o]) vector(s, o, j) = make_uint4(0, 0, 0, 0);
+    }
+    // row `row` of a tensor that ends `total` elements behind its base
+    __device__ __forceinline__ void copy(const uint32_t stage, const int o, const void *base, const uint64_t row, const uint64_t total) const
+    {
+        if constexpr (kVector) {
+            const uint4 *const from = reinterpret_cast<const uint4 *>(static_cast<const unsigned char *>(base) + row * c.d * C::kES) + c.t;
+#pragma unroll
+            for (int j = 0; j < kHold; ++j)
+                if (c.has(j, 0, 0)) copy_ahead(&vector(stage, o, j), from + j * c.team);
+        } else {
+            const uint64_t begin = row * c.d * C::kES, end = begin + c.d * C::kES, all = total * C::kES;
+            unsigned char *const to = at + (stage * kOperands + o) * slot_bytes;
+            for (uint64_t b = (begin & ~15ull) + 16 * c.t; b < end; b += 16 * c.team) {
+                const uint32_t size = b + 16 <= all ? 16u : static_cast<uint32_t>(all - b);      // nothing is read behind the tensor
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr(to + (b - (begin & ~15ull)))),
+                             "l"(static_cast<const unsigned char *>(base) + b), "r"(size)
+                             : "memory");
+            }
+        }
+    }
+    // what this thread holds of an operand's row (`row`: its number in its tensor)
+    __device__ __forceinline__ void read(const uint32_t stage, const int o, const int j, const uint64_t row, const bool present, Pair (&v)[C::kP]) const
+    {
+        if constexpr (kVector) {
+            widen_pairs<DT>(vector(stage, o, j), v);
+        } else {
+            if (!present) {
+                c.fill(v, 0);
+                return;
+            }
+            const Elem *const from = reinterpret_cast<const Elem *>(at + (stage * kOperands + o) * slot_bytes + (row * c.d * C::kES & 15u));
+#pragma unroll
+            for (int k = 0; k < C::kP; ++k)
+                v[k] = Pair::of(c.has(j, k, 0) ? static_cast<typename C::Acc>(Num<DT>::widen(from[c.column(j, k, 0)])) : typename C::Acc(0),
+                                c.has(j, k, 1) ? static_cast<typename C::Acc>(Num<DT>::widen(from[c.column(j, k, 1)])) : typename C::Acc(0));
+        }
+    }
+};
 
 // scale * gate * w_post of a thread's columns (kRowGate: without the gate, which changes from row to row)
-template <int DT, int kHold, bool kRowGate>
-__device__ __forceinline__ void branch_factors(const NormArgs &a, const uint64_t group, const uint32_t count,
-                                               Two<typename Num<DT>::Acc> (&gw)[kHold][kPairs<DT>])
+template <int DT, int kHold, bool kVector, bool kRowGate>
+__device__ __forceinline__ void branch_factors(const NormArgs &a, const uint64_t group, const Columns<DT, kHold, kVector> &c,
+                                               Two<typename Num<DT>::Acc> (&gw)[kHold][Columns<DT, kHold, kVector>::kP])
 {
-    using Acc = typename Num<DT>::Acc;
+    using C    = Columns<DT, kHold, kVector>;
+    using Elem = typename C::Elem;
 #pragma unroll
     for (int j = 0; j < kHold; ++j) {
-        const uint32_t i = j * blockDim.x + threadIdx.x;
-#pragma unroll
-        for (int k = 0; k < kPairs<DT>; ++k) gw[j][k] = both(static_cast<Acc>(a.scale));
-        if (i >= count) continue;
-        Two<Acc> w[kPairs<DT>];
+        typename C::Pair w[C::kP];
+        c.fill(gw[j], static_cast<typename C::Acc>(a.scale));
         if (a.w_post) {
-            read_pairs<DT>(a.w_post, i, w);
+            c.fill(w, 1);
+            c.read(static_cast<const Elem *>(a.w_post), j, w);
 #pragma unroll
-            for (int k = 0; k < kPairs<DT>; ++k) gw[j][k] = gw[j][k] * w[k];
+            for (int k = 0; k < C::kP; ++k) gw[j][k] = gw[j][k] * w[k];
         }
         if (!kRowGate && a.gate) {
-            read_pairs<DT>(row_of<typename Num<DT>::Elem>(a.gate, group, a.d), i, w);
+            c.fill(w, 1);
+            c.read(static_cast<const Elem *>(a.gate) + group * a.d, j, w);
 #pragma unroll
-            for (int k = 0; k < kPairs<DT>; ++k) gw[j][k] = gw[j][k] * w[k];
+            for (int k = 0; k < C::kP; ++k) gw[j][k] = gw[j][k] * w[k];
         }
     }
 }
 
 // Forward.  In one turn of the loop: the sum of f^2 of a row, x' and its sum of the row before, n of the row before that.
 // kRowGate: the gate changes from row to row and comes through the ring like a third operand.
-template <int DT, int kHold, bool kRowGate>
+template <int DT, int kHold, bool kVector, bool kRowGate>
 __global__ void __launch_bounds__(kMaxTeam, 1)
-block_norm_fwd_ring_kernel(const NormArgs a)
+block_norm_fwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
 {
     in_stream_order();
-    using Elem               = typename Num<DT>::Elem;
-    using Acc                = typename Num<DT>::Acc;
-    constexpr int      kP    = kPairs<DT>;
-    constexpr int      kOperands = kRowGate ? 3 : 2;
-    constexpr uint32_t stages    = kRingStages<kHold>;
-    extern __shared__ uint4 ring[];                                    // [stage][operand][hold][thread]
+    using C    = Columns<DT, kHold, kVector>;
+    using Elem = typename C::Elem;
+    using Acc  = typename C::Acc;
+    using Pair = typename C::Pair;
+    constexpr int kP = C::kP, kOperands = kRowGate ? 3 : 2;
+    using Ring = RowRing<DT, kHold, kVector, kOperands>;
+    extern __shared__ uint4 shared[];
     __shared__ Acc part[2][2][kMaxWarps];                              // [turn][of f, of x'][warp]
-    const uint32_t t = threadIdx.x, team = blockDim.x, warps = team / 32;
-    const uint32_t count = static_cast<uint32_t>(a.d / kLanes<DT>);
+    const uint32_t t = threadIdx.x, warps = blockDim.x / 32;
+    const C        c{t, blockDim.x, static_cast<uint32_t>(a.d)};
+    const Ring     ring(c, shared, slot_bytes);
     const Acc      eps = static_cast<Acc>(a.eps), of_d = Acc(1) / static_cast<Acc>(a.d);
-    const Extent   all_x = extent_of(a.x_out, a.rows * a.d * sizeof(Elem)), all_n = extent_of(a.n_out, a.rows * a.d * sizeof(Elem));
+    const uint64_t total = a.rows * a.d;
+    const Extent   all_x = extent_of(a.x_out, total * sizeof(Elem)), all_n = extent_of(a.n_out, total * sizeof(Elem));
 
-    const auto slot = [&](const uint32_t stage, const int operand, const int j) -> uint4 & {
-        return ring[((stage * kOperands + operand) * kHold + j) * team + t];
-    };
-    // the row to copy next, and where its vectors and those of the two rows that are written begin
-    const uint64_t stride = static_cast<uint64_t>(gridDim.x) * count;
-    uint64_t       next = blockIdx.x, at_next = next * count + t, at_y = at_next, at_n = at_next;
+    uint64_t next = blockIdx.x;                                        // the row to copy next
     // (a commit for every turn, also behind the last row: the waits count groups)
     const auto fill = [&](const uint32_t stage) {
         if (next < a.rows) {
-            const uint4 *const x = static_cast<const uint4 *>(a.x) + at_next, *const f = static_cast<const uint4 *>(a.f) + at_next;
-#pragma unroll
-            for (int j = 0; j < kHold; ++j)
-                if (j * team + t < count) {
-                    copy_ahead(&slot(stage, 0, j), x + j * team);
-                    if (a.f) copy_ahead(&slot(stage, 1, j), f + j * team);
-                    if constexpr (kRowGate) copy_ahead(&slot(stage, 2, j), static_cast<const uint4 *>(a.gate) + next / a.gate_rows * count + j * team + t);
-                }
-            next += gridDim.x, at_next += stride;
+            ring.copy(stage, 0, a.x, next, total);
+            if (a.f) ring.copy(stage, 1, a.f, next, total);
+            if constexpr (kRowGate) ring.copy(stage, 2, a.gate, next / a.gate_rows, round_up_div(a.rows, a.gate_rows) * a.d);
+            next += gridDim.x;
         }
         copy_commit();
     };
-#pragma unroll
-    for (int j = 0; j < kHold; ++j)
-        for (uint32_t s = 0; s < stages; ++s)                          // columns beyond the row, and an f left out, are zeros
-#pragma unroll
-            for (int o = 0; o < kOperands; ++o)
-                if (j * team + t >= count || (o == 1 && !a.f)) slot(s, o, j) = make_uint4(0, 0, 0, 0);
-    for (uint32_t s = 0; s + 1 < stages; ++s) fill(s);
+    bool present[kOperands];
+    present[0] = true, present[1] = a.f != nullptr;
+    if constexpr (kRowGate) present[2] = true;
+    ring.clear(present);
+    for (uint32_t s = 0; s + 1 < Ring::stages; ++s) fill(s);
 
-    Two<Acc> gw[kHold][kP], w_pre[kHold][kP], y[kHold][kP];
-    branch_factors<DT, kHold, kRowGate>(a, 0, count, gw);
+    Pair gw[kHold][kP], w_pre[kHold][kP], y[kHold][kP];
+    branch_factors<DT, kHold, kVector, kRowGate>(a, 0, c, gw);
 #pragma unroll
     for (int j = 0; j < kHold; ++j) {
-#pragma unroll
-        for (int k = 0; k < kP; ++k) w_pre[j][k] = both(Acc(1));
-        if (a.w_pre && j * team + t < count) read_pairs<DT>(a.w_pre, j * team + t, w_pre[j]);
+        c.fill(w_pre[j], 1);
+        if (a.w_pre) c.read(static_cast<const Elem *>(a.w_pre), j, w_pre[j]);
+    }
+    if constexpr (!kVector) {                                          // the first row, copied by all
+        copy_wait<Ring::kBehind + 1>();
+        __syncthreads();
     }
     const uint64_t mine = (a.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;      // rows of this CTA (the grid is not wider than the rows)
-    uint32_t       stage_a = 0, stage_b = 0, stage_c = stages - 1;
-    for (uint64_t turn = 0; turn < mine + 2; ++turn) {
+    const uint64_t stride = static_cast<uint64_t>(gridDim.x) * a.d;
+    uint64_t       row = blockIdx.x, at_y = row * a.d, at_n = at_y;    // of the turn; where the rows written next begin
+    uint32_t       stage_a = 0, stage_b = 0, stage_c = Ring::stages - 1;
+    for (uint64_t turn = 0; turn < mine + 2; ++turn, row += gridDim.x) {
         const Acc(*const before)[kMaxWarps] = part[(turn & 1) ^ 1];
         Acc(*const now)[kMaxWarps]          = part[turn & 1];
         if (turn < mine) {
-            copy_wait<static_cast<int>(stages) - 2>();                 // (stages - 1 rows and one more per turn so far are on their way)
+            if constexpr (kVector) copy_wait<Ring::kBehind>();
             if (a.w_post) {
-                Two<Acc> s = both(Acc(0));
+                Pair s = both(Acc(0));
 #pragma unroll
                 for (int j = 0; j < kHold; ++j) {
-                    Two<Acc> f[kP];
-                    widen_pairs<DT>(slot(stage_a, 1, j), f);
+                    Pair f[kP];
+                    ring.read(stage_a, 1, j, row, true, f);
 #pragma unroll
                     for (int k = 0; k < kP; ++k) s = fma2(f[k], f[k], s);
                 }
@@ -494,34 +613,29 @@ block_norm_fwd_ring_kernel(const NormArgs a)
         }
         if (turn >= 2 && a.n_out) {
             // ---- n of the row two before, whose x' waits in y
-            const Two<Acc> r   = both(root_of(cta_sum(before[1], warps) * of_d + eps));
-            uint4 *const   out = static_cast<uint4 *>(a.n_out) + at_n;
-            at_n += stride;
+            const Pair r = both(root_of(cta_sum(before[1], warps) * of_d + eps));
 #pragma unroll
             for (int j = 0; j < kHold; ++j) {
-                const uint32_t i = j * team + t;
-                if (i >= count) continue;
-                Two<Acc> n[kP];
+                Pair n[kP];
 #pragma unroll
                 for (int k = 0; k < kP; ++k) n[k] = y[j][k] * r * w_pre[j][k];
-                if (all_n.holds(out + j * team, 16)) out[j * team] = narrow_pairs<DT>(n);
+                c.write(static_cast<Elem *>(a.n_out) + at_n, j, n, all_n);
             }
+            at_n += stride;
         }
         if (turn >= 1 && turn <= mine) {
             // ---- x' of the row before
-            const Two<Acc> rf  = both(a.w_post ? root_of(cta_sum(before[0], warps) * of_d + eps) : Acc(1));
-            uint4 *const   out = static_cast<uint4 *>(a.x_out) + at_y;
-            at_y += stride;
-            Two<Acc>       s   = both(Acc(0));
+            const uint64_t before_row = row - gridDim.x;
+            const Pair     rf = both(a.w_post ? root_of(cta_sum(before[0], warps) * of_d + eps) : Acc(1));
+            Pair           s  = both(Acc(0));
 #pragma unroll
             for (int j = 0; j < kHold; ++j) {
-                const uint32_t i = j * team + t;
-                Two<Acc>       f[kP];
-                widen_pairs<DT>(slot(stage_b, 0, j), y[j]);
-                widen_pairs<DT>(slot(stage_b, 1, j), f);
+                Pair f[kP];
+                ring.read(stage_b, 0, j, before_row, true, y[j]);
+                ring.read(stage_b, 1, j, before_row, a.f != nullptr, f);
                 if constexpr (kRowGate) {
-                    Two<Acc> g[kP];
-                    widen_pairs<DT>(slot(stage_b, 2, j), g);
+                    Pair g[kP];
+                    ring.read(stage_b, 2, j, before_row / a.gate_rows, true, g);
 #pragma unroll
                     for (int k = 0; k < kP; ++k) f[k] = f[k] * g[k];
                 }
@@ -530,113 +644,110 @@ block_norm_fwd_ring_kernel(const NormArgs a)
                     y[j][k] = fma2(f[k] * rf, gw[j][k], y[j][k]);
                     s       = fma2(y[j][k], y[j][k], s);
                 }
-                if (a.x_out && i < count && all_x.holds(out + j * team, 16)) out[j * team] = narrow_pairs<DT>(y[j]);
+                if (a.x_out) c.write(static_cast<Elem *>(a.x_out) + at_y, j, y[j], all_x);
             }
+            at_y += stride;
             if (a.n_out) {
                 const Acc v = warp_sum(s.low() + s.high());
                 if (t % 32 == 0) now[1][t / 32] = v;
             }
-            stage_b = stage_b + 1 == stages ? 0 : stage_b + 1;
+            stage_b = stage_b + 1 == Ring::stages ? 0 : stage_b + 1;
         }
+        if constexpr (!kVector) copy_wait<Ring::kBehind>();            // the next row's copies, those of all with the barrier
         __syncthreads();                                               // this turn's sums are there; those of the turn before are free
         fill(stage_c);
-        stage_c = stage_c + 1 == stages ? 0 : stage_c + 1;
-        stage_a = stage_a + 1 == stages ? 0 : stage_a + 1;
+        stage_c = stage_c + 1 == Ring::stages ? 0 : stage_c + 1;
+        stage_a = stage_a + 1 == Ring::stages ? 0 : stage_a + 1;
     }
 }
 
 // Backward, over the rows of a chunk.  In one turn of the loop: the six sums of a row, the outputs of the row before.
 // kRowGate: the gate changes from row to row and comes through the ring like a fifth operand.
-template <int DT, int kHold, bool kRowGate>
+template <int DT, int kHold, bool kVector, bool kRowGate>
 __global__ void __launch_bounds__(kMaxTeam, 1)
-block_norm_bwd_ring_kernel(const NormArgs a)
+block_norm_bwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
 {
     in_stream_order();
-    using X                  = Access<DT, true>;
-    using Elem               = typename X::Elem;
-    using Acc                = typename X::Acc;
-    constexpr int      kP    = kPairs<DT>;
-    constexpr int      kOperands = kRowGate ? 5 : 4;
-    constexpr uint32_t stages    = kRingStages<kHold>;
-    extern __shared__ uint4 ring[];                                    // [stage][operand][hold][thread]
+    using C    = Columns<DT, kHold, kVector>;
+    using Elem = typename C::Elem;
+    using Acc  = typename C::Acc;
+    using Pair = typename C::Pair;
+    constexpr int kP = C::kP, kOperands = kRowGate ? 5 : 4;
+    using Ring = RowRing<DT, kHold, kVector, kOperands>;
+    extern __shared__ uint4 shared[];
     __shared__ Acc part[2][kMaxWarps][8];
-    const uint32_t t = threadIdx.x, team = blockDim.x, chunk = blockIdx.x, warps = team / 32;
-    const uint32_t count = static_cast<uint32_t>(a.d / kLanes<DT>);
+    const uint32_t t = threadIdx.x, chunk = blockIdx.x, warps = blockDim.x / 32;
+    const C        c{t, blockDim.x, static_cast<uint32_t>(a.d)};
+    const Ring     ring(c, shared, slot_bytes);
     const Acc      scale = static_cast<Acc>(a.scale), eps = static_cast<Acc>(a.eps), of_d = Acc(1) / static_cast<Acc>(a.d);
-    const uint64_t bytes = a.rows * a.d * sizeof(Elem);
-    const Extent   all_x = extent_of(a.x_out, bytes), all_f = extent_of(a.n_out, bytes);
-    const Extent   all_g = extent_of(a.dgate, round_up_div(a.rows, a.gate_rows) * a.d * sizeof(Elem));
-    const Extent   part_g = extent_of(a.part_gate, 2ull * a.chunks * a.d * sizeof(Acc));
+    const uint64_t total = a.rows * a.d, gates = round_up_div(a.rows, a.gate_rows) * a.d;
+    const Extent   all_x = extent_of(a.x_out, total * sizeof(Elem)), all_f = extent_of(a.n_out, total * sizeof(Elem));
+    const Extent   all_g = extent_of(a.dgate, gates * sizeof(Elem)), part_g = extent_of(a.part_gate, 2ull * a.chunks * a.d * sizeof(Acc));
     const Extent   part_w = extent_of(a.part_pre, a.chunks * a.d * sizeof(Acc)), part_p = extent_of(a.part_post, a.chunks * a.d * sizeof(Acc));
-    const Chunk    c        = chunk_of(a, chunk);
+    const Chunk    rows     = chunk_of(a, chunk);
     const uint64_t of_chunk = a.group_chunks ? chunk / a.group_chunks : 0;       // the group of all its rows, unless kRowGate
 
-    const auto slot = [&](const uint32_t stage, const int operand, const int j) -> uint4 & {
-        return ring[((stage * kOperands + operand) * kHold + j) * team + t];
-    };
-    // the row to copy next, and where its vectors and those of the row that is written begin
-    uint64_t next = c.first, at_next = next * count + t, at_out = at_next;
+    uint64_t next = rows.first;                                        // the row to copy next
     // (a commit for every row of the ring, also behind the chunk's end: the waits count groups)
     const auto fill = [&](const uint32_t stage) {
-        if (next < c.end) {
-            const uint4 *const x = static_cast<const uint4 *>(a.x) + at_next, *const f = static_cast<const uint4 *>(a.f) + at_next;
-            const uint4 *const dn = static_cast<const uint4 *>(a.dn) + at_next, *const dy = static_cast<const uint4 *>(a.dy) + at_next;
-#pragma unroll
-            for (int j = 0; j < kHold; ++j)
-                if (j * team + t < count) {
-                    copy_ahead(&slot(stage, 0, j), x + j * team);
-                    if (a.f) copy_ahead(&slot(stage, 1, j), f + j * team);
-                    if (a.dn) copy_ahead(&slot(stage, 2, j), dn + j * team);
-                    if (a.dy) copy_ahead(&slot(stage, 3, j), dy + j * team);
-                    if constexpr (kRowGate) copy_ahead(&slot(stage, 4, j), static_cast<const uint4 *>(a.gate) + next / a.gate_rows * count + j * team + t);
-                }
-            ++next, at_next += count;
+        if (next < rows.end) {
+            ring.copy(stage, 0, a.x, next, total);
+            if (a.f) ring.copy(stage, 1, a.f, next, total);
+            if (a.dn) ring.copy(stage, 2, a.dn, next, total);
+            if (a.dy) ring.copy(stage, 3, a.dy, next, total);
+            if constexpr (kRowGate) ring.copy(stage, 4, a.gate, next / a.gate_rows, gates);
+            ++next;
         }
         copy_commit();
     };
-    // columns beyond the row, and operands that the call leaves out, are zeros
-#pragma unroll
-    for (int j = 0; j < kHold; ++j)
-        for (uint32_t s = 0; s < stages; ++s)
-#pragma unroll
-            for (int o = 0; o < kOperands; ++o)
-                if (j * team + t >= count || (o == 1 && !a.f) || (o == 2 && !a.dn) || (o == 3 && !a.dy)) slot(s, o, j) = make_uint4(0, 0, 0, 0);
-    for (uint32_t s = 0; s + 1 < stages; ++s) fill(s);
+    bool present[kOperands];
+    present[0] = true, present[1] = a.f != nullptr, present[2] = a.dn != nullptr, present[3] = a.dy != nullptr;
+    if constexpr (kRowGate) present[4] = true;
+    ring.clear(present);
+    for (uint32_t s = 0; s + 1 < Ring::stages; ++s) fill(s);
 
-    Two<Acc> w_pre[kHold][kP], gw[kHold][kP];
-    branch_factors<DT, kHold, kRowGate>(a, of_chunk, count, gw);
+    Pair w_pre[kHold][kP], gw[kHold][kP];
+    branch_factors<DT, kHold, kVector, kRowGate>(a, of_chunk, c, gw);
 #pragma unroll
     for (int j = 0; j < kHold; ++j) {
-#pragma unroll
-        for (int k = 0; k < kP; ++k) w_pre[j][k] = both(Acc(1));
-        if (a.w_pre && j * team + t < count) read_pairs<DT>(a.w_pre, j * team + t, w_pre[j]);
+        c.fill(w_pre[j], 1);
+        if (a.w_pre) c.read(static_cast<const Elem *>(a.w_pre), j, w_pre[j]);
     }
+    // a row's operands
+    const auto operands = [&](const uint32_t stage, const uint64_t row, const int j, Pair (&x)[kP], Pair (&f)[kP], Pair (&dn)[kP], Pair (&dy)[kP], Pair (&g)[kP]) {
+        ring.read(stage, 0, j, row, true, x);
+        ring.read(stage, 1, j, row, a.f != nullptr, f);
+        ring.read(stage, 2, j, row, a.dn != nullptr, dn);
+        ring.read(stage, 3, j, row, a.dy != nullptr, dy);
+        if constexpr (kRowGate) ring.read(stage, 4, j, row / a.gate_rows, true, g);
+    };
 
     // sum_pre: of dn x' r.  sum_f: of t f rf, of the rows that share a gate; times scale w_post it is the gate's gradient, times
     // scale gate its share of w_post's (sum_post).
-    Two<Acc> sum_pre[kHold][kP], sum_f[kHold][kP], sum_post[kRowGate ? kHold : 1][kP];
+    Pair sum_pre[kHold][kP], sum_f[kHold][kP], sum_post[kRowGate ? kHold : 1][kP];
 #pragma unroll
-    for (int j = 0; j < kHold; ++j)
-#pragma unroll
-        for (int k = 0; k < kP; ++k) sum_pre[j][k] = sum_f[j][k] = sum_post[kRowGate ? j : 0][k] = both(Acc(0));
-    uint32_t stage_a = 0, stage_b = 0, stage_c = stages - 1;           // of the row whose sums are taken, of the one before, to fill
-    for (uint64_t row = c.first; row <= c.end; ++row) {
-        if (row < c.end) {
+    for (int j = 0; j < kHold; ++j) c.fill(sum_pre[j], 0), c.fill(sum_f[j], 0), c.fill(sum_post[kRowGate ? j : 0], 0);
+    if constexpr (!kVector) {                                          // the first row, copied by all
+        copy_wait<Ring::kBehind + 1>();
+        __syncthreads();
+    }
+    uint32_t stage_a = 0, stage_b = 0, stage_c = Ring::stages - 1;     // of the row whose sums are taken, of the one before, to fill
+    uint64_t at_out = rows.first * a.d;
+    for (uint64_t row = rows.first; row <= rows.end; ++row) {
+        if (row < rows.end) {
             // ---- this row's sums
-            copy_wait<static_cast<int>(stages) - 2>();                 // (stages - 1 rows and one more per row so far are on their way)
-            Two<Acc> p[6];
+            if constexpr (kVector) copy_wait<Ring::kBehind>();
+            Pair p[6];
 #pragma unroll
             for (int k = 0; k < 6; ++k) p[k] = both(Acc(0));
 #pragma unroll
             for (int j = 0; j < kHold; ++j) {
-                Two<Acc> x[kP], f[kP], dn[kP], dy[kP], g[kP];
-                widen_pairs<DT>(slot(stage_a, 0, j), x), widen_pairs<DT>(slot(stage_a, 1, j), f);
-                widen_pairs<DT>(slot(stage_a, 2, j), dn), widen_pairs<DT>(slot(stage_a, 3, j), dy);
-                if constexpr (kRowGate) widen_pairs<DT>(slot(stage_a, 4, j), g);
+                Pair x[kP], f[kP], dn[kP], dy[kP], g[kP];
+                operands(stage_a, row, j, x, f, dn, dy, g);
 #pragma unroll
                 for (int k = 0; k < kP; ++k) {
-                    const Two<Acc> wn = dn[k] * w_pre[j][k];
-                    Two<Acc>       q  = gw[j][k] * f[k];
+                    const Pair wn = dn[k] * w_pre[j][k];
+                    Pair       q  = gw[j][k] * f[k];
                     if constexpr (kRowGate) q = q * g[k];
                     p[0] = fma2(x[k], x[k], p[0]);
                     p[1] = fma2(wn, x[k], p[1]);
@@ -652,99 +763,70 @@ block_norm_bwd_ring_kernel(const NormArgs a)
             const Acc v = warp_sums8(s);
             if (t % 4 == 0) part[row & 1][t / 32][t % 32 / 4] = v;
         }
-        if (row > c.first) {
+        if (row > rows.first) {
             // ---- the row before: its outputs
             const uint64_t before = row - 1;
             Acc            s[6];
             cta_sums(part[before & 1], warps, s);
             const RowFactors<Acc> q = factors_of(s, of_d, eps, a.w_post != nullptr);
-            const Two<Acc> r = both(q.r), rrc = both(-q.rrc), rf = both(q.rf), rf3m = both(-q.rf3m);
-            uint4 *const dx = static_cast<uint4 *>(a.x_out) + at_out, *const df = static_cast<uint4 *>(a.n_out) + at_out;
-            at_out += count;
+            const Pair r = both(q.r), rrc = both(-q.rrc), rf = both(q.rf), rf3m = both(-q.rf3m);
 #pragma unroll
             for (int j = 0; j < kHold; ++j) {
-                const uint32_t i = j * team + t;
-                Two<Acc> x[kP], f[kP], dn[kP], dy[kP], g[kP];
-                widen_pairs<DT>(slot(stage_b, 0, j), x), widen_pairs<DT>(slot(stage_b, 1, j), f);
-                widen_pairs<DT>(slot(stage_b, 2, j), dn), widen_pairs<DT>(slot(stage_b, 3, j), dy);
-                if constexpr (kRowGate) widen_pairs<DT>(slot(stage_b, 4, j), g);
+                Pair x[kP], f[kP], dn[kP], dy[kP], g[kP];
+                operands(stage_b, before, j, x, f, dn, dy, g);
 #pragma unroll
                 for (int k = 0; k < kP; ++k) {
-                    const Two<Acc> tv = fma2(rrc, x[k], fma2(r, dn[k] * w_pre[j][k], dy[k]));
-                    sum_pre[j][k]     = fma2(dn[k], x[k] * r, sum_pre[j][k]);
-                    sum_f[j][k]       = fma2(tv, f[k] * rf, sum_f[j][k]);
-                    Two<Acc> tg       = tv * gw[j][k];
+                    const Pair tv = fma2(rrc, x[k], fma2(r, dn[k] * w_pre[j][k], dy[k]));
+                    sum_pre[j][k] = fma2(dn[k], x[k] * r, sum_pre[j][k]);
+                    sum_f[j][k]   = fma2(tv, f[k] * rf, sum_f[j][k]);
+                    Pair tg       = tv * gw[j][k];
                     if constexpr (kRowGate) tg = tg * g[k];
                     f[k]  = fma2(tg, rf, rf3m * f[k]);
                     dy[k] = tv;
                 }
-                if (i < count) {
-                    if (a.x_out && all_x.holds(dx + j * team, 16)) dx[j * team] = narrow_pairs<DT>(dy);
-                    if (a.n_out && all_f.holds(df + j * team, 16)) df[j * team] = narrow_pairs<DT>(f);
-                }
+                if (a.x_out) c.write(static_cast<Elem *>(a.x_out) + at_out, j, dy, all_x);
+                if (a.n_out) c.write(static_cast<Elem *>(a.n_out) + at_out, j, f, all_f);
             }
+            at_out += a.d;
             // the last of the group's rows in this chunk: its gate's gradient, or this chunk's share of it
-            if (a.gate && (row == c.end || (kRowGate && row % a.gate_rows == 0))) {
+            if (a.gate && (row == rows.end || (kRowGate && row % a.gate_rows == 0))) {
                 const uint64_t group = before / a.gate_rows;
                 uint64_t       to;
-                const bool     whole = whole_group(a, c, group, chunk, to);
+                const bool     whole = whole_group(a, rows, group, chunk, to);
 #pragma unroll
                 for (int j = 0; j < kHold; ++j) {
-                    const uint32_t i = j * team + t;
-                    Two<Acc>       w[kP], g[kP];
-#pragma unroll
-                    for (int k = 0; k < kP; ++k) w[k] = both(Acc(1)), g[k] = both(Acc(0));
-                    if (i < count) {
-                        if (a.w_post) read_pairs<DT>(a.w_post, i, w);
-                        if (kRowGate) widen_pairs<DT>(slot(stage_b, 4, j), g);
-                    }
+                    Pair w[kP], g[kP];
+                    c.fill(w, 1);
+                    if (a.w_post) c.read(static_cast<const Elem *>(a.w_post), j, w);
+                    if constexpr (kRowGate) ring.read(stage_b, 4, j, group, true, g);
 #pragma unroll
                     for (int k = 0; k < kP; ++k) {
                         w[k] = w[k] * both(scale) * sum_f[j][k];
                         if constexpr (kRowGate) sum_post[j][k] = fma2(both(scale) * g[k], sum_f[j][k], sum_post[j][k]), sum_f[j][k] = both(Acc(0));
                     }
-                    if (a.dgate && i < count) {
-                        uint4 *const out = static_cast<uint4 *>(row_of<Elem>(a.dgate, group, a.d)) + i;
-                        if (whole) {
-                            if (all_g.holds(out, 16)) *out = narrow_pairs<DT>(w);
-                        } else {
-#pragma unroll
-                            for (int k = 0; k < 2 * kP; ++k) {
-                                Acc *const o = reinterpret_cast<Acc *>(a.part_gate) + to * a.d + i * 2 * kP + k;
-                                if (part_g.holds(o, sizeof(Acc))) *o = k % 2 ? w[k / 2].high() : w[k / 2].low();
-                            }
-                        }
-                    }
+                    if (a.dgate && whole) c.write(static_cast<Elem *>(a.dgate) + group * a.d, j, w, all_g);
+                    if (a.dgate && !whole) c.write_sums(reinterpret_cast<Acc *>(a.part_gate) + to * a.d, j, w, part_g);
                 }
             }
-            stage_b = stage_b + 1 == stages ? 0 : stage_b + 1;
+            stage_b = stage_b + 1 == Ring::stages ? 0 : stage_b + 1;
         }
+        if constexpr (!kVector) copy_wait<Ring::kBehind>();            // the next row's copies, those of all with the barrier
         __syncthreads();                                               // the sums of this row are there; the words of the one before are free
         fill(stage_c);
-        stage_c = stage_c + 1 == stages ? 0 : stage_c + 1;
-        stage_a = stage_a + 1 == stages ? 0 : stage_a + 1;
+        stage_c = stage_c + 1 == Ring::stages ? 0 : stage_c + 1;
+        stage_a = stage_a + 1 == Ring::stages ? 0 : stage_a + 1;
     }
 #pragma unroll
     for (int j = 0; j < kHold; ++j) {
-        const uint32_t i = j * team + t;
-        if (i >= count) continue;
         if (!kRowGate && a.dw_post) {
-            Two<Acc> g[kP];
-#pragma unroll
-            for (int k = 0; k < kP; ++k) g[k] = both(Acc(1));
-            if (a.gate) read_pairs<DT>(row_of<Elem>(a.gate, of_chunk, a.d), i, g);
+            Pair g[kP];
+            c.fill(g, 1);
+            if (a.gate) c.read(static_cast<const Elem *>(a.gate) + of_chunk * a.d, j, g);
 #pragma unroll
             for (int k = 0; k < kP; ++k) sum_f[j][k] = sum_f[j][k] * both(scale) * g[k];
         }
-#pragma unroll
-        for (int k = 0; k < 2 * kP; ++k) {
-            const uint64_t o    = chunk * a.d + i * 2 * kP + k;
-            const Two<Acc> post = kRowGate ? sum_post[kRowGate ? j : 0][k / 2] : sum_f[j][k / 2];
-            if (a.dw_pre && part_w.holds(reinterpret_cast<Acc *>(a.part_pre) + o, sizeof(Acc)))
-                reinterpret_cast<Acc *>(a.part_pre)[o] = k % 2 ? sum_pre[j][k / 2].high() : sum_pre[j][k / 2].low();
-            if (a.dw_post && part_p.holds(reinterpret_cast<Acc *>(a.part_post) + o, sizeof(Acc)))
-                reinterpret_cast<Acc *>(a.part_post)[o] = k % 2 ? post.high() : post.low();
-        }
+        if (a.dw_pre) c.write_sums(reinterpret_cast<Acc *>(a.part_pre) + chunk * a.d, j, sum_pre[j], part_w);
+        if (a.dw_post) c.write_sums(reinterpret_cast<Acc *>(a.part_post) + chunk * a.d, j, kRowGate ? sum_post[kRowGate ? j : 0] : sum_f[j], part_p);
     }
 }
 
@@ -1014,28 +1096,59 @@ block_norm_finish_kernel(const NormArgs a)
 constexpr uint32_t kMaxChunks  = 4096;      // chunks of rows of a backward pass
 constexpr uint32_t kLongChunks = 64;        // the same for rows longer than a CTA's registers
 
+// threads of a CTA that holds `count` accesses, `hold` per thread
+uint32_t team_of(uint64_t count, uint32_t hold) { return static_cast<uint32_t>(round_up_div(round_up_div(count, hold), 32) * 32); }
+// Vectors per thread of the ring kernels: two from 64 on, which halves what the sums over a row cost per element; CTAs of an SM:
+// 512 threads' worth.  Rows of single elements: eight columns per thread, sixteen where that takes more than a CTA.
+uint32_t hold_of(uint64_t count) { return count < 64 ? 1 : 2; }
+constexpr size_t kMostShared = 220 * 1024;
+
+// How a ring kernel takes rows of d elements: hold 0 if it cannot.
+struct RingPlan {
+    uint32_t hold, team, slot;     // slot: bytes of an operand's row, rows of single elements
+    size_t   smem;
+};
+RingPlan ring_plan(uint64_t d, int es, uint32_t operands)
+{
+    const uint64_t lanes = 16 / static_cast<uint64_t>(es);
+    RingPlan       p{};
+    if (d % lanes == 0) {
+        const uint64_t count = d / lanes;
+        if (count > 2 * kMaxTeam) return p;
+        p.hold = hold_of(count), p.team = team_of(count, p.hold);
+        p.smem = static_cast<size_t>(p.hold == 1 ? kRingStages<1, true> : kRingStages<2, true>) * operands * p.hold * p.team * 16;
+    } else {
+        if (d > 16 * kMaxTeam) return p;
+        p.hold = d <= 8 * kMaxTeam ? 1 : 2, p.team = team_of(d, 8 * p.hold);
+        p.slot = static_cast<uint32_t>((d * static_cast<uint64_t>(es) + 15) / 16 * 16 + 16);
+        p.smem = static_cast<size_t>(kRingStages<1, false>) * operands * p.slot;
+    }
+    if (p.smem > kMostShared) p.hold = 0;
+    return p;
+}
+
 // Can a CTA's registers hold a row of the backward pass?
 bool row_fits(uint64_t d, int es)
 {
     const uint64_t lanes = 16 / static_cast<uint64_t>(es);
-    return d <= kMaxTeam * (d % lanes == 0 ? 2 * lanes : 8);
+    return d % lanes == 0 ? d <= 2 * lanes * kMaxTeam : d <= 8 * kMaxTeam || ring_plan(d, es, 5).hold != 0;
 }
 
-// threads of a CTA that holds `count` accesses, `hold` per thread
-uint32_t team_of(uint64_t count, uint32_t hold) { return static_cast<uint32_t>(round_up_div(round_up_div(count, hold), 32) * 32); }
-// Vectors per thread of the ring kernels: two from 64 on, which halves what the sums over a row cost per element; CTAs of an SM:
-// 512 threads' worth.
-uint32_t hold_of(uint64_t count) { return count < 64 ? 1 : 2; }
-
-template <int kHold>
-size_t ring_bytes(uint32_t team, uint32_t operands) { return static_cast<size_t>(kRingStages<kHold>) * operands * kHold * team * 16; }
-constexpr size_t kMostShared = 220 * 1024;
-
 template <typename K>
-cudaError_t start_ring(K kernel, const NormArgs &a, unsigned grid, uint32_t team, size_t smem, cudaStream_t stream)
+cudaError_t start_ring(K kernel, const NormArgs &a, unsigned grid, const RingPlan &p, cudaStream_t stream)
 {
-    const cudaError_t e = reported(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem)));
-    return e != cudaSuccess ? e : launch(kernel, grid, team, smem, stream, a);
+    const cudaError_t e = reported(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(p.smem)));
+    return e != cudaSuccess ? e : launch(kernel, grid, p.team, p.smem, stream, a, p.slot);
+}
+
+// go(hold, whether rows are whole vectors)
+template <typename F>
+cudaError_t with_ring(const RingPlan &p, bool vector, const F &go)
+{
+    using std::bool_constant;
+    using std::integral_constant;
+    if (p.hold == 1) return vector ? go(integral_constant<int, 1>(), bool_constant<true>()) : go(integral_constant<int, 1>(), bool_constant<false>());
+    return vector ? go(integral_constant<int, 2>(), bool_constant<true>()) : go(integral_constant<int, 2>(), bool_constant<false>());
 }
 
 template <int DT, bool kVector, int kHold, bool kCta>
@@ -1051,26 +1164,25 @@ cudaError_t forward(const NormArgs &a, cudaStream_t stream)
 {
     const int sms = sm_count();
     if (sms == 0) return cudaErrorInvalidDevice;
-    const uint64_t count = a.d / kLanes<DT>;
-    if (a.d % kLanes<DT> == 0 && count <= 2 * kMaxTeam) {
-        const bool     row_gate = a.gate && a.gate_rows < a.rows;
-        const uint32_t hold = hold_of(count), team = team_of(count, hold);
-        const uint64_t most = static_cast<uint64_t>(sms) * (2 * kMaxTeam / team < 32 ? 2 * kMaxTeam / team : 32);
-        const unsigned grid = static_cast<unsigned>(a.rows < most ? a.rows : most);
-        if (hold == 1)
-            return row_gate ? start_ring(block_norm_fwd_ring_kernel<DT, 1, true>, a, grid, team, ring_bytes<1>(team, 3), stream)
-                            : start_ring(block_norm_fwd_ring_kernel<DT, 1, false>, a, grid, team, ring_bytes<1>(team, 2), stream);
-        return row_gate ? start_ring(block_norm_fwd_ring_kernel<DT, 2, true>, a, grid, team, ring_bytes<2>(team, 3), stream)
-                        : start_ring(block_norm_fwd_ring_kernel<DT, 2, false>, a, grid, team, ring_bytes<2>(team, 2), stream);
+    const uint64_t count    = a.d / kLanes<DT>;
+    const bool     vector   = a.d % kLanes<DT> == 0, row_gate = a.gate && a.gate_rows < a.rows;
+    const RingPlan p        = ring_plan(a.d, static_cast<int>(sizeof(typename Num<DT>::Elem)), row_gate ? 3 : 2);
+    if (p.hold != 0) {
+        // 512 threads an SM (three CTAs of 256 where the registers allow them: bf16 16384 x 4096 97 us against 86)
+        const uint32_t resident = kMaxTeam / p.team;
+        const uint64_t most     = static_cast<uint64_t>(sms) * (resident < 1 ? 1 : resident);
+        const unsigned grid     = static_cast<unsigned>(a.rows < most ? a.rows : most);
+        const auto     go   = [&](auto hold, auto vec) {
+            return row_gate ? start_ring(block_norm_fwd_ring_kernel<DT, decltype(hold)::value, decltype(vec)::value, true>, a, grid, p, stream)
+                            : start_ring(block_norm_fwd_ring_kernel<DT, decltype(hold)::value, decltype(vec)::value, false>, a, grid, p, stream);
+        };
+        return with_ring(p, vector, go);
     }
-    if (a.d % kLanes<DT> == 0) {
+    if (vector) {
         if (count <= 4 * kMaxTeam) return start_fwd<DT, true, 4, true>(a, team_of(count, 4), sms, stream);
         return start_fwd<DT, true, 0, true>(a, kMaxTeam, sms, stream);
     }
-    if (a.d <= 32) return start_fwd<DT, false, 1, false>(a, 32 * kWarpTeams, sms, stream);
-    if (a.d <= 64) return start_fwd<DT, false, 2, false>(a, 32 * kWarpTeams, sms, stream);
-    if (a.d <= 128) return start_fwd<DT, false, 4, false>(a, 32 * kWarpTeams, sms, stream);
-    if (a.d <= 2 * kMaxTeam) return start_fwd<DT, false, 2, true>(a, team_of(a.d, 2), sms, stream);
+    // (single elements whose ring does not fit shared memory)
     if (a.d <= 4 * kMaxTeam) return start_fwd<DT, false, 4, true>(a, team_of(a.d, 4), sms, stream);
     return start_fwd<DT, false, 0, true>(a, kMaxTeam, sms, stream);
 }
@@ -1082,27 +1194,21 @@ cudaError_t start_bwd(const NormArgs &a, uint32_t threads, cudaStream_t stream)
     return launch(block_norm_bwd_kernel<DT, kVector, kHold, kCta>, static_cast<unsigned>(round_up_div(a.chunks, teams)), threads, 0, stream, a);
 }
 
+// rows that a CTA's registers hold (row_fits)
 template <int DT>
-cudaError_t bwd_vectors(const NormArgs &a, cudaStream_t stream)
+cudaError_t bwd_of(const NormArgs &a, cudaStream_t stream)
 {
-    const uint64_t count    = a.d / kLanes<DT>;
-    const bool     row_gate = a.gate && !a.group_chunks;
-    const uint32_t hold = hold_of(count), team = team_of(count, hold);
-    if (hold == 1)
-        return row_gate ? start_ring(block_norm_bwd_ring_kernel<DT, 1, true>, a, a.chunks, team, ring_bytes<1>(team, 5), stream)
-                        : start_ring(block_norm_bwd_ring_kernel<DT, 1, false>, a, a.chunks, team, ring_bytes<1>(team, 4), stream);
-    if (!row_gate) return start_ring(block_norm_bwd_ring_kernel<DT, 2, false>, a, a.chunks, team, ring_bytes<2>(team, 4), stream);
-    if (ring_bytes<2>(team, 5) <= kMostShared) return start_ring(block_norm_bwd_ring_kernel<DT, 2, true>, a, a.chunks, team, ring_bytes<2>(team, 5), stream);
-    return start_bwd<DT, true, 2, true>(a, team, stream);              // five operands of such rows do not fit shared memory three times
-}
-template <int DT>
-cudaError_t bwd_elements(const NormArgs &a, cudaStream_t stream)
-{
-    if (a.d <= 32) return start_bwd<DT, false, 1, false>(a, 32 * kWarpTeams, stream);
-    if (a.d <= 64) return start_bwd<DT, false, 2, false>(a, 32 * kWarpTeams, stream);
-    if (a.d <= kMaxTeam) return start_bwd<DT, false, 1, true>(a, team_of(a.d, 1), stream);
-    if (a.d <= 2 * kMaxTeam) return start_bwd<DT, false, 2, true>(a, team_of(a.d, 2), stream);
-    return start_bwd<DT, false, 8, true>(a, team_of(a.d, 8), stream);
+    const bool     vector = a.d % kLanes<DT> == 0, row_gate = a.gate && !a.group_chunks;
+    const RingPlan p      = ring_plan(a.d, static_cast<int>(sizeof(typename Num<DT>::Elem)), row_gate ? 5 : 4);
+    if (p.hold != 0) {
+        const auto go = [&](auto hold, auto vec) {
+            return row_gate ? start_ring(block_norm_bwd_ring_kernel<DT, decltype(hold)::value, decltype(vec)::value, true>, a, a.chunks, p, stream)
+                            : start_ring(block_norm_bwd_ring_kernel<DT, decltype(hold)::value, decltype(vec)::value, false>, a, a.chunks, p, stream);
+        };
+        return with_ring(p, vector, go);
+    }
+    // (the operands of such rows do not fit shared memory several times)
+    return vector ? start_bwd<DT, true, 2, true>(a, team_of(a.d / kLanes<DT>, 2), stream) : start_bwd<DT, false, 8, true>(a, team_of(a.d, 8), stream);
 }
 
 // The most chunks of a backward pass: as many teams as the SMs hold at a time.
@@ -1111,9 +1217,7 @@ uint32_t chunks_of(uint64_t rows, uint64_t d, int es, int sms)
     const uint64_t lanes = 16 / static_cast<uint64_t>(es), count = d / lanes;
     uint64_t       most;
     if (!row_fits(d, es)) most = kLongChunks;
-    else if (d % lanes == 0) most = static_cast<uint64_t>(sms) * (kMaxTeam / team_of(count, hold_of(count)));
-    else if (d <= 64) most = static_cast<uint64_t>(sms) * 24;
-    else most = static_cast<uint64_t>(sms) * (d <= 256 ? 6 : d <= 512 ? 3 : 2);
+    else most = static_cast<uint64_t>(sms) * (kMaxTeam / (d % lanes == 0 ? team_of(count, hold_of(count)) : team_of(d, d <= 8 * kMaxTeam ? 8 : 16)));
     if (most > kMaxChunks) most = kMaxChunks;
     if (most > rows / 4) most = rows / 4 > static_cast<uint64_t>(sms) ? rows / 4 : static_cast<uint64_t>(sms);   // partial rows cost, too
     return static_cast<uint32_t>(most < rows ? most : rows);
@@ -1149,7 +1253,7 @@ cudaError_t backward(const NormArgs &a, cudaStream_t stream)
         if (!a.dgate && !a.dw_pre && !a.dw_post) return cudaSuccess;
         e = launch(block_norm_bwd_columns_kernel<DT>, static_cast<unsigned>(round_up_div(a.d, 128) * a.chunks), 128, 0, stream, a);
     } else {
-        e = a.d % kLanes<DT> == 0 ? bwd_vectors<DT>(a, stream) : bwd_elements<DT>(a, stream);
+        e = bwd_of<DT>(a, stream);
     }
     if (e != cudaSuccess || (!a.dgate && !a.dw_pre && !a.dw_post)) return e;
     const uint64_t groups = round_up_div(a.rows, a.gate_rows), borders = a.chunks - 1;

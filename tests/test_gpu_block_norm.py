@@ -10,7 +10,7 @@ KINDS = ["f32", "f16", "bf16", "f64"]
 SCALE, EPS = 0.375, 2.0 ** -20                      # both exact in binary32
 
 # rows, d: one row, one element, every form of the kernels (a warp or a CTA per row, whole vectors or not, rows read again)
-SIZES = [(1, 1), (1, 2048), (5, 7), (3, 64), (37, 72), (130, 256), (33, 520), (19, 1000), (9, 1025), (700, 1024), (6, 4096), (5, 4100), (4, 8192),
+SIZES = [(1, 1), (1, 2048), (5, 7), (3, 64), (37, 72), (130, 256), (33, 520), (19, 1000), (9, 1025), (700, 1024), (900, 1001), (700, 2047), (300, 4093), (6, 4096), (5, 4100), (4, 8192),
          (3, 8193), (2, 16392), (3, 20001)]
 
 
@@ -168,7 +168,7 @@ def test_backward(size, kind):
 # groups that end inside the CTAs' chunks of rows, cross them, cross several of them, one row each, one group
 @pytest.mark.parametrize("kind", ["f32", "bf16", "f64"])
 @pytest.mark.parametrize("rows,groups", [(6000, 1), (6000, 6000), (6000, 3000), (6000, 5), (6000, 400), (6001, 1), (5999, 7), (13000, 2), (24, 8)])
-@pytest.mark.parametrize("d", [64, 72, 33, 1000, 2048])
+@pytest.mark.parametrize("d", [64, 72, 33, 1000, 1003, 2048])
 def test_gate_groups(rows, groups, d, kind):
     if rows % groups:
         groups = 1 if rows == 6001 else 857              # 5999 = 7 * 857
