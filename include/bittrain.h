@@ -592,8 +592,7 @@ int bt_block_norm_fwd(const void *x, uint64_t rows, uint64_t d, uint64_t gate_ro
  * gradient of the residual stream), grad_f, grad_gate (the gate's shape), grad_w_post and grad_w_pre (d elements).
  * Any output may be NULL; no output may overlap an input.  The sums over rows are added in a fixed order.  workspace_bytes >=
  * bt_block_norm_workspace_bytes(rows, d, dtype) (asked with the same device current), contents as for
- * bt_glu_fwd; it may be NULL where neither grad_gate nor a weight's gradient is wanted and a row has at most
- * 1024 16-byte vectors (d a multiple of a vector) or 4096 elements.  rows == 0 sets the weights' gradients to +0.
+ * bt_glu_fwd; it may be NULL where neither grad_gate nor a weight's gradient is wanted and d <= 8192.  rows == 0 sets the weights' gradients to +0.
  */
 size_t bt_block_norm_workspace_bytes(uint64_t rows, uint64_t d, int dtype);
 

@@ -33,40 +33,9 @@ struct NormArgs {
     double      scale, eps;
 };
 
-constexpr int      kMaxTeam   = 512;                                    // threads of a CTA that takes a row
-constexpr int      kMaxWarps  = kMaxTeam / 32;
-constexpr uint32_t kWarpTeams = 4;                                      // warps of a CTA whose teams are warps
-
-// kVector: 16-byte accesses, else single elements (rows that do not all begin on a 16-byte boundary)
-template <int DT, bool kVector>
-struct Access {
-    using Elem              = typename Num<DT>::Elem;
-    using Acc               = typename Num<DT>::Acc;
-    static constexpr int kW = kVector ? kLanes<DT> : 1;
-    using Raw               = typename std::conditional<kVector, uint4, Elem>::type;
-    __device__ static __forceinline__ Raw load(const void *row, const uint32_t i)
-    {
-        return static_cast<const Raw *>(row)[i];
-    }
-    __device__ static __forceinline__ void widen(const Raw &w, Acc (&v)[kW])
-    {
-        if constexpr (kVector) widen_vec<DT>(w, v);
-        else v[0] = Num<DT>::widen(w);
-    }
-    __device__ static __forceinline__ void read(const void *row, const uint32_t i, Acc (&v)[kW]) { widen(load(row, i), v); }
-    // weights and gates, which no output overlaps
-    __device__ static __forceinline__ void read_shared(const void *row, const uint32_t i, Acc (&v)[kW])
-    {
-        widen(__ldg(static_cast<const Raw *>(row) + i), v);
-    }
-    __device__ static __forceinline__ void store(void *row, const uint32_t i, const Acc (&v)[kW], const Extent &e)
-    {
-        Raw *const p = static_cast<Raw *>(row) + i;
-        if (!e.holds(p, sizeof(Raw))) return;
-        if constexpr (kVector) *p = narrow_vec<DT>(v);
-        else *p = Num<DT>::narrow(v[0]);
-    }
-};
+constexpr int kMaxTeam    = 512;                                        // threads of a CTA
+constexpr int kMaxWarps   = kMaxTeam / 32;
+constexpr int kMaxCluster = 8;                                          // CTAs that share a row
 
 template <typename Elem>
 __device__ __forceinline__ const void *row_of(const void *base, const uint64_t row, const uint64_t d)
@@ -82,176 +51,71 @@ __device__ __forceinline__ void *row_of(void *base, const uint64_t row, const ui
 __device__ __forceinline__ float  root_of(float v) { return rsqrtf(v); }
 __device__ __forceinline__ double root_of(double v) { return rsqrt(v); }
 
-// The sums of a team: a warp, or (kCta) the CTA.  `turn` alternates between two sets of words, so that one barrier serves a
-// reduction: words are written again only behind the barrier of the reduction in between.
-template <bool kCta, int kSums, typename A>
+// The sums of a CTA.  `turn` alternates between two sets of words, so that one barrier serves a reduction: words are written
+// again only behind the barrier of the reduction in between.
+template <int kSums, typename A>
 __device__ __forceinline__ void team_sums(A (&s)[kSums], A (*words)[kSums][kMaxWarps], uint32_t &turn)
 {
+    A (&w)[kSums][kMaxWarps] = words[turn & 1];
+    ++turn;
 #pragma unroll
-    for (int k = 0; k < kSums; ++k) s[k] = warp_sum(s[k]);
-    if constexpr (kCta) {
-        const uint32_t warps = blockDim.x / 32;
-        A (&w)[kSums][kMaxWarps] = words[turn & 1];
-        ++turn;
-        if (threadIdx.x % 32 == 0) {
-#pragma unroll
-            for (int k = 0; k < kSums; ++k) w[k][threadIdx.x / 32] = s[k];
-        }
-        __syncthreads();
-#pragma unroll
-        for (int k = 0; k < kSums; ++k) {
-            const A v = threadIdx.x % 32 < warps ? w[k][threadIdx.x % 32] : A(0);
-            s[k]      = warp_sum(v);
-        }
+    for (int k = 0; k < kSums; ++k) {
+        s[k] = warp_sum(s[k]);
+        if (threadIdx.x % 32 == 0) w[k][threadIdx.x / 32] = s[k];
     }
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kSums; ++k) s[k] = warp_sum(threadIdx.x % 32 < blockDim.x / 32 ? w[k][threadIdx.x % 32] : A(0));
 }
 
-// ---------------------------------------------------------------------------------------------- forward
-// kHold accesses of each of x and f per thread; 0: rows of any length, read again for each use.
-template <int DT, bool kVector, int kHold, bool kCta>
-__global__ void __launch_bounds__(kCta ? kMaxTeam : 32 * kWarpTeams)
-block_norm_fwd_kernel(const NormArgs a)
+// ---------------------------------------------------------------------------------------------- forward, rows of any length
+// For rows that the ring kernels below do not hold: a row is read again for each use.
+template <int DT>
+__global__ void __launch_bounds__(kMaxTeam)
+block_norm_fwd_long_kernel(const NormArgs a)
 {
     in_stream_order();
-    using X                = Access<DT, kVector>;
-    using Elem             = typename X::Elem;
-    using Acc              = typename X::Acc;
-    constexpr int  kW      = X::kW;
+    using Elem = typename Num<DT>::Elem;
+    using Acc  = typename Num<DT>::Acc;
     __shared__ Acc words[2][1][kMaxWarps];
-    uint32_t       turn    = 0;
-    const uint32_t team    = kCta ? blockDim.x : 32;
-    const uint32_t t       = kCta ? threadIdx.x : threadIdx.x % 32;
-    const uint32_t count   = static_cast<uint32_t>(a.d / kW);
+    uint32_t       turn  = 0;
     const Acc      scale = static_cast<Acc>(a.scale), eps = static_cast<Acc>(a.eps), of_d = Acc(1) / static_cast<Acc>(a.d);
-    const uint64_t first   = kCta ? blockIdx.x : static_cast<uint64_t>(blockIdx.x) * (blockDim.x / 32) + threadIdx.x / 32;
-    const uint64_t step    = kCta ? gridDim.x : static_cast<uint64_t>(gridDim.x) * (blockDim.x / 32);
-    const Extent   all_x = extent_of(a.x_out, a.rows * a.d * sizeof(Elem)), all_n = extent_of(a.n_out, a.rows * a.d * sizeof(Elem));
-    for (uint64_t row = first; row < a.rows; row += step) {
-        const void *x = row_of<Elem>(a.x, row, a.d), *f = row_of<Elem>(a.f, row, a.d);
-        const void *gate = a.gate ? row_of<Elem>(a.gate, row / a.gate_rows, a.d) : nullptr;
-        void       *x_out = row_of<Elem>(a.x_out, row, a.d), *n_out = row_of<Elem>(a.n_out, row, a.d);
-        if constexpr (kHold > 0) {
-            Acc v[kHold][kW];
-            if (f) {
-                Acc fv[kHold][kW], s[1] = {0};
-#pragma unroll
-                for (int j = 0; j < kHold; ++j)
-                    if (j * team + t < count) {
-                        X::read(f, j * team + t, fv[j]);
-                        X::read(x, j * team + t, v[j]);
-                    }
-                Acc rf = 1;
-                if (a.w_post) {
-#pragma unroll
-                    for (int j = 0; j < kHold; ++j)
-                        if (j * team + t < count) {
-#pragma unroll
-                            for (int k = 0; k < kW; ++k) s[0] += fv[j][k] * fv[j][k];
-                        }
-                    team_sums<kCta>(s, words, turn);
-                    rf = root_of(s[0] * of_d + eps);
-                }
-                rf *= scale;
-#pragma unroll
-                for (int j = 0; j < kHold; ++j)
-                    if (j * team + t < count) {
-                        Acc w[kW];
-#pragma unroll
-                        for (int k = 0; k < kW; ++k) fv[j][k] *= rf;
-                        if (a.w_post) {
-                            X::read_shared(a.w_post, j * team + t, w);
-#pragma unroll
-                            for (int k = 0; k < kW; ++k) fv[j][k] *= w[k];
-                        }
-                        if (gate) {
-                            X::read_shared(gate, j * team + t, w);
-#pragma unroll
-                            for (int k = 0; k < kW; ++k) fv[j][k] *= w[k];
-                        }
-#pragma unroll
-                        for (int k = 0; k < kW; ++k) v[j][k] += fv[j][k];
-                        X::store(x_out, j * team + t, v[j], all_x);
-                    }
-            } else {
-#pragma unroll
-                for (int j = 0; j < kHold; ++j)
-                    if (j * team + t < count) X::read(x, j * team + t, v[j]);
+    const uint64_t bytes = a.rows * a.d * sizeof(Elem);
+    const Extent   all_x = extent_of(a.x_out, bytes), all_n = extent_of(a.n_out, bytes);
+    const Elem    *w_post = static_cast<const Elem *>(a.w_post), *w_pre = static_cast<const Elem *>(a.w_pre);
+    for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+        const Elem *x = static_cast<const Elem *>(a.x) + row * a.d, *f = static_cast<const Elem *>(row_of<Elem>(a.f, row, a.d));
+        const Elem *gate = static_cast<const Elem *>(row_of<Elem>(a.gate, row / a.gate_rows, a.d));
+        Elem       *x_out = static_cast<Elem *>(row_of<Elem>(a.x_out, row, a.d)), *n_out = static_cast<Elem *>(row_of<Elem>(a.n_out, row, a.d));
+        Acc         s[1] = {0}, rf = scale;
+        if (w_post) {
+            for (uint64_t i = threadIdx.x; i < a.d; i += blockDim.x) {
+                const Acc v = Num<DT>::widen(f[i]);
+                s[0] += v * v;
             }
-            if (!n_out) continue;
-            Acc s[1] = {0};
-#pragma unroll
-            for (int j = 0; j < kHold; ++j)
-                if (j * team + t < count) {
-#pragma unroll
-                    for (int k = 0; k < kW; ++k) s[0] += v[j][k] * v[j][k];
-                }
-            team_sums<kCta>(s, words, turn);
-            const Acc r = root_of(s[0] * of_d + eps);
-#pragma unroll
-            for (int j = 0; j < kHold; ++j)
-                if (j * team + t < count) {
-                    Acc w[kW];
-                    X::read_shared(a.w_pre, j * team + t, w);
-#pragma unroll
-                    for (int k = 0; k < kW; ++k) v[j][k] = v[j][k] * r * w[k];
-                    X::store(n_out, j * team + t, v[j], all_n);
-                }
-        } else {
-            Acc rf = 1;
-            if (f && a.w_post) {
-                Acc s[1] = {0};
-                for (uint32_t i = t; i < count; i += team) {
-                    Acc w[kW];
-                    X::read(f, i, w);
-#pragma unroll
-                    for (int k = 0; k < kW; ++k) s[0] += w[k] * w[k];
-                }
-                team_sums<kCta>(s, words, turn);
-                rf = root_of(s[0] * of_d + eps);
+            team_sums(s, words, turn);
+            rf *= root_of(s[0] * of_d + eps);
+        }
+        const auto sum_at = [&](const uint64_t i) {
+            Acc p = f ? Num<DT>::widen(f[i]) * rf : Acc(0);
+            if (w_post) p *= Num<DT>::widen(__ldg(w_post + i));
+            if (gate) p *= Num<DT>::widen(__ldg(gate + i));
+            return Num<DT>::widen(x[i]) + p;
+        };
+        Acc r = 0;
+        if (n_out) {
+            s[0] = 0;
+            for (uint64_t i = threadIdx.x; i < a.d; i += blockDim.x) {
+                const Acc v = sum_at(i);
+                s[0] += v * v;
             }
-            rf *= scale;
-            const auto sum_at = [&](const uint32_t i, Acc (&v)[kW]) {
-                X::read(x, i, v);
-                if (!f) return;
-                Acc p[kW], w[kW];
-                X::read(f, i, p);
-#pragma unroll
-                for (int k = 0; k < kW; ++k) p[k] *= rf;
-                if (a.w_post) {
-                    X::read_shared(a.w_post, i, w);
-#pragma unroll
-                    for (int k = 0; k < kW; ++k) p[k] *= w[k];
-                }
-                if (gate) {
-                    X::read_shared(gate, i, w);
-#pragma unroll
-                    for (int k = 0; k < kW; ++k) p[k] *= w[k];
-                }
-#pragma unroll
-                for (int k = 0; k < kW; ++k) v[k] += p[k];
-            };
-            Acc r = 0;
-            if (n_out) {
-                Acc s[1] = {0};
-                for (uint32_t i = t; i < count; i += team) {
-                    Acc v[kW];
-                    sum_at(i, v);
-#pragma unroll
-                    for (int k = 0; k < kW; ++k) s[0] += v[k] * v[k];
-                }
-                team_sums<kCta>(s, words, turn);
-                r = root_of(s[0] * of_d + eps);
-            }
-            for (uint32_t i = t; i < count; i += team) {
-                Acc v[kW], w[kW];
-                sum_at(i, v);
-                if (f) X::store(x_out, i, v, all_x);
-                if (!n_out) continue;
-                X::read_shared(a.w_pre, i, w);
-#pragma unroll
-                for (int k = 0; k < kW; ++k) v[k] = v[k] * r * w[k];
-                X::store(n_out, i, v, all_n);
-            }
+            team_sums(s, words, turn);
+            r = root_of(s[0] * of_d + eps);
+        }
+        for (uint64_t i = threadIdx.x; i < a.d; i += blockDim.x) {
+            const Acc v = sum_at(i);
+            if (x_out && all_x.holds(x_out + i, sizeof(Elem))) x_out[i] = Num<DT>::narrow(v);
+            if (n_out && all_n.holds(n_out + i, sizeof(Elem))) n_out[i] = Num<DT>::narrow(v * r * Num<DT>::widen(__ldg(w_pre + i)));
         }
     }
 }
@@ -324,7 +188,7 @@ __device__ __forceinline__ bool whole_group(const NormArgs &a, const Chunk &c, c
 }
 
 // ---------------------------------------------------------------------------------------------- rows through a ring
-// A CTA per row, and a ring of rows in shared memory, filled by asynchronous copies several rows ahead (RowRing).  The work on
+// A CTA per row -- a cluster of up to eight where a CTA's registers do not hold one (kWide) -- and a ring of rows in shared memory, filled by asynchronous copies several rows ahead (RowRing).  The work on
 // consecutive rows overlaps, so that one barrier per row serves all its sums: while a row's sums meet, the next
 // row's are taken and the outputs of the one before are written.
 __device__ __forceinline__ void copy_ahead(void *to, const void *from)
@@ -355,28 +219,78 @@ __device__ __forceinline__ A warp_sums8(A (&v)[8])
     A s = v[0] + __shfl_xor_sync(0xFFFFFFFFu, v[0], 2);
     return s + __shfl_xor_sync(0xFFFFFFFFu, s, 1);
 }
-// kSums of the eight sums over the CTA's warps (at most 16 of them), the same in every lane
-template <int kSums, typename A>
+// The CTAs of a cluster that share a row (kWide), or the one CTA.  Every warp's sums go to the words of every CTA, so that behind
+// the barrier each has them all.
+template <bool kWide>
+struct Team {
+    static constexpr uint32_t kMostWarps = kWide ? kMaxCluster * kMaxWarps : kMaxWarps;
+    uint32_t                  ctas, rank, warps;                       // warps: of all CTAs
+    __device__ __forceinline__ Team()
+    {
+        ctas = 1, rank = 0;
+        if constexpr (kWide) {
+            asm("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(ctas));
+            asm("mov.u32 %0, %%cluster_ctaid.x;" : "=r"(rank));
+        }
+        warps = ctas * (blockDim.x / 32);
+    }
+    __device__ __forceinline__ uint32_t warp() const { return rank * (blockDim.x / 32) + threadIdx.x / 32; }
+    template <typename A>
+    __device__ __forceinline__ void put(A *word, const A v) const
+    {
+        if constexpr (kWide) {
+            for (uint32_t r = 0; r < ctas; ++r) {
+                uint32_t to;
+                asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(to) : "r"(smem_addr(word)), "r"(r));
+                if constexpr (sizeof(A) == 8) asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(to), "d"(v) : "memory");
+                else asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(v) : "memory");
+            }
+        } else {
+            *word = v;
+        }
+    }
+    __device__ __forceinline__ void sync() const
+    {
+        if constexpr (kWide) {
+            __syncwarp();
+            asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        } else {
+            __syncthreads();
+        }
+    }
+};
+// kSums of the eight sums over all warps, the same in every lane
+template <int kSums, uint32_t kMostWarps, typename A>
 __device__ __forceinline__ void cta_sums(const A (*part)[8], const uint32_t warps, A (&s)[kSums])
 {
     const uint32_t lane = threadIdx.x % 32;
     A              v    = 0;
+    if constexpr (kMostWarps <= kMaxWarps) {
 #pragma unroll
-    for (uint32_t k = 0; k < kMaxWarps / 4; ++k) {
-        const uint32_t w = k * 4 + lane / 8;
-        if (w < warps) v += part[w][lane % 8];
+        for (uint32_t k = 0; k < kMostWarps / 4; ++k) {
+            const uint32_t w = k * 4 + lane / 8;
+            if (w < warps) v += part[w][lane % 8];
+        }
+    } else {
+        for (uint32_t w = lane / 8; w < warps; w += 4) v += part[w][lane % 8];
     }
     v += __shfl_xor_sync(0xFFFFFFFFu, v, 8);
     v += __shfl_xor_sync(0xFFFFFFFFu, v, 16);
 #pragma unroll
     for (int k = 0; k < kSums; ++k) s[k] = __shfl_sync(0xFFFFFFFFu, v, k);
 }
-// the sum over a warp's lanes and over the CTA's warps, in two steps
-template <typename A>
+// the sum over all warps of one word each
+template <uint32_t kMostWarps, typename A>
 __device__ __forceinline__ A cta_sum(const A *part, const uint32_t warps)
 {
     const uint32_t lane = threadIdx.x % 32;
-    return warp_sum(lane < warps ? part[lane] : A(0));
+    if constexpr (kMostWarps <= 32) {
+        return warp_sum(lane < warps ? part[lane] : A(0));
+    } else {
+        A v = 0;
+        for (uint32_t w = lane; w < warps; w += 32) v += part[w];
+        return warp_sum(v);
+    }
 }
 
 // rows of the ring (rows that are copied by all: one more, see RowRing)
@@ -392,9 +306,10 @@ struct Columns {
     using Pair               = Two<Acc>;
     static constexpr int kP  = kVector ? kPairs<DT> : 4;
     static constexpr int kES = static_cast<int>(sizeof(Elem));
-    uint32_t t, team, d;
+    uint32_t t, team, d, first;                                        // d columns from `first` on are this CTA's
+    uint64_t row_d;                                                    // columns of a row
 
-    // the column of half `h` of pair k of hold j
+    // the column (of this CTA's) of half `h` of pair k of hold j
     __device__ __forceinline__ uint32_t column(const int j, const int k, const int h) const
     {
         return kVector ? (j * team + t) * (2 * kP) + 2 * k + h : ((j * kP + k) * 2 + h) * team + t;
@@ -405,7 +320,7 @@ struct Columns {
 #pragma unroll
         for (int k = 0; k < kP; ++k) v[k] = both(with);
     }
-    // a row of global memory that no output of the call overlaps; columns beyond it keep what v holds
+    // (this CTA's part of) a row of global memory that no output of the call overlaps; columns beyond it keep what v holds
     __device__ __forceinline__ void read(const Elem *row, const int j, Pair (&v)[kP]) const
     {
         if constexpr (kVector) {
@@ -479,12 +394,12 @@ struct RowRing {
     __device__ __forceinline__ void copy(const uint32_t stage, const int o, const void *base, const uint64_t row, const uint64_t total) const
     {
         if constexpr (kVector) {
-            const uint4 *const from = reinterpret_cast<const uint4 *>(static_cast<const unsigned char *>(base) + row * c.d * C::kES) + c.t;
+            const uint4 *const from = reinterpret_cast<const uint4 *>(static_cast<const unsigned char *>(base) + (row * c.row_d + c.first) * C::kES) + c.t;
 #pragma unroll
             for (int j = 0; j < kHold; ++j)
                 if (c.has(j, 0, 0)) copy_ahead(&vector(stage, o, j), from + j * c.team);
         } else {
-            const uint64_t begin = row * c.d * C::kES, end = begin + c.d * C::kES, all = total * C::kES;
+            const uint64_t begin = (row * c.row_d + c.first) * C::kES, end = begin + c.d * C::kES, all = total * C::kES;
             unsigned char *const to = at + (stage * kOperands + o) * slot_bytes;
             for (uint64_t b = (begin & ~15ull) + 16 * c.t; b < end; b += 16 * c.team) {
                 const uint32_t size = b + 16 <= all ? 16u : static_cast<uint32_t>(all - b);      // nothing is read behind the tensor
@@ -504,7 +419,7 @@ struct RowRing {
                 c.fill(v, 0);
                 return;
             }
-            const Elem *const from = reinterpret_cast<const Elem *>(at + (stage * kOperands + o) * slot_bytes + (row * c.d * C::kES & 15u));
+            const Elem *const from = reinterpret_cast<const Elem *>(at + (stage * kOperands + o) * slot_bytes + ((row * c.row_d + c.first) * C::kES & 15u));
 #pragma unroll
             for (int k = 0; k < C::kP; ++k)
                 v[k] = Pair::of(c.has(j, k, 0) ? static_cast<typename C::Acc>(Num<DT>::widen(from[c.column(j, k, 0)])) : typename C::Acc(0),
@@ -526,13 +441,13 @@ __device__ __forceinline__ void branch_factors(const NormArgs &a, const uint64_t
         c.fill(gw[j], static_cast<typename C::Acc>(a.scale));
         if (a.w_post) {
             c.fill(w, 1);
-            c.read(static_cast<const Elem *>(a.w_post), j, w);
+            c.read(static_cast<const Elem *>(a.w_post) + c.first, j, w);
 #pragma unroll
             for (int k = 0; k < C::kP; ++k) gw[j][k] = gw[j][k] * w[k];
         }
         if (!kRowGate && a.gate) {
             c.fill(w, 1);
-            c.read(static_cast<const Elem *>(a.gate) + group * a.d, j, w);
+            c.read(static_cast<const Elem *>(a.gate) + group * a.d + c.first, j, w);
 #pragma unroll
             for (int k = 0; k < C::kP; ++k) gw[j][k] = gw[j][k] * w[k];
         }
@@ -541,9 +456,9 @@ __device__ __forceinline__ void branch_factors(const NormArgs &a, const uint64_t
 
 // Forward.  In one turn of the loop: the sum of f^2 of a row, x' and its sum of the row before, n of the row before that.
 // kRowGate: the gate changes from row to row and comes through the ring like a third operand.
-template <int DT, int kHold, bool kVector, bool kRowGate>
+template <int DT, int kHold, bool kVector, bool kRowGate, bool kWide>
 __global__ void __launch_bounds__(kMaxTeam, 1)
-block_norm_fwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
+block_norm_fwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes, const uint32_t columns)
 {
     in_stream_order();
     using C    = Columns<DT, kHold, kVector>;
@@ -553,22 +468,24 @@ block_norm_fwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
     constexpr int kP = C::kP, kOperands = kRowGate ? 3 : 2;
     using Ring = RowRing<DT, kHold, kVector, kOperands>;
     extern __shared__ uint4 shared[];
-    __shared__ Acc part[2][2][kMaxWarps];                              // [turn][of f, of x'][warp]
-    const uint32_t t = threadIdx.x, warps = blockDim.x / 32;
-    const C        c{t, blockDim.x, static_cast<uint32_t>(a.d)};
+    using T = Team<kWide>;
+    const T    team;
+    __shared__ Acc part[2][2][T::kMostWarps];                          // [turn][of f, of x'][warp]
+    const uint32_t t = threadIdx.x, warps = team.warps, mine0 = team.rank * columns, cluster = blockIdx.x / team.ctas, clusters = gridDim.x / team.ctas;
+    const C        c{t, blockDim.x, kWide ? (a.d > mine0 ? (a.d - mine0 < columns ? static_cast<uint32_t>(a.d - mine0) : columns) : 0u) : static_cast<uint32_t>(a.d), mine0, a.d};
     const Ring     ring(c, shared, slot_bytes);
     const Acc      eps = static_cast<Acc>(a.eps), of_d = Acc(1) / static_cast<Acc>(a.d);
     const uint64_t total = a.rows * a.d;
     const Extent   all_x = extent_of(a.x_out, total * sizeof(Elem)), all_n = extent_of(a.n_out, total * sizeof(Elem));
 
-    uint64_t next = blockIdx.x;                                        // the row to copy next
+    uint64_t next = cluster;                                        // the row to copy next
     // (a commit for every turn, also behind the last row: the waits count groups)
     const auto fill = [&](const uint32_t stage) {
         if (next < a.rows) {
             ring.copy(stage, 0, a.x, next, total);
             if (a.f) ring.copy(stage, 1, a.f, next, total);
             if constexpr (kRowGate) ring.copy(stage, 2, a.gate, next / a.gate_rows, round_up_div(a.rows, a.gate_rows) * a.d);
-            next += gridDim.x;
+            next += clusters;
         }
         copy_commit();
     };
@@ -583,19 +500,20 @@ block_norm_fwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
 #pragma unroll
     for (int j = 0; j < kHold; ++j) {
         c.fill(w_pre[j], 1);
-        if (a.w_pre) c.read(static_cast<const Elem *>(a.w_pre), j, w_pre[j]);
+        if (a.w_pre) c.read(static_cast<const Elem *>(a.w_pre) + c.first, j, w_pre[j]);
     }
     if constexpr (!kVector) {                                          // the first row, copied by all
         copy_wait<Ring::kBehind + 1>();
         __syncthreads();
     }
-    const uint64_t mine = (a.rows - blockIdx.x + gridDim.x - 1) / gridDim.x;      // rows of this CTA (the grid is not wider than the rows)
-    const uint64_t stride = static_cast<uint64_t>(gridDim.x) * a.d;
-    uint64_t       row = blockIdx.x, at_y = row * a.d, at_n = at_y;    // of the turn; where the rows written next begin
+    if constexpr (kWide) team.sync();                                  // every CTA of the cluster has begun: its words may be written
+    const uint64_t mine = (a.rows - cluster + clusters - 1) / clusters;           // rows of this CTA (there are no more clusters than rows)
+    const uint64_t stride = static_cast<uint64_t>(clusters) * a.d;
+    uint64_t       row = cluster, at_y = row * a.d + c.first, at_n = at_y;    // of the turn; where the rows written next begin
     uint32_t       stage_a = 0, stage_b = 0, stage_c = Ring::stages - 1;
-    for (uint64_t turn = 0; turn < mine + 2; ++turn, row += gridDim.x) {
-        const Acc(*const before)[kMaxWarps] = part[(turn & 1) ^ 1];
-        Acc(*const now)[kMaxWarps]          = part[turn & 1];
+    for (uint64_t turn = 0; turn < mine + 2; ++turn, row += clusters) {
+        const Acc(*const before)[T::kMostWarps] = part[(turn & 1) ^ 1];
+        Acc(*const now)[T::kMostWarps]          = part[turn & 1];
         if (turn < mine) {
             if constexpr (kVector) copy_wait<Ring::kBehind>();
             if (a.w_post) {
@@ -608,12 +526,12 @@ block_norm_fwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
                     for (int k = 0; k < kP; ++k) s = fma2(f[k], f[k], s);
                 }
                 const Acc v = warp_sum(s.low() + s.high());
-                if (t % 32 == 0) now[0][t / 32] = v;
+                if (t % 32 == 0) team.put(&now[0][team.warp()], v);
             }
         }
         if (turn >= 2 && a.n_out) {
             // ---- n of the row two before, whose x' waits in y
-            const Pair r = both(root_of(cta_sum(before[1], warps) * of_d + eps));
+            const Pair r = both(root_of(cta_sum<T::kMostWarps>(before[1], warps) * of_d + eps));
 #pragma unroll
             for (int j = 0; j < kHold; ++j) {
                 Pair n[kP];
@@ -625,8 +543,8 @@ block_norm_fwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
         }
         if (turn >= 1 && turn <= mine) {
             // ---- x' of the row before
-            const uint64_t before_row = row - gridDim.x;
-            const Pair     rf = both(a.w_post ? root_of(cta_sum(before[0], warps) * of_d + eps) : Acc(1));
+            const uint64_t before_row = row - clusters;
+            const Pair     rf = both(a.w_post ? root_of(cta_sum<T::kMostWarps>(before[0], warps) * of_d + eps) : Acc(1));
             Pair           s  = both(Acc(0));
 #pragma unroll
             for (int j = 0; j < kHold; ++j) {
@@ -649,12 +567,12 @@ block_norm_fwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
             at_y += stride;
             if (a.n_out) {
                 const Acc v = warp_sum(s.low() + s.high());
-                if (t % 32 == 0) now[1][t / 32] = v;
+                if (t % 32 == 0) team.put(&now[1][team.warp()], v);
             }
             stage_b = stage_b + 1 == Ring::stages ? 0 : stage_b + 1;
         }
         if constexpr (!kVector) copy_wait<Ring::kBehind>();            // the next row's copies, those of all with the barrier
-        __syncthreads();                                               // this turn's sums are there; those of the turn before are free
+        team.sync();                                                   // this turn's sums are there; those of the turn before are free
         fill(stage_c);
         stage_c = stage_c + 1 == Ring::stages ? 0 : stage_c + 1;
         stage_a = stage_a + 1 == Ring::stages ? 0 : stage_a + 1;
@@ -663,9 +581,9 @@ block_norm_fwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
 
 // Backward, over the rows of a chunk.  In one turn of the loop: the six sums of a row, the outputs of the row before.
 // kRowGate: the gate changes from row to row and comes through the ring like a fifth operand.
-template <int DT, int kHold, bool kVector, bool kRowGate>
+template <int DT, int kHold, bool kVector, bool kRowGate, bool kWide>
 __global__ void __launch_bounds__(kMaxTeam, 1)
-block_norm_bwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
+block_norm_bwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes, const uint32_t columns)
 {
     in_stream_order();
     using C    = Columns<DT, kHold, kVector>;
@@ -675,9 +593,11 @@ block_norm_bwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
     constexpr int kP = C::kP, kOperands = kRowGate ? 5 : 4;
     using Ring = RowRing<DT, kHold, kVector, kOperands>;
     extern __shared__ uint4 shared[];
-    __shared__ Acc part[2][kMaxWarps][8];
-    const uint32_t t = threadIdx.x, chunk = blockIdx.x, warps = blockDim.x / 32;
-    const C        c{t, blockDim.x, static_cast<uint32_t>(a.d)};
+    using T = Team<kWide>;
+    const T    team;
+    __shared__ Acc part[2][T::kMostWarps][8];
+    const uint32_t t = threadIdx.x, warps = team.warps, mine0 = team.rank * columns, chunk = blockIdx.x / team.ctas;
+    const C        c{t, blockDim.x, kWide ? (a.d > mine0 ? (a.d - mine0 < columns ? static_cast<uint32_t>(a.d - mine0) : columns) : 0u) : static_cast<uint32_t>(a.d), mine0, a.d};
     const Ring     ring(c, shared, slot_bytes);
     const Acc      scale = static_cast<Acc>(a.scale), eps = static_cast<Acc>(a.eps), of_d = Acc(1) / static_cast<Acc>(a.d);
     const uint64_t total = a.rows * a.d, gates = round_up_div(a.rows, a.gate_rows) * a.d;
@@ -711,7 +631,7 @@ block_norm_bwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
 #pragma unroll
     for (int j = 0; j < kHold; ++j) {
         c.fill(w_pre[j], 1);
-        if (a.w_pre) c.read(static_cast<const Elem *>(a.w_pre), j, w_pre[j]);
+        if (a.w_pre) c.read(static_cast<const Elem *>(a.w_pre) + c.first, j, w_pre[j]);
     }
     // a row's operands
     const auto operands = [&](const uint32_t stage, const uint64_t row, const int j, Pair (&x)[kP], Pair (&f)[kP], Pair (&dn)[kP], Pair (&dy)[kP], Pair (&g)[kP]) {
@@ -731,8 +651,9 @@ block_norm_bwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
         copy_wait<Ring::kBehind + 1>();
         __syncthreads();
     }
+    if constexpr (kWide) team.sync();                                  // every CTA of the cluster has begun: its words may be written
     uint32_t stage_a = 0, stage_b = 0, stage_c = Ring::stages - 1;     // of the row whose sums are taken, of the one before, to fill
-    uint64_t at_out = rows.first * a.d;
+    uint64_t at_out = rows.first * a.d + c.first;
     for (uint64_t row = rows.first; row <= rows.end; ++row) {
         if (row < rows.end) {
             // ---- this row's sums
@@ -761,13 +682,13 @@ block_norm_bwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
 #pragma unroll
             for (int k = 0; k < 6; ++k) s[k] = p[k].low() + p[k].high();
             const Acc v = warp_sums8(s);
-            if (t % 4 == 0) part[row & 1][t / 32][t % 32 / 4] = v;
+            if (t % 4 == 0) team.put(&part[row & 1][team.warp()][t % 32 / 4], v);
         }
         if (row > rows.first) {
             // ---- the row before: its outputs
             const uint64_t before = row - 1;
             Acc            s[6];
-            cta_sums(part[before & 1], warps, s);
+            cta_sums<6, T::kMostWarps>(part[before & 1], warps, s);
             const RowFactors<Acc> q = factors_of(s, of_d, eps, a.w_post != nullptr);
             const Pair r = both(q.r), rrc = both(-q.rrc), rf = both(q.rf), rf3m = both(-q.rf3m);
 #pragma unroll
@@ -797,21 +718,21 @@ block_norm_bwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
                 for (int j = 0; j < kHold; ++j) {
                     Pair w[kP], g[kP];
                     c.fill(w, 1);
-                    if (a.w_post) c.read(static_cast<const Elem *>(a.w_post), j, w);
+                    if (a.w_post) c.read(static_cast<const Elem *>(a.w_post) + c.first, j, w);
                     if constexpr (kRowGate) ring.read(stage_b, 4, j, group, true, g);
 #pragma unroll
                     for (int k = 0; k < kP; ++k) {
                         w[k] = w[k] * both(scale) * sum_f[j][k];
                         if constexpr (kRowGate) sum_post[j][k] = fma2(both(scale) * g[k], sum_f[j][k], sum_post[j][k]), sum_f[j][k] = both(Acc(0));
                     }
-                    if (a.dgate && whole) c.write(static_cast<Elem *>(a.dgate) + group * a.d, j, w, all_g);
-                    if (a.dgate && !whole) c.write_sums(reinterpret_cast<Acc *>(a.part_gate) + to * a.d, j, w, part_g);
+                    if (a.dgate && whole) c.write(static_cast<Elem *>(a.dgate) + group * a.d + c.first, j, w, all_g);
+                    if (a.dgate && !whole) c.write_sums(reinterpret_cast<Acc *>(a.part_gate) + to * a.d + c.first, j, w, part_g);
                 }
             }
             stage_b = stage_b + 1 == Ring::stages ? 0 : stage_b + 1;
         }
         if constexpr (!kVector) copy_wait<Ring::kBehind>();            // the next row's copies, those of all with the barrier
-        __syncthreads();                                               // the sums of this row are there; the words of the one before are free
+        team.sync();                                                   // the sums of this row are there; the words of the one before are free
         fill(stage_c);
         stage_c = stage_c + 1 == Ring::stages ? 0 : stage_c + 1;
         stage_a = stage_a + 1 == Ring::stages ? 0 : stage_a + 1;
@@ -821,144 +742,23 @@ block_norm_bwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes)
         if (!kRowGate && a.dw_post) {
             Pair g[kP];
             c.fill(g, 1);
-            if (a.gate) c.read(static_cast<const Elem *>(a.gate) + of_chunk * a.d, j, g);
+            if (a.gate) c.read(static_cast<const Elem *>(a.gate) + of_chunk * a.d + c.first, j, g);
 #pragma unroll
             for (int k = 0; k < kP; ++k) sum_f[j][k] = sum_f[j][k] * both(scale) * g[k];
         }
-        if (a.dw_pre) c.write_sums(reinterpret_cast<Acc *>(a.part_pre) + chunk * a.d, j, sum_pre[j], part_w);
-        if (a.dw_post) c.write_sums(reinterpret_cast<Acc *>(a.part_post) + chunk * a.d, j, kRowGate ? sum_post[kRowGate ? j : 0] : sum_f[j], part_p);
+        if (a.dw_pre) c.write_sums(reinterpret_cast<Acc *>(a.part_pre) + chunk * a.d + c.first, j, sum_pre[j], part_w);
+        if (a.dw_post) c.write_sums(reinterpret_cast<Acc *>(a.part_post) + chunk * a.d + c.first, j, kRowGate ? sum_post[kRowGate ? j : 0] : sum_f[j], part_p);
     }
 }
 
-// kHold accesses of every operand per thread, held in registers with the column sums.
-template <int DT, bool kVector, int kHold, bool kCta>
-__global__ void __launch_bounds__(kCta ? kMaxTeam : 32 * kWarpTeams)
-block_norm_bwd_kernel(const NormArgs a)
-{
-    in_stream_order();
-    using X                = Access<DT, kVector>;
-    using Elem             = typename X::Elem;
-    using Acc              = typename X::Acc;
-    constexpr int  kW      = X::kW;
-    __shared__ Acc words[2][6][kMaxWarps];
-    uint32_t       turn    = 0;
-    const uint32_t team    = kCta ? blockDim.x : 32;
-    const uint32_t t       = kCta ? threadIdx.x : threadIdx.x % 32;
-    const uint32_t chunk   = kCta ? blockIdx.x : blockIdx.x * (blockDim.x / 32) + threadIdx.x / 32;
-    const uint32_t count   = static_cast<uint32_t>(a.d / kW);
-    const Acc      scale = static_cast<Acc>(a.scale), eps = static_cast<Acc>(a.eps), of_d = Acc(1) / static_cast<Acc>(a.d);
-    const uint64_t bytes = a.rows * a.d * sizeof(Elem);
-    const Extent   all_x = extent_of(a.x_out, bytes), all_f = extent_of(a.n_out, bytes);
-    const Extent   all_g = extent_of(a.dgate, round_up_div(a.rows, a.gate_rows) * a.d * sizeof(Elem));
-    const Extent   part_g = extent_of(a.part_gate, 2ull * a.chunks * a.d * sizeof(Acc));
-    const Extent   part_w = extent_of(a.part_pre, a.chunks * a.d * sizeof(Acc)), part_p = extent_of(a.part_post, a.chunks * a.d * sizeof(Acc));
-    if (chunk >= a.chunks) return;                                     // (a whole team; a CTA team is a CTA)
-    const Chunk c = chunk_of(a, chunk);
-    Acc         sum_pre[kHold][kW] = {}, sum_post[kHold][kW] = {}, sum_gate[kHold][kW] = {};
-    for (uint64_t row = c.first; row < c.end; ++row) {
-        const void *x = row_of<Elem>(a.x, row, a.d), *f = row_of<Elem>(a.f, row, a.d);
-        const void *dn = row_of<Elem>(a.dn, row, a.d), *dy = row_of<Elem>(a.dy, row, a.d);
-        const uint64_t group = row / a.gate_rows;
-        const void    *gate  = a.gate ? row_of<Elem>(a.gate, group, a.d) : nullptr;
-        // the operands wait in registers as they lie in memory; weights and gate are read again from the L1
-        typename X::Raw xr[kHold], fr[kHold], nr[kHold], yr[kHold];
-        Acc             s[6] = {};
-#pragma unroll
-        for (int j = 0; j < kHold; ++j) {
-            const uint32_t i = j * team + t;
-            if (i >= count) continue;
-            xr[j] = X::load(x, i);
-            if (f) fr[j] = X::load(f, i);
-            if (dn) nr[j] = X::load(dn, i);
-            if (dy) yr[j] = X::load(dy, i);
-        }
-        // element values of access j: x', f, dx', dn, w_pre, scale * gate, w_post
-        const auto element = [&](const int j, Acc (&xv)[kW], Acc (&fv)[kW], Acc (&dyv)[kW], Acc (&dnv)[kW], Acc (&wpre)[kW], Acc (&gw)[kW], Acc (&pw)[kW]) {
-            const uint32_t i = j * team + t;
-#pragma unroll
-            for (int k = 0; k < kW; ++k) fv[k] = dnv[k] = dyv[k] = 0, wpre[k] = pw[k] = gw[k] = 1;
-            X::widen(xr[j], xv);
-            if (f) X::widen(fr[j], fv);
-            if (dn) X::widen(nr[j], dnv), X::read_shared(a.w_pre, i, wpre);
-            if (dy) X::widen(yr[j], dyv);
-            if (a.w_post) X::read_shared(a.w_post, i, pw);
-            if (gate) X::read_shared(gate, i, gw);
-#pragma unroll
-            for (int k = 0; k < kW; ++k) gw[k] *= scale;
-        };
-#pragma unroll
-        for (int j = 0; j < kHold; ++j) {
-            if (j * team + t >= count) continue;
-            Acc xv[kW], fv[kW], dyv[kW], dnv[kW], wpre[kW], gw[kW], pw[kW];
-            element(j, xv, fv, dyv, dnv, wpre, gw, pw);
-#pragma unroll
-            for (int k = 0; k < kW; ++k) add_sums(s, xv[k], fv[k], dyv[k], dnv[k] * wpre[k], gw[k] * pw[k]);
-        }
-        team_sums<kCta>(s, words, turn);
-        const RowFactors<Acc> q = factors_of(s, of_d, eps, a.w_post != nullptr);
-        void *dx = row_of<Elem>(a.x_out, row, a.d), *df = row_of<Elem>(a.n_out, row, a.d);
-#pragma unroll
-        for (int j = 0; j < kHold; ++j) {
-            const uint32_t i = j * team + t;
-            if (i >= count) continue;
-            Acc xv[kW], fv[kW], dyv[kW], dnv[kW], wpre[kW], gw[kW], pw[kW];
-            element(j, xv, fv, dyv, dnv, wpre, gw, pw);
-#pragma unroll
-            for (int k = 0; k < kW; ++k) {
-                const Acc tv = dyv[k] + q.r * (dnv[k] * wpre[k]) - q.rrc * xv[k];
-                sum_pre[j][k] += dnv[k] * (xv[k] * q.r);
-                const Acc fh = fv[k] * q.rf, dp = tv * gw[k];
-                sum_gate[j][k] += scale * tv * (fh * pw[k]);
-                sum_post[j][k] += dp * fh;
-                fv[k]  = dp * pw[k] * q.rf - q.rf3m * fv[k];
-                dyv[k] = tv;
-            }
-            if (dx) X::store(dx, i, dyv, all_x);
-            if (df) X::store(df, i, fv, all_f);
-        }
-        // the last of the group's rows in this chunk: its gate's gradient, or this chunk's share of it
-        if (a.dgate && (row + 1 == c.end || (row + 1) % a.gate_rows == 0)) {
-            uint64_t   slot;
-            const bool whole = whole_group(a, c, group, chunk, slot);
-#pragma unroll
-            for (int j = 0; j < kHold; ++j) {
-                const uint32_t i = j * team + t;
-                if (i < count) {
-                    if (whole) X::store(row_of<Elem>(a.dgate, group, a.d), i, sum_gate[j], all_g);
-                    else
-#pragma unroll
-                        for (int k = 0; k < kW; ++k) {
-                            Acc *const o = reinterpret_cast<Acc *>(a.part_gate) + slot * a.d + i * kW + k;
-                            if (part_g.holds(o, sizeof(Acc))) *o = sum_gate[j][k];
-                        }
-                }
-#pragma unroll
-                for (int k = 0; k < kW; ++k) sum_gate[j][k] = 0;
-            }
-        }
-    }
-#pragma unroll
-    for (int j = 0; j < kHold; ++j) {
-        const uint32_t i = j * team + t;
-        if (i >= count) continue;
-#pragma unroll
-        for (int k = 0; k < kW; ++k) {
-            const uint64_t o = chunk * a.d + i * kW + k;
-            if (a.dw_pre && part_w.holds(reinterpret_cast<Acc *>(a.part_pre) + o, sizeof(Acc))) reinterpret_cast<Acc *>(a.part_pre)[o] = sum_pre[j][k];
-            if (a.dw_post && part_p.holds(reinterpret_cast<Acc *>(a.part_post) + o, sizeof(Acc))) reinterpret_cast<Acc *>(a.part_post)[o] = sum_post[j][k];
-        }
-    }
-}
-
-// Rows longer than a CTA's registers: dx and df by a kernel that reads a row twice and leaves its factors behind ...
+// Rows that the ring kernel does not hold: dx and df by a kernel that reads a row twice and leaves its factors behind ...
 template <int DT>
 __global__ void __launch_bounds__(kMaxTeam)
 block_norm_bwd_rows_kernel(const NormArgs a)
 {
     in_stream_order();
-    using X    = Access<DT, false>;
-    using Elem = typename X::Elem;
-    using Acc  = typename X::Acc;
+    using Elem = typename Num<DT>::Elem;
+    using Acc  = typename Num<DT>::Acc;
     __shared__ Acc words[2][6][kMaxWarps];
     uint32_t       turn = 0;
     const Acc      scale = static_cast<Acc>(a.scale), eps = static_cast<Acc>(a.eps), of_d = Acc(1) / static_cast<Acc>(a.d);
@@ -973,16 +773,15 @@ block_norm_bwd_rows_kernel(const NormArgs a)
         Acc         s[6] = {};
         for (uint64_t i = threadIdx.x; i < a.d; i += blockDim.x)
             add_sums(s, at(x, i, 0), at(f, i, 0), at(dy, i, 0), dn ? at(dn, i, 0) * at(w_pre, i, 1) : Acc(0), scale * at(gate, i, 1) * at(w_post, i, 1));
-        team_sums<true>(s, words, turn);
+        team_sums(s, words, turn);
         const RowFactors<Acc> q = factors_of(s, of_d, eps, w_post != nullptr);
         if (threadIdx.x == 0 && all_s.holds(static_cast<RowFactors<Acc> *>(a.stats) + row, sizeof(q))) static_cast<RowFactors<Acc> *>(a.stats)[row] = q;
-        void *dx = row_of<Elem>(a.x_out, row, a.d), *df = row_of<Elem>(a.n_out, row, a.d);
+        Elem *dx = static_cast<Elem *>(row_of<Elem>(a.x_out, row, a.d)), *df = static_cast<Elem *>(row_of<Elem>(a.n_out, row, a.d));
         for (uint64_t i = threadIdx.x; i < a.d; i += blockDim.x) {
             const Acc xv = at(x, i, 0), wn = dn ? at(dn, i, 0) * at(w_pre, i, 1) : Acc(0), gw = scale * at(gate, i, 1) * at(w_post, i, 1);
-            Acc       t[1] = {at(dy, i, 0) + q.r * wn - q.rrc * xv};
-            Acc       o[1] = {t[0] * gw * q.rf - q.rf3m * at(f, i, 0)};
-            if (dx) X::store(dx, static_cast<uint32_t>(i), t, all_x);
-            if (df) X::store(df, static_cast<uint32_t>(i), o, all_f);
+            const Acc tv = at(dy, i, 0) + q.r * wn - q.rrc * xv;
+            if (dx && all_x.holds(dx + i, sizeof(Elem))) dx[i] = Num<DT>::narrow(tv);
+            if (df && all_f.holds(df + i, sizeof(Elem))) df[i] = Num<DT>::narrow(tv * gw * q.rf - q.rf3m * at(f, i, 0));
         }
     }
 }
@@ -1093,9 +892,6 @@ block_norm_finish_kernel(const NormArgs a)
 }
 
 // ---------------------------------------------------------------------------------------------- host side
-constexpr uint32_t kMaxChunks  = 4096;      // chunks of rows of a backward pass
-constexpr uint32_t kLongChunks = 64;        // the same for rows longer than a CTA's registers
-
 // threads of a CTA that holds `count` accesses, `hold` per thread
 uint32_t team_of(uint64_t count, uint32_t hold) { return static_cast<uint32_t>(round_up_div(round_up_div(count, hold), 32) * 32); }
 // Vectors per thread of the ring kernels: two from 64 on, which halves what the sums over a row cost per element; CTAs of an SM:
@@ -1106,57 +902,64 @@ constexpr size_t kMostShared = 220 * 1024;
 // How a ring kernel takes rows of d elements: hold 0 if it cannot.
 struct RingPlan {
     uint32_t hold, team, slot;     // slot: bytes of an operand's row, rows of single elements
+    uint32_t ctas, columns;        // of a cluster; of a CTA
     size_t   smem;
 };
 RingPlan ring_plan(uint64_t d, int es, uint32_t operands)
 {
-    const uint64_t lanes = 16 / static_cast<uint64_t>(es);
+    const uint64_t lanes  = 16 / static_cast<uint64_t>(es);
+    const bool     vector = d % lanes == 0;
     RingPlan       p{};
-    if (d % lanes == 0) {
-        const uint64_t count = d / lanes;
-        if (count > 2 * kMaxTeam) return p;
-        p.hold = hold_of(count), p.team = team_of(count, p.hold);
-        p.smem = static_cast<size_t>(p.hold == 1 ? kRingStages<1, true> : kRingStages<2, true>) * operands * p.hold * p.team * 16;
-    } else {
-        if (d > 16 * kMaxTeam) return p;
-        p.hold = d <= 8 * kMaxTeam ? 1 : 2, p.team = team_of(d, 8 * p.hold);
-        p.slot = static_cast<uint32_t>((d * static_cast<uint64_t>(es) + 15) / 16 * 16 + 16);
-        p.smem = static_cast<size_t>(kRingStages<1, false>) * operands * p.slot;
+    for (uint32_t ctas = 1; ctas <= kMaxCluster; ctas *= 2) {
+        const uint64_t columns = vector ? round_up_div(d / lanes, ctas) * lanes : round_up_div(d, ctas);
+        const uint64_t count   = vector ? columns / lanes : columns;
+        if (count > (vector ? 2u : 16u) * kMaxTeam) continue;
+        p.ctas = ctas, p.columns = static_cast<uint32_t>(columns);
+        p.hold = vector ? (ctas > 1 ? 2 : hold_of(count)) : count <= 8 * kMaxTeam ? 1 : 2;
+        p.team = team_of(count, (vector ? 1 : 8) * p.hold);
+        p.slot = vector ? 0 : static_cast<uint32_t>((columns * static_cast<uint64_t>(es) + 15) / 16 * 16 + 16);
+        p.smem = vector ? static_cast<size_t>(p.hold == 1 ? kRingStages<1, true> : kRingStages<2, true>) * operands * p.hold * p.team * 16
+                        : static_cast<size_t>(kRingStages<1, false>) * operands * p.slot;
+        if (p.smem <= kMostShared) return p;
     }
-    if (p.smem > kMostShared) p.hold = 0;
+    p.hold = 0;
     return p;
 }
-
-// Can a CTA's registers hold a row of the backward pass?
-bool row_fits(uint64_t d, int es)
-{
-    const uint64_t lanes = 16 / static_cast<uint64_t>(es);
-    return d % lanes == 0 ? d <= 2 * lanes * kMaxTeam : d <= 8 * kMaxTeam || ring_plan(d, es, 5).hold != 0;
-}
+// Does a backward pass go through the ring, whatever its gate?
+bool row_fits(uint64_t d, int es) { return ring_plan(d, es, 5).hold != 0; }
+// 512 threads an SM at a time (three CTAs of 256 where the registers allow them: bf16 16384 x 4096 forward 97 us against 85)
+uint64_t resident_teams(const RingPlan &p, int sms) { return static_cast<uint64_t>(sms) * (kMaxTeam / p.team) / p.ctas; }
 
 template <typename K>
-cudaError_t start_ring(K kernel, const NormArgs &a, unsigned grid, const RingPlan &p, cudaStream_t stream)
+cudaError_t start_ring(K kernel, const NormArgs &a, uint64_t teams, const RingPlan &p, cudaStream_t stream)
 {
     const cudaError_t e = reported(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(p.smem)));
-    return e != cudaSuccess ? e : launch(kernel, grid, p.team, p.smem, stream, a, p.slot);
+    if (e != cudaSuccess) return e;
+    const unsigned grid = static_cast<unsigned>(teams * p.ctas);
+    if (p.ctas == 1) return launch(kernel, grid, p.team, p.smem, stream, a, p.slot, p.columns);
+    cudaLaunchAttribute attr[2];
+    attr[0].id                                         = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id                                         = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x                           = p.ctas;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cudaLaunchConfig_t c{};
+    c.gridDim = dim3(grid), c.blockDim = dim3(p.team), c.dynamicSmemBytes = p.smem, c.stream = stream;
+    c.attrs = attr, c.numAttrs = 2;
+    return reported(cudaLaunchKernelEx(&c, kernel, a, p.slot, p.columns));
 }
 
-// go(hold, whether rows are whole vectors)
+// go(hold, whether rows are whole vectors, whether clusters share rows)
 template <typename F>
 cudaError_t with_ring(const RingPlan &p, bool vector, const F &go)
 {
-    using std::bool_constant;
-    using std::integral_constant;
-    if (p.hold == 1) return vector ? go(integral_constant<int, 1>(), bool_constant<true>()) : go(integral_constant<int, 1>(), bool_constant<false>());
-    return vector ? go(integral_constant<int, 2>(), bool_constant<true>()) : go(integral_constant<int, 2>(), bool_constant<false>());
-}
-
-template <int DT, bool kVector, int kHold, bool kCta>
-cudaError_t start_fwd(const NormArgs &a, uint32_t threads, int sms, cudaStream_t stream)
-{
-    const uint64_t teams = kCta ? 1 : kWarpTeams, want = round_up_div(a.rows, teams);
-    const uint64_t most  = static_cast<uint64_t>(sms) * (2048 / threads);
-    return launch(block_norm_fwd_kernel<DT, kVector, kHold, kCta>, static_cast<unsigned>(want < most ? want : most), threads, 0, stream, a);
+    using One  = std::integral_constant<int, 1>;
+    using More = std::integral_constant<int, 2>;
+    using Yes  = std::bool_constant<true>;
+    using No   = std::bool_constant<false>;
+    if (p.ctas > 1) return vector ? go(More(), Yes(), Yes()) : p.hold == 1 ? go(One(), No(), Yes()) : go(More(), No(), Yes());
+    if (p.hold == 1) return vector ? go(One(), Yes(), No()) : go(One(), No(), No());
+    return vector ? go(More(), Yes(), No()) : go(More(), No(), No());
 }
 
 template <int DT>
@@ -1164,62 +967,48 @@ cudaError_t forward(const NormArgs &a, cudaStream_t stream)
 {
     const int sms = sm_count();
     if (sms == 0) return cudaErrorInvalidDevice;
-    const uint64_t count    = a.d / kLanes<DT>;
-    const bool     vector   = a.d % kLanes<DT> == 0, row_gate = a.gate && a.gate_rows < a.rows;
-    const RingPlan p        = ring_plan(a.d, static_cast<int>(sizeof(typename Num<DT>::Elem)), row_gate ? 3 : 2);
-    if (p.hold != 0) {
-        // 512 threads an SM (three CTAs of 256 where the registers allow them: bf16 16384 x 4096 97 us against 86)
-        const uint32_t resident = kMaxTeam / p.team;
-        const uint64_t most     = static_cast<uint64_t>(sms) * (resident < 1 ? 1 : resident);
-        const unsigned grid     = static_cast<unsigned>(a.rows < most ? a.rows : most);
-        const auto     go   = [&](auto hold, auto vec) {
-            return row_gate ? start_ring(block_norm_fwd_ring_kernel<DT, decltype(hold)::value, decltype(vec)::value, true>, a, grid, p, stream)
-                            : start_ring(block_norm_fwd_ring_kernel<DT, decltype(hold)::value, decltype(vec)::value, false>, a, grid, p, stream);
-        };
-        return with_ring(p, vector, go);
+    const bool     vector = a.d % kLanes<DT> == 0, row_gate = a.gate && a.gate_rows < a.rows;
+    const RingPlan p      = ring_plan(a.d, static_cast<int>(sizeof(typename Num<DT>::Elem)), row_gate ? 3 : 2);
+    if (p.hold == 0) {
+        const uint64_t most = static_cast<uint64_t>(sms) * 4;
+        return launch(block_norm_fwd_long_kernel<DT>, static_cast<unsigned>(a.rows < most ? a.rows : most), kMaxTeam, 0, stream, a);
     }
-    if (vector) {
-        if (count <= 4 * kMaxTeam) return start_fwd<DT, true, 4, true>(a, team_of(count, 4), sms, stream);
-        return start_fwd<DT, true, 0, true>(a, kMaxTeam, sms, stream);
-    }
-    // (single elements whose ring does not fit shared memory)
-    if (a.d <= 4 * kMaxTeam) return start_fwd<DT, false, 4, true>(a, team_of(a.d, 4), sms, stream);
-    return start_fwd<DT, false, 0, true>(a, kMaxTeam, sms, stream);
+    const uint64_t most  = resident_teams(p, sms);
+    const uint64_t teams = a.rows < most ? a.rows : most > 0 ? most : 1;
+    return with_ring(p, vector, [&](auto hold, auto vec, auto wide) {
+        constexpr int  kHold = decltype(hold)::value;
+        constexpr bool kVec = decltype(vec)::value, kWide = decltype(wide)::value;
+        return row_gate ? start_ring(block_norm_fwd_ring_kernel<DT, kHold, kVec, true, kWide>, a, teams, p, stream)
+                        : start_ring(block_norm_fwd_ring_kernel<DT, kHold, kVec, false, kWide>, a, teams, p, stream);
+    });
 }
 
-template <int DT, bool kVector, int kHold, bool kCta>
-cudaError_t start_bwd(const NormArgs &a, uint32_t threads, cudaStream_t stream)
-{
-    const uint32_t teams = kCta ? 1 : kWarpTeams;
-    return launch(block_norm_bwd_kernel<DT, kVector, kHold, kCta>, static_cast<unsigned>(round_up_div(a.chunks, teams)), threads, 0, stream, a);
-}
-
-// rows that a CTA's registers hold (row_fits)
+// rows that the ring holds (row_fits)
 template <int DT>
-cudaError_t bwd_of(const NormArgs &a, cudaStream_t stream)
+cudaError_t bwd_ring(const NormArgs &a, cudaStream_t stream)
 {
     const bool     vector = a.d % kLanes<DT> == 0, row_gate = a.gate && !a.group_chunks;
     const RingPlan p      = ring_plan(a.d, static_cast<int>(sizeof(typename Num<DT>::Elem)), row_gate ? 5 : 4);
-    if (p.hold != 0) {
-        const auto go = [&](auto hold, auto vec) {
-            return row_gate ? start_ring(block_norm_bwd_ring_kernel<DT, decltype(hold)::value, decltype(vec)::value, true>, a, a.chunks, p, stream)
-                            : start_ring(block_norm_bwd_ring_kernel<DT, decltype(hold)::value, decltype(vec)::value, false>, a, a.chunks, p, stream);
-        };
-        return with_ring(p, vector, go);
-    }
-    // (the operands of such rows do not fit shared memory several times)
-    return vector ? start_bwd<DT, true, 2, true>(a, team_of(a.d / kLanes<DT>, 2), stream) : start_bwd<DT, false, 8, true>(a, team_of(a.d, 8), stream);
+    return with_ring(p, vector, [&](auto hold, auto vec, auto wide) {
+        constexpr int  kHold = decltype(hold)::value;
+        constexpr bool kVec = decltype(vec)::value, kWide = decltype(wide)::value;
+        return row_gate ? start_ring(block_norm_bwd_ring_kernel<DT, kHold, kVec, true, kWide>, a, a.chunks, p, stream)
+                        : start_ring(block_norm_bwd_ring_kernel<DT, kHold, kVec, false, kWide>, a, a.chunks, p, stream);
+    });
 }
 
-// The most chunks of a backward pass: as many teams as the SMs hold at a time.
+constexpr uint32_t kMaxChunks  = 4096;      // chunks of rows of a backward pass
+constexpr uint32_t kLongChunks = 64;        // the same for rows that the ring does not hold
+
+// The most chunks of a backward pass: as many teams as the SMs hold at a time.  (Few rows: four a chunk at least where that still
+// leaves a chunk for every SM; partial rows cost, too.)
 uint32_t chunks_of(uint64_t rows, uint64_t d, int es, int sms)
 {
-    const uint64_t lanes = 16 / static_cast<uint64_t>(es), count = d / lanes;
-    uint64_t       most;
-    if (!row_fits(d, es)) most = kLongChunks;
-    else most = static_cast<uint64_t>(sms) * (kMaxTeam / (d % lanes == 0 ? team_of(count, hold_of(count)) : team_of(d, d <= 8 * kMaxTeam ? 8 : 16)));
+    uint64_t most = row_fits(d, es) ? resident_teams(ring_plan(d, es, 4), sms) : kLongChunks;
     if (most > kMaxChunks) most = kMaxChunks;
-    if (most > rows / 4) most = rows / 4 > static_cast<uint64_t>(sms) ? rows / 4 : static_cast<uint64_t>(sms);   // partial rows cost, too
+    const uint64_t least = most < static_cast<uint64_t>(sms) ? most : static_cast<uint64_t>(sms);
+    if (most > rows / 4) most = rows / 4 > least ? rows / 4 : least;
+    if (most == 0) most = 1;
     return static_cast<uint32_t>(most < rows ? most : rows);
 }
 // how the rows are dealt: inside the groups of rows with a gate while every group can have a chunk
@@ -1253,7 +1042,7 @@ cudaError_t backward(const NormArgs &a, cudaStream_t stream)
         if (!a.dgate && !a.dw_pre && !a.dw_post) return cudaSuccess;
         e = launch(block_norm_bwd_columns_kernel<DT>, static_cast<unsigned>(round_up_div(a.d, 128) * a.chunks), 128, 0, stream, a);
     } else {
-        e = bwd_of<DT>(a, stream);
+        e = bwd_ring<DT>(a, stream);
     }
     if (e != cudaSuccess || (!a.dgate && !a.dw_pre && !a.dw_post)) return e;
     const uint64_t groups = round_up_div(a.rows, a.gate_rows), borders = a.chunks - 1;

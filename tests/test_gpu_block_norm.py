@@ -9,9 +9,10 @@ pytestmark = pytest.mark.gpu
 KINDS = ["f32", "f16", "bf16", "f64"]
 SCALE, EPS = 0.375, 2.0 ** -20                      # both exact in binary32
 
-# rows, d: one row, one element, every form of the kernels (a warp or a CTA per row, whole vectors or not, rows read again)
+# rows, d: one row, one element, every form of the kernels (a CTA per row or a cluster, whole vectors or not, rows read again)
 SIZES = [(1, 1), (1, 2048), (5, 7), (3, 64), (37, 72), (130, 256), (33, 520), (19, 1000), (9, 1025), (700, 1024), (900, 1001), (700, 2047), (300, 4093), (6, 4096), (5, 4100), (4, 8192),
-         (3, 8193), (2, 16392), (3, 20001)]
+         (3, 8193), (2, 16392), (3, 20001),
+         (400, 8200), (90, 16384), (3, 40001), (2, 70000), (2, 131073)]
 
 
 def chain(d):
@@ -85,7 +86,7 @@ def test_forward(size, kind):
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("parts", PARTS)
-@pytest.mark.parametrize("size", [(24, 64), (12, 1000), (6, 2048), (3, 16400)])
+@pytest.mark.parametrize("size", [(24, 64), (12, 1000), (6, 2048), (3, 16400), (6, 8201), (3, 70000)])
 def test_forward_of_some_parts(size, parts, kind):
     t = make(*size, kind, groups=3, seed=4)
     check_forward(t, parts, kind, forward(t, parts))
@@ -176,15 +177,17 @@ def test_gate_groups(rows, groups, d, kind):
     check_backward(t, PARTS[0], kind, backward(t, PARTS[0]))
 
 
-def test_gate_groups_in_long_rows():
+@pytest.mark.parametrize("d,kind", [(16392, "f32"), (9000, "bf16"), (70000, "bf16"), (5001, "f32")])
+def test_gate_groups_in_long_rows(d, kind):
     for groups in (1, 10, 50, 150):
-        t = make(150, 16392, "f32", groups=groups, seed=9)
-        check_backward(t, PARTS[0], "f32", backward(t, PARTS[0]))
+        t = make(150, d, kind, groups=groups, seed=9)
+        check_forward(t, PARTS[0], kind, forward(t, PARTS[0]))
+        check_backward(t, PARTS[0], kind, backward(t, PARTS[0]))
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
 @pytest.mark.parametrize("parts", [p for p in PARTS if "w_pre" in p])
-@pytest.mark.parametrize("size", [(24, 64), (12, 1000), (6, 2048), (3, 16400)])
+@pytest.mark.parametrize("size", [(24, 64), (12, 1000), (6, 2048), (3, 16400), (6, 8201), (3, 70000)])
 def test_backward_of_some_parts(size, parts, kind):
     t = make(*size, kind, groups=3, seed=7)
     check_backward(t, parts, kind, backward(t, parts))
@@ -223,7 +226,7 @@ def test_backward_against_differences():
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
-@pytest.mark.parametrize("d", [64, 1000, 2048, 16400])
+@pytest.mark.parametrize("d", [64, 1000, 1001, 2048, 16400, 70000])
 def test_rows_of_zeros_infinities_and_nans(kind, d):
     """A row of zeros has the finite factor 1 / sqrt(eps); a NaN or an infinity stays in its row."""
     t = make(8, d, kind, seed=17)
