@@ -149,8 +149,9 @@ cudaError_t backward_of(const GluCall &c, cudaStream_t stream)
 }
 
 // ---------------------------------------------------------------------------------------------- slopes
-// du = dh act(g), dg = dh u act'(g): 16 bytes of each per thread.  Bound by HBM.  ReLU: a select, so that a closed gate's
-// gradient is +0 whatever dh and u hold.
+// du = dh act(g), dg = dh u act'(g): 16 bytes of each per thread.  Bound by HBM; with the logistic functions twice and in full
+// precision the issue slots were (bf16 4096 x 4736 SiLU 37 us), so act and act' share one, for 16-bit types the fast one.
+// ReLU: a select, so that a closed gate's gradient is +0 whatever dh and u hold.
 struct SlopeArgs {
     const void *dh, *g, *u;
     void       *dg, *du;
@@ -168,8 +169,10 @@ __device__ __forceinline__ void slopes(const typename Num<DT>::Acc dh, const typ
         dg             = off ? Acc(0) : dh * u;
         du             = off ? Acc(0) : dh * g;
     } else {
-        dg = dh * u * act_slope<kAct>(g);
-        du = dh * act_of<kAct>(g);
+        Acc act, slope;
+        act_and_slope<DT, kAct>(g, act, slope);
+        dg = dh * u * slope;
+        du = dh * act;
     }
 }
 template <int DT, int kAct>

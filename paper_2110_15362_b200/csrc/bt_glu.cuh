@@ -26,24 +26,6 @@ __device__ __forceinline__ A act_of(const A g)
     else if constexpr (kAct == BT_ACT_GELU) return A(0.5) * g * erfc_of(-A(0.70710678118654752440) * g);
     else return g * sigmoid_of(A(1.5957691216057307118) * (g + A(0.044715) * g * g * g));
 }
-// act'(g), given a stored gate (ReLU: the gate as it is stored, max(g, 0))
-template <int kAct, typename A>
-__device__ __forceinline__ A act_slope(const A g)
-{
-    if constexpr (kAct == BT_ACT_RELU) {
-        return g <= A(0) ? A(0) : A(1);
-    } else if constexpr (kAct == BT_ACT_SILU) {
-        const A s = sigmoid_of(g);
-        return s * (A(1) + g * (A(1) - s));
-    } else if constexpr (kAct == BT_ACT_GELU) {
-        return A(0.5) * erfc_of(-A(0.70710678118654752440) * g) + g * A(0.39894228040143267794) * exp_of(A(-0.5) * g * g);
-    } else {
-        if (g > A(64) || g < A(-64)) return g > A(0) ? A(1) : A(0);                  // g^2 must not overflow below
-        const A s = sigmoid_of(A(1.5957691216057307118) * (g + A(0.044715) * g * g * g));
-        return s + g * s * (A(1) - s) * A(1.5957691216057307118) * (A(1) + A(3 * 0.044715) * g * g);
-    }
-}
-
 // The same for values that are rounded to 16 bits: the logistic function by the fast exponential and reciprocal (a few units in
 // the 22nd bit).
 __device__ __forceinline__ float sigmoid_short(const float v) { return __fdividef(1.0f, 1.0f + __expf(-v)); }
@@ -53,6 +35,31 @@ __device__ __forceinline__ float act_short(const float g)
     if constexpr (kAct == BT_ACT_SILU) return g * sigmoid_short(g);
     else if constexpr (kAct == BT_ACT_GELU_TANH) return g * sigmoid_short(1.5957691216057307f * (g + 0.044715f * g * g * g));
     else return act_of<kAct>(g);
+}
+
+// act(g) and act'(g) of a stored gate, not ReLU
+template <int DT, int kAct>
+__device__ __forceinline__ void act_and_slope(const typename Num<DT>::Acc g, typename Num<DT>::Acc &act, typename Num<DT>::Acc &slope)
+{
+    using A            = typename Num<DT>::Acc;
+    const auto sigmoid = [](const A v) {
+        if constexpr (DT == BT_F16 || DT == BT_BF16) return sigmoid_short(v);
+        else return sigmoid_of(v);
+    };
+    if constexpr (kAct == BT_ACT_SILU) {
+        const A s = sigmoid(g);
+        act       = g * s;
+        slope     = s * (A(1) + g * (A(1) - s));
+    } else if constexpr (kAct == BT_ACT_GELU) {
+        const A c = A(0.5) * erfc_of(-A(0.70710678118654752440) * g);
+        act       = g * c;
+        slope     = c + g * A(0.39894228040143267794) * exp_of(A(-0.5) * g * g);
+    } else {
+        const A s = sigmoid(A(1.5957691216057307118) * (g + A(0.044715) * g * g * g));
+        act       = g * s;
+        // (far out the slope is 1 or 0, and g^2 must not overflow)
+        slope = g > A(64) ? A(1) : g < A(-64) ? A(0) : s + g * s * (A(1) - s) * A(1.5957691216057307118) * (A(1) + A(3 * 0.044715) * g * g);
+    }
 }
 
 // One call of the block, forward or backward (sizes checked, none of them 0).
