@@ -26,8 +26,9 @@
  *     synchronises nor prints.  Nothing about a tensor or a call outlives the
  *     call.  What the library does keep, all of it on the host: the calling
  *     thread's CTA limit (bt_set_max_ctas, off by default), a process-wide
- *     counter from which every compress launch draws its 64-bit tag, and, per
- *     device, the address of bt_compress_noalloc's built-in scratch array.
+ *     counter from which every compress launch draws its 64-bit tag, per
+ *     device the address of bt_compress_noalloc's built-in scratch array, and
+ *     the address of the driver's tensor-map encoder (bt_glu_*).
  *   - Calls are asynchronous on `stream` (a cudaStream_t passed as void*, NULL
  *     for the default stream) on the current device.
  *   - Tensors are flat contiguous arrays of n elements (Algorithm 1 flattens
@@ -540,6 +541,9 @@ enum { BT_ACT_RELU = 0, BT_ACT_SILU = 1, BT_ACT_GELU = 2, BT_ACT_GELU_TANH = 3 }
 /*
  * Gated feed-forward block, both projections, the activation and the product in one kernel:
  *   g = x w_gate^T,  u = x w_up^T,  h = act(g) * u
+ * 16-bit types and BT_F32 run on the tensor cores where d_in and d_ff are multiples of 8 (BT_F32 as three bfloat16 planes
+ * per operand, with the error of a binary32 sum; there an infinity in an operand may give a NaN where the formula has an
+ * infinity), all others, and BT_F64, on the CUDA cores; few rows have kernels of their own.
  * x is rows x d_in, w_gate and w_up are d_ff x d_in, h is rows x d_ff.  For a backward pass g_out and u_out
  * (rows x d_ff, each may be NULL) receive what bt_glu_bwd reads: g -- with BT_ACT_RELU max(g, 0), as sparse as
  * h, so that bt_compress and bt_mask_compress can stash both under one bitmap -- and u.  No output may overlap
