@@ -1,15 +1,16 @@
 // The gated feed-forward block's products on the tensor cores (tcgen05, sums in TMEM in binary32).
 //
-// One kernel, three uses (kUse).  A pair of CTAs (cta_group::2) computes tiles of 256 x kN outputs: each CTA holds 128 rows of
+// One kernel, two uses (kUse).  A pair of CTAs (cta_group::2) computes tiles of 256 x kN outputs: each CTA holds 128 rows of
 // A and half of B's kN rows, 64 of the summed axis per stage, and the pair's sums of its own 128 rows in its TMEM.
 //
-//   kForward      A = x, B = Wg and Wu: the pair's first CTA brings kN / 2 rows of Wg, the second the same rows of Wu, so that
-//                 columns 0 .. kN/2 of the tile are g and the others u; the epilogue writes act(g) u (and g and u).
-//   kInputGrad    A = dg then du, B = Wg then Wu read along their rows (the summed axis is not the contiguous one): one sum over
-//                 both products.
-//   kWeightGrad   A = dg (or du) and B = x, both read along their rows; the tiles of both gradients in one launch.
+//   kForward    A = x, B = Wg and Wu: the pair's first CTA brings kN / 2 rows of Wg, the second the same rows of Wu, so that
+//               columns 0 .. kN/2 of the tile are g and the others u; the epilogue writes act(g) u (and g and u).
+//   kBackward   the tiles of both kinds of gradients in one launch.  dx: A = dg then du, B = Wg then Wu read along their rows (the
+//               summed axis is not the contiguous one), one sum over both products.  dWg and dWu: A = dg or du and B = x, both
+//               read along their rows.  A pair takes its tiles of dx first, whose sums are the longer ones where that matters,
+//               then as many of the others as even the pairs out (UnitPlan): no round of tiles is left half empty between the two.
 //
-// Per CTA: one thread loads tiles by TMA into a ring of stages, one thread of the pair's first CTA issues the products, eight
+// Per CTA: one warp loads tiles by TMA into a ring of stages, one of the pair's first CTA issues the products, eight
 // warps bring sums from TMEM to the output through shared memory and TMA while the next tile is summed into the other half
 // of TMEM.  Rows, columns and depths beyond a tensor are read as zeros and never written (TMA's bounds).  The summed axis and both output
 // axes may have any size; rows of every operand must begin on 16-byte boundaries (d_in and d_ff multiples of 8).
@@ -33,7 +34,7 @@
 namespace bt {
 namespace {
 
-enum { kForward, kInputGrad, kWeightGrad };
+enum { kForward, kBackward };
 
 constexpr int kDepth      = 64;                       // of the summed axis per stage: 128 bytes, the widest swizzle
 constexpr int kRows       = 128;                      // of A per CTA
@@ -56,14 +57,21 @@ struct Shape {
     static constexpr int kSmem   = kBytes + 1024 + 256;                // room to start on 1024 bytes; barriers
 };
 
+// The tiles of an output.
+struct Grid {
+    uint64_t size_i, size_j;                           // of the output
+    uint32_t tiles_i, tiles_j;
+};
 struct MmaArgs {
-    CUtensorMap a[2], b[2], out[3];
-    uint32_t    blocks;                                // of the summed axis, of one product
-    uint32_t    tiles_i, tiles_j, tiles;               // of one output; of all
+    CUtensorMap a[2], b[3], out[3];                    // forward: x; Wg, Wu; h, g, u.  Backward: dg, du; Wg, Wu, x; dx, dWg, dWu
+    Grid        grid[2];                               // forward: [0]; backward: of dx, of dWg and dWu
+    uint32_t    blocks[2];                             // of the summed axis: forward [0]; backward of one product of dx, of dWg or dWu
     uint32_t    outputs;                               // forward: bit 0 h, bit 1 g, bit 2 u
-    uint64_t    size_i, size_j;                        // of an output
-    // kInputGrad with few tiles: the summed axis of a tile is dealt to `splits` units of split_blocks each, whose sums go to
-    // `partial` in binary32 (join_kernel adds them up)
+    // The units of a launch.  Forward: units[0] tiles.  Backward: units[0] of dx -- a tile, or where there are few of them one of
+    // `splits` parts of its summed axis, split_blocks blocks each, whose sums go to `partial` in binary32 (join_kernel adds them
+    // up) -- and units[1] tiles of the weights' gradients, of which a pair that has one unit of dx more than others (the first
+    // units[0] % pairs of them) takes the first `common` at most.
+    uint32_t    units[2], common;
     uint32_t    splits, split_blocks;
     float4     *partial;
     int32_t    *dev_status;
@@ -176,11 +184,12 @@ __device__ __forceinline__ uint64_t operand(uint32_t addr)
 template <bool kAcross>
 constexpr uint32_t kStep = kAcross ? 16 * 128 : 32;
 
-template <int DT, bool kAcrossA, bool kAcrossB, int kN>
+// the instruction's descriptor; kAcrossABit is set where A's rows lie along the other axis
+template <int DT, bool kAcrossB, int kN>
 constexpr uint32_t kInstruction = 1u << 4 |                                                    // sums in binary32
                                   (DT == BT_F16 ? 0u : 1u) << 7 | (DT == BT_F16 ? 0u : 1u) << 10 |     // operands: binary16 or bfloat16
-                                  (kAcrossA ? 1u : 0u) << 15 | (kAcrossB ? 1u : 0u) << 16 |    // which axis is contiguous
-                                  static_cast<uint32_t>(kN / 8) << 17 | static_cast<uint32_t>(256 / 16) << 24;
+                                  (kAcrossB ? 1u : 0u) << 16 | static_cast<uint32_t>(kN / 8) << 17 | static_cast<uint32_t>(256 / 16) << 24;
+constexpr uint32_t kAcrossABit = 1u << 15;
 
 // ---------------------------------------------------------------------------------------------- waits
 // A CTA's word that says that one of its roles gave up.  A whole warp waits, and all its lanes get the same answer.
@@ -221,18 +230,50 @@ struct Ring {
 struct Tile {
     uint32_t which, i, j;
 };
-__device__ __forceinline__ Tile tile_at(const MmaArgs &p, uint32_t t)
+__device__ __forceinline__ Tile tile_at(const Grid &g, uint32_t t)
 {
     Tile           r;
-    const uint32_t per = p.tiles_i * p.tiles_j;
+    const uint32_t per = g.tiles_i * g.tiles_j;
     r.which            = t / per;
     t -= r.which * per;
-    const uint32_t group = t / (8 * p.tiles_j), first = group * 8;
-    const uint32_t high = p.tiles_i - first < 8 ? p.tiles_i - first : 8;
-    t -= group * 8 * p.tiles_j;
+    const uint32_t group = t / (8 * g.tiles_j), first = group * 8;
+    const uint32_t high = g.tiles_i - first < 8 ? g.tiles_i - first : 8;
+    t -= group * 8 * g.tiles_j;
     r.i = first + t % high;
     r.j = t / high;
     return r;
+}
+
+// What a pair of CTAs does next: the n-th unit of pair c of `pairs`.
+struct Unit {
+    bool     valid, weights;                           // weights: a tile of dWg or dWu
+    Tile     tile;
+    uint32_t begin, end, number;                       // blocks of the summed axis; number among the units of dx
+};
+template <int kUse>
+__device__ __forceinline__ Unit unit_at(const MmaArgs &p, const uint32_t n, const uint32_t c, const uint32_t pairs)
+{
+    Unit u;
+    u.number = n * pairs + c, u.weights = false;
+    u.begin = 0, u.end = p.blocks[0] * (kUse == kBackward ? 2 : 1);
+    u.valid = u.number < p.units[0];
+    if (u.valid) {
+        if (kUse == kBackward && p.splits > 1) {
+            u.tile  = tile_at(p.grid[0], u.number / p.splits);
+            u.begin = u.number % p.splits * p.split_blocks;
+            if (u.begin + p.split_blocks < u.end) u.end = u.begin + p.split_blocks;
+        } else {
+            u.tile = tile_at(p.grid[0], u.number);
+        }
+    } else if constexpr (kUse == kBackward) {
+        const uint32_t more = p.units[0] % pairs, k = n - (p.units[0] / pairs + (c < more ? 1 : 0));
+        const uint32_t t    = k < p.common ? k * pairs + c : p.common * pairs + (k - p.common) * (pairs - more) + (c - more);
+        u.weights = true;
+        u.valid   = t < p.units[1] && (k < p.common || c >= more);
+        if (u.valid) u.tile = tile_at(p.grid[1], t);
+        u.end = p.blocks[1];
+    }
+    return u;
 }
 
 template <int DT>
@@ -254,8 +295,8 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
     static_assert(DT != BT_F32 || kN == 128, "two sums per tile, twice");
     using S                     = Shape<kN>;
     constexpr uint32_t kSums    = DT == BT_F32 ? 2 * kN : kN;            // TMEM columns of a tile
-    constexpr bool     kAcrossA = kUse == kWeightGrad, kAcrossB = kUse != kForward;
-    constexpr uint32_t kIdesc   = kInstruction<DT, kAcrossA, kAcrossB, kN>;
+    constexpr bool     kAcrossB = kUse == kBackward;
+    constexpr uint32_t kIdesc   = kInstruction<DT, kAcrossB, kN>;
     constexpr int      kStages  = S::kStages;
     extern __shared__ unsigned char raw[];
     const uint32_t base = (smem_addr(raw) + 1023) & ~1023u;
@@ -276,27 +317,12 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
         if (lane == 31) *gave_up = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 0 && lane < 7) prefetch_map(lane < 2 ? &p.a[lane] : lane < 4 ? &p.b[lane - 2] : &p.out[lane - 4]);
+    if (warp == 0 && lane < 8) prefetch_map(lane < 2 ? &p.a[lane] : lane < 5 ? &p.b[lane - 2] : &p.out[lane - 5]);
     // the first unit's place is worked out while the barriers are set up
-    const uint32_t first = blockIdx.x / 2, step = gridDim.x / 2;
-    const uint32_t blocks = p.blocks * (kUse == kInputGrad ? 2 : 1);
-    const bool     split  = kUse == kInputGrad && p.splits > 1;
-    // the part of the summed axis of unit t
-    const auto from_block = [&](const uint32_t t) { return split ? t % p.splits * p.split_blocks : 0u; };
-    const auto end_block = [&](const uint32_t t) {
-        const uint32_t end = from_block(t) + p.split_blocks;
-        return split && end < blocks ? end : blocks;
-    };
-    struct Unit {
-        Tile     tile;
-        uint32_t begin, end;
-    };
-    const auto unit_at = [&](const uint32_t t) {
-        Unit u;
-        if (t < p.tiles) u.tile = tile_at(p, split ? t / p.splits : t), u.begin = from_block(t), u.end = end_block(t);
-        return u;
-    };
-    const Unit first_unit = unit_at(first);
+    const uint32_t pair_of = blockIdx.x / 2, pairs = gridDim.x / 2;
+    const auto     nth     = [&](const uint32_t n) { return unit_at<kUse>(p, n, pair_of, pairs); };
+    const Unit     first_unit = nth(0);
+    const bool     split      = kUse == kBackward && p.splits > 1;
     __syncwarp();
     cluster_sync();
     in_stream_order();
@@ -320,12 +346,12 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
         bool           ok          = true;
         const uint32_t leader_bars = in_first_cta(full(0));
         Unit           unit        = first_unit;
-        for (uint32_t t = first; t < p.tiles && ok; t += step, unit = unit_at(t)) {
+        for (uint32_t n = 0; unit.valid && ok; unit = nth(++n)) {
             const Tile tile = unit.tile;
             const int  i0   = static_cast<int>(tile.i * 256 + rank * kRows);
             for (uint32_t k = unit.begin; k < unit.end && ok; ++k) {
-                const uint32_t pair = kUse == kInputGrad ? (k >= p.blocks ? 1u : 0u) : 0u;
-                const int      k0   = static_cast<int>((k - pair * p.blocks) * kDepth);
+                const uint32_t second = kUse == kBackward && !unit.weights && k >= p.blocks[0] ? 1u : 0u;      // dx: the product with Wu
+                const int      k0     = static_cast<int>((k - second * p.blocks[0]) * kDepth);
 #pragma unroll
                 for (int plane = 0; plane < static_cast<int>(kPlanes<DT>); ++plane) {
                     if (!(ok = wait(empty(ring.stage), ring.phase ^ 1))) break;
@@ -339,15 +365,13 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
                             tma_load(a, &p.a[0], k0, i0, plane, bar);
                             tma_load(b, rank == 0 ? &p.b[0] : &p.b[1], k0, static_cast<int>(tile.j * (kN / 2)), plane, bar);
                         } else {
+                            // boxes of 64 x 64: of 64 rows of A, whichever way they lie, and of 64 rows of B
                             const int          j0    = static_cast<int>(tile.j * kN + rank * (kN / 2));
-                            const CUtensorMap *map_a = (kUse == kInputGrad ? pair : tile.which) == 0 ? &p.a[0] : &p.a[1];
-                            const CUtensorMap *map_b = kUse == kInputGrad && pair != 0 ? &p.b[1] : &p.b[0];
-                            if constexpr (kUse == kInputGrad) {
-                                tma_load(a, map_a, k0, i0, plane, bar);
-                            } else {
+                            const CUtensorMap *map_a = (unit.weights ? tile.which : second) == 0 ? &p.a[0] : &p.a[1];
+                            const CUtensorMap *map_b = unit.weights ? &p.b[2] : second == 0 ? &p.b[0] : &p.b[1];
 #pragma unroll
-                                for (int v = 0; v < kRows / 64; ++v) tma_load(a + v * 64 * kDepth * 2, map_a, i0 + 64 * v, k0, plane, bar);
-                            }
+                            for (int v = 0; v < kRows / 64; ++v)
+                                tma_load(a + v * 64 * kDepth * 2, map_a, unit.weights ? i0 + 64 * v : k0, unit.weights ? k0 : i0 + 64 * v, plane, bar);
 #pragma unroll
                             for (int v = 0; v < kN / 2 / 64; ++v) tma_load(b + v * 64 * kDepth * 2, map_b, j0 + 64 * v, k0, plane, bar);
                         }
@@ -369,8 +393,11 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
             Ring<2>       half;
             bool          ok = true;
             Unit          unit = first_unit;
-            for (uint32_t t = first; t < p.tiles && ok; t += step, unit = unit_at(t)) {
+            for (uint32_t n = 0; unit.valid && ok; unit = nth(++n)) {
                 const uint32_t end = unit.end;
+                // which way A's rows lie
+                const uint32_t idesc = kIdesc | (unit.weights ? kAcrossABit : 0u), step_a = (unit.weights ? kStep<true> : kStep<false>) >> 4;
+                const auto     operand_a = [&](const uint32_t at) { return unit.weights ? operand<true>(at) : operand<false>(at); };
                 // binary32: a chunk of blocks at a time; else all of them
                 for (uint32_t begin = unit.begin; begin < end && ok;) {
                     const uint32_t stop = DT == BT_F32 && begin + kChunk < end ? begin + kChunk : end;
@@ -385,13 +412,13 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
                             const auto product = [&](const uint32_t to, const uint64_t da, const uint64_t db, const bool add) {
 #pragma unroll
                                 for (int q = 0; q < kDepth / 16; ++q)
-                                    mma_pair(to, da + q * (kStep<kAcrossA> >> 4), db + q * (kStep<kAcrossB> >> 4), kIdesc, add || q != 0);
+                                    mma_pair(to, da + q * step_a, db + q * (kStep<kAcrossB> >> 4), idesc, add || q != 0);
                             };
 #pragma unroll
                             for (int s = 0; s < 3; ++s) {
                                 if (ok && !(ok = wait(full(ring.stage), ring.phase))) break;
                                 const uint32_t at = base + ring.stage * (S::kABytes + S::kBBytes);
-                                slot[s] = ring.stage, a[s] = operand<kAcrossA>(at), b[s] = operand<kAcrossB>(at + S::kABytes);
+                                slot[s] = ring.stage, a[s] = operand_a(at), b[s] = operand<kAcrossB>(at + S::kABytes);
                                 if (elect_one()) {
                                     if (s == 0) product(d, a[0], b[0], k != begin);
                                     if (s == 1) product(d + kN, a[0], b[1], k != begin), product(d + kN, a[1], b[0], true), product(d + kN, a[1], b[1], true);
@@ -407,11 +434,11 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
                         } else {
                             if (!(ok = wait(full(ring.stage), ring.phase))) break;
                             const uint32_t a = base + ring.stage * (S::kABytes + S::kBBytes), b = a + S::kABytes;
-                            const uint64_t da = operand<kAcrossA>(a), db = operand<kAcrossB>(b);
+                            const uint64_t da = operand_a(a), db = operand<kAcrossB>(b);
                             if (elect_one()) {
 #pragma unroll
                                 for (int q = 0; q < kDepth / 16; ++q)
-                                    mma_pair(d, da + q * (kStep<kAcrossA> >> 4), db + q * (kStep<kAcrossB> >> 4), kIdesc, k != begin || q != 0);
+                                    mma_pair(d, da + q * step_a, db + q * (kStep<kAcrossB> >> 4), idesc, k != begin || q != 0);
                                 commit_pair(empty(ring.stage));
                             }
                             __syncwarp();
@@ -453,8 +480,9 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
             // 64 columns of the tile per warp, in registers from chunk to chunk: forward 32 of g and 32 of u, else the `turn`th 64
             bool ok = true;
             Unit unit = first_unit;
-            for (uint32_t t = first; t < p.tiles && ok; t += step, unit = unit_at(t)) {
+            for (uint32_t n = 0; unit.valid && ok; unit = nth(++n)) {
                 const Tile     tile = unit.tile;
+                const Grid    &grid = p.grid[unit.weights ? 1 : 0];
                 const uint32_t i0   = tile.i * 256 + rank * kRows + quarter * 32, end = unit.end;
                 uint32_t       sum[2][32];
 #pragma unroll
@@ -480,10 +508,10 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
                     half.next();
                 }
                 if (!ok) break;
-                if (i0 >= p.size_i) continue;
+                if (i0 >= grid.size_i) continue;
                 if constexpr (kUse == kForward) {
                     const uint32_t j0 = tile.j * (kN / 2) + turn * 32;
-                    if (j0 >= p.size_j) continue;
+                    if (j0 >= grid.size_j) continue;
                     uint32_t act[32];
 #pragma unroll
                     for (int c = 0; c < 32; ++c) {
@@ -495,9 +523,9 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
                     if (p.outputs & 2) stage_out(sum[0], &p.out[1], j0, i0);
                     if (p.outputs & 4) stage_out(sum[1], &p.out[2], j0, i0);
                 } else {
-                    if (split) {
-                        float4 *const out = p.partial + ((static_cast<uint64_t>(t) * 2 + rank) * (kN / 64) + turn) * (16 * kRows) + quarter * 32 + lane;
-                        const Extent  all = extent_of(p.partial, static_cast<uint64_t>(p.tiles) * 2 * (kN / 64) * (16 * kRows) * sizeof(float4));
+                    if (split && !unit.weights) {
+                        float4 *const out = p.partial + ((static_cast<uint64_t>(unit.number) * 2 + rank) * (kN / 64) + turn) * (16 * kRows) + quarter * 32 + lane;
+                        const Extent  all = extent_of(p.partial, static_cast<uint64_t>(p.units[0]) * 2 * (kN / 64) * (16 * kRows) * sizeof(float4));
 #pragma unroll
                         for (int c = 0; c < 16; ++c)
                             if (all.holds(out + c * kRows, sizeof(float4)))
@@ -508,14 +536,15 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
 #pragma unroll
                     for (int part = 0; part < 2; ++part) {
                         const uint32_t j0 = tile.j * kN + turn * 64 + part * 32;
-                        if (j0 < p.size_j) stage_out(sum[part], &p.out[tile.which], j0, i0);
+                        if (j0 < grid.size_j) stage_out(sum[part], &p.out[unit.weights ? 1 + tile.which : 0], j0, i0);
                     }
                 }
             }
         }
         Unit unit = first_unit;
-        for (uint32_t t = first; DT != BT_F32 && t < p.tiles; t += step, unit = unit_at(t)) {
+        for (uint32_t n = 0; DT != BT_F32 && unit.valid; unit = nth(++n)) {
             const Tile     tile = unit.tile;
+            const Grid    &grid = p.grid[unit.weights ? 1 : 0];
             const uint32_t i0 = tile.i * 256 + rank * kRows + quarter * 32;
             if (!wait(ready(half.stage), half.phase)) break;
             tmem_fence_after();
@@ -524,11 +553,11 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
                 const uint32_t chunk = item % kChunks, what = item / kChunks;
                 const uint32_t j0 = tile.j * (kUse == kForward ? kN / 2 : kN) + chunk * 64;
                 if (kUse == kForward && !(p.outputs >> what & 1)) continue;
-                if (j0 >= p.size_j || i0 >= p.size_i) continue;         // (the whole warp alike)
-                if (split) {
+                if (j0 >= grid.size_j || i0 >= grid.size_i) continue;         // (the whole warp alike)
+                if (split && !unit.weights) {
                     // as they lie in TMEM, four columns of 32 rows at a time
-                    float4 *const out = p.partial + ((static_cast<uint64_t>(t) * 2 + rank) * kChunks + chunk) * (16 * kRows) + quarter * 32 + lane;
-                    const Extent  all = extent_of(p.partial, static_cast<uint64_t>(p.tiles) * 2 * kChunks * (16 * kRows) * sizeof(float4));
+                    float4 *const out = p.partial + ((static_cast<uint64_t>(unit.number) * 2 + rank) * kChunks + chunk) * (16 * kRows) + quarter * 32 + lane;
+                    const Extent  all = extent_of(p.partial, static_cast<uint64_t>(p.units[0]) * 2 * kChunks * (16 * kRows) * sizeof(float4));
 #pragma unroll
                     for (int part = 0; part < 2; ++part) {
                         uint32_t v[32];
@@ -566,7 +595,7 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
                         for (int c = 0; c < 16; ++c) packed[part * 16 + c] = pack2<DT>(__uint_as_float(v[2 * c]), __uint_as_float(v[2 * c + 1]));
                     }
                 }
-                stage_out(packed, &p.out[kUse == kForward ? what : tile.which], j0, i0);
+                stage_out(packed, &p.out[kUse == kForward ? what : unit.weights ? 1 + tile.which : 0], j0, i0);
             }
             tmem_fence_before();
             __syncwarp();
@@ -592,31 +621,31 @@ glu_mma_kernel(const __grid_constant__ MmaArgs p)
 // The sums of a tile's units added up, rounded and written: a CTA takes eight columns of a CTA's 128 rows.
 template <int DT, int kN>
 __global__ void __launch_bounds__(kRows)
-join_kernel(const float4 *__restrict__ partial, const uint32_t splits, void *to, const uint64_t size_i, const uint64_t size_j, const MmaArgs p)
+join_kernel(const float4 *__restrict__ partial, const uint32_t splits, void *to, const Grid grid)
 {
     in_stream_order();
     constexpr uint32_t kChunks = kN / 64;
     uint32_t           b       = blockIdx.x;
     const uint32_t eight = b % 8, chunk = (b /= 8) % kChunks, rank = (b /= kChunks) % 2;
     const uint32_t t     = b / 2;
-    const Tile     tile  = tile_at(p, t);
+    const Tile     tile  = tile_at(grid, t);
     const uint64_t i = tile.i * 256ull + rank * kRows + threadIdx.x, j = tile.j * static_cast<uint64_t>(kN) + chunk * 64 + eight * 8;
-    if (i >= size_i || j >= size_j) return;
+    if (i >= grid.size_i || j >= grid.size_j) return;
     float s[8] = {};
     for (uint32_t k = 0; k < splits; ++k) {
         const float4 *const from = partial + ((static_cast<uint64_t>(t * splits + k) * 2 + rank) * kChunks + chunk) * (16 * kRows) + eight * 2 * kRows + threadIdx.x;
         const float4 lo = from[0], hi = from[kRows];
         s[0] += lo.x, s[1] += lo.y, s[2] += lo.z, s[3] += lo.w, s[4] += hi.x, s[5] += hi.y, s[6] += hi.z, s[7] += hi.w;
     }
-    // (size_j is a multiple of 8)
-    uint4 *const out = reinterpret_cast<uint4 *>(static_cast<typename Num<DT>::Elem *>(to) + i * size_j + j);
+    // (a row's length is a multiple of 8)
+    uint4 *const out = reinterpret_cast<uint4 *>(static_cast<typename Num<DT>::Elem *>(to) + i * grid.size_j + j);
     constexpr int kL = kLanes<DT>;
 #pragma unroll
     for (int q = 0; q < 8 / kL; ++q) {
         float v[kL];
 #pragma unroll
         for (int c = 0; c < kL; ++c) v[c] = s[q * kL + c];
-        if (extent_of(to, size_i * size_j * sizeof(typename Num<DT>::Elem)).holds(out + q, 16)) out[q] = narrow_vec<DT>(v);
+        if (extent_of(to, grid.size_i * grid.size_j * sizeof(typename Num<DT>::Elem)).holds(out + q, 16)) out[q] = narrow_vec<DT>(v);
     }
 }
 
@@ -705,140 +734,146 @@ bool out_map(CUtensorMap &m, int dtype, void *at, uint64_t rows, uint64_t column
 }
 
 template <int DT, int kUse, int kAct, int kN>
-cudaError_t start(const MmaArgs &p, cudaStream_t stream, int sms)
+cudaError_t start(const MmaArgs &p, uint64_t pairs, cudaStream_t stream)
 {
     const auto        kernel = glu_mma_kernel<DT, kUse, kAct, kN>;
     const cudaError_t e      = reported(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, Shape<kN>::kSmem));
-    if (e != cudaSuccess) return e;
-    const uint32_t pairs = static_cast<uint32_t>(sms) / 2;
-    return launch(kernel, 2 * (p.tiles < pairs ? p.tiles : pairs), kThreads, Shape<kN>::kSmem, stream, p);
+    return e != cudaSuccess ? e : launch(kernel, static_cast<unsigned>(2 * pairs), kThreads, Shape<kN>::kSmem, stream, p);
 }
 
-// tiles of `columns` output columns, for `outputs` outputs of size_i x size_j; false if there are more than 31 bits of them
-bool set_tiles(MmaArgs &p, uint64_t size_i, uint64_t size_j, uint32_t columns, uint32_t outputs)
+// the tiles of `columns` columns of an output
+Grid grid_of(uint64_t size_i, uint64_t size_j, uint32_t columns)
 {
-    p.size_i = size_i, p.size_j = size_j;
-    p.tiles_i            = static_cast<uint32_t>(round_up_div(size_i, 256));
-    p.tiles_j            = static_cast<uint32_t>(round_up_div(size_j, columns));
-    const uint64_t tiles = static_cast<uint64_t>(p.tiles_i) * p.tiles_j * outputs;
-    p.tiles              = static_cast<uint32_t>(tiles);
-    return tiles < 0x7FFFFFFFull;
+    return Grid{size_i, size_j, static_cast<uint32_t>(round_up_div(size_i, 256)), static_cast<uint32_t>(round_up_div(size_j, columns))};
 }
+uint64_t tiles_of(const Grid &g) { return static_cast<uint64_t>(g.tiles_i) * g.tiles_j; }
 
-// How long `units` tiles of `blocks` blocks of 64 summed elements take, in ns: the tensor cores' time where few pairs of CTAs
-// run, more where the L2 is shared by many (measured: a block of a 256 x 256 tile 280 to 400 ns, of a 256 x 128 tile 150 to 207).
+// How long a block of 64 summed elements takes, in ns: the tensor cores' time where few pairs of CTAs run, more where the L2 is
+// shared by many (measured: a block of a 256 x 256 tile 280 to 400 ns, of a 256 x 128 tile 150 to 207).
+double block_ns(uint32_t columns, uint64_t active)
+{
+    const double alone = columns == 256 ? 280 : 150, shared = (columns == 256 ? 5.4 : 2.8) * static_cast<double>(active);
+    return alone > shared ? alone : shared;
+}
 double tiles_ns(uint64_t units, uint64_t blocks, uint32_t columns, uint64_t pairs)
 {
-    const double alone = columns == 256 ? 280 : 150, shared = columns == 256 ? 5.4 : 2.8;
-    const auto   block = [&](uint64_t active) { return alone > shared * static_cast<double>(active) ? alone : shared * static_cast<double>(active); };
-    double       ns    = static_cast<double>(units / pairs) * block(pairs);
-    if (units % pairs) ns += block(units % pairs);
+    double ns = static_cast<double>(units / pairs) * block_ns(columns, pairs);
+    if (units % pairs) ns += block_ns(columns, units % pairs);
     return ns * static_cast<double>(blocks);
 }
-// Tiles of 256 or of 128 columns (columns256 output columns, or half of them)?  cross: the operands' rows do not begin on 32 bytes,
-// so that a copied row of 128 bytes takes five sectors of the L2 in place of four (measured: 1.3 times the time of wide tiles, 1.5 of
-// the others).
-bool wide_tiles(uint64_t size_i, uint64_t size_j, uint64_t outputs, uint64_t columns256, uint64_t blocks, bool cross, int sms)
+// Forward: tiles of 256 columns (128 of the output), or of 128?  cross: the operands' rows do not begin on 32 bytes, so that a
+// copied row of 128 bytes takes five sectors of the L2 in place of four (measured: 1.3 times the time of wide tiles, 1.5 of the others).
+bool wide_tiles(const GluCall &c, uint64_t pairs)
 {
-    const uint64_t pairs = static_cast<uint64_t>(sms) / 2, rows = round_up_div(size_i, 256) * outputs;
-    return tiles_ns(rows * round_up_div(size_j, columns256), blocks, 256, pairs) * (cross ? 1.3 : 1.0) <=
-           tiles_ns(rows * round_up_div(size_j, columns256 / 2), blocks, 128, pairs) * (cross ? 1.5 : 1.0);
+    const bool     cross = c.d_in % 16 != 0;
+    const uint64_t rows = round_up_div(c.rows, 256), blocks = round_up_div(c.d_in, kDepth);
+    return tiles_ns(rows * round_up_div(c.d_ff, 128), blocks, 256, pairs) * (cross ? 1.3 : 1.0) <=
+           tiles_ns(rows * round_up_div(c.d_ff, 64), blocks, 128, pairs) * (cross ? 1.5 : 1.0);
 }
 
 template <int DT, int kN>
-cudaError_t forward_of(const GluCall &c, int sms, cudaStream_t stream)
+cudaError_t forward_of(const GluCall &c, uint64_t most_pairs, cudaStream_t stream)
 {
     MmaArgs p{};
     bool    ok = map_of(p.a[0], DT, c.x, c.rows, c.d_in, kRows) && map_of(p.b[0], DT, c.w_gate, c.d_ff, c.d_in, kN / 2) &&
               map_of(p.b[1], DT, c.w_up, c.d_ff, c.d_in, kN / 2) && out_map(p.out[0], DT, c.h, c.rows, c.d_ff);
     if (c.g) ok = ok && out_map(p.out[1], DT, c.g, c.rows, c.d_ff);
     if (c.u) ok = ok && out_map(p.out[2], DT, c.u, c.rows, c.d_ff);
-    if (!ok || !set_tiles(p, c.rows, c.d_ff, kN / 2, 1)) return cudaErrorInvalidValue;
+    p.grid[0] = grid_of(c.rows, c.d_ff, kN / 2);
+    if (!ok || tiles_of(p.grid[0]) > 0x7FFFFFFFull) return cudaErrorInvalidValue;
+    p.units[0]   = static_cast<uint32_t>(tiles_of(p.grid[0]));
     p.outputs    = 1u | (c.g ? 2u : 0u) | (c.u ? 4u : 0u);
-    p.blocks     = static_cast<uint32_t>(round_up_div(c.d_in, kDepth));
+    p.blocks[0]  = static_cast<uint32_t>(round_up_div(c.d_in, kDepth));
     p.dev_status = c.dev_status;
-    return with_act<DT>(c.act, [&](auto dt, auto act) { return start<decltype(dt)::value, kForward, decltype(act)::value, kN>(p, stream, sms); });
+    const uint64_t pairs = p.units[0] < most_pairs ? p.units[0] : most_pairs;
+    return with_act<DT>(c.act, [&](auto dt, auto act) { return start<decltype(dt)::value, kForward, decltype(act)::value, kN>(p, pairs, stream); });
 }
 
-// How the input gradient is computed: columns of a tile and units per tile.  Units cost a second launch and the store of the
-// last sums (3 us), and 30 ns per 128 KB of sums that go out and in.
-struct SplitPlan {
+// How a backward pass is dealt out: columns of a tile, parts of dx's summed axis, tiles of the weights' gradients.
+struct UnitPlan {
     uint32_t columns, splits, split_blocks;
-    uint64_t tiles;
+    uint64_t units[2], pairs, common;
 };
-SplitPlan input_grad_plan(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, int sms)
+// The least length in which every pair of CTAs gets through its share: units[0] of length `long_unit` dealt one after the other, then
+// units[1] of `short_unit` to even the pairs out.  common: how many of the latter the pairs take that have a unit more of the former.
+uint64_t level(const uint64_t (&units)[2], uint64_t long_unit, uint64_t short_unit, uint64_t pairs, uint64_t &common)
 {
-    const uint64_t pairs = static_cast<uint64_t>(sms) / 2, blocks = 2 * round_up_div(d_ff, kDepth);
-    const uint64_t each_block = dtype == BT_F32 ? 6 : 1;                 // products
-    SplitPlan      best{};
+    const uint64_t more = units[0] % pairs, base = units[0] / pairs * long_unit, high = base + (more ? long_unit : 0);
+    const auto     room = [&](uint64_t length, uint64_t used) { return length > used ? (length - used) / short_unit : 0; };
+    const uint64_t even = round_up_div(units[0] * long_unit + units[1] * short_unit, pairs);
+    uint64_t       lo = high > even ? high : even, hi = lo + short_unit;             // (at hi every pair has room for its share and a unit more)
+    while (lo < hi) {
+        const uint64_t mid = (lo + hi) / 2;
+        if (more * room(mid, high) + (pairs - more) * room(mid, base) >= units[1]) hi = mid;
+        else lo = mid + 1;
+    }
+    common = more ? room(lo, high) : room(lo, base);
+    return lo;
+}
+// By estimated time, in products of a block: binary32 takes six per block.  A tile's start and stores take as long as 6 of them (12
+// for binary32's twice as many bytes), hidden behind the next tile's sums but for one, so that no tile of the weights' gradients is
+// shorter (64 x 2048 x 8192: 2.2 us for 256 columns).  Parts of dx cost the store of their sums (4), a second launch and the last
+// stores (3 us), and 40 ns per 128 KB of sums that go out and in.  Each choice measured against the others: 1021 x 1024 x 2752 in 128
+// columns 23.8 us, in 256 33.4 whole and 25.9 with dx in two parts; 64 x 2048 x 8192 in 256 columns 80.6 us whole, 34.8 with dx in four.
+UnitPlan unit_plan(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, bool dx, bool weights, int sms)
+{
+    const uint64_t most = static_cast<uint64_t>(sms) / 2, blocks = 2 * round_up_div(d_ff, kDepth), in_rows = round_up_div(rows, kDepth);
+    const uint64_t products = dtype == BT_F32 ? 6 : 1, least_tile = dtype == BT_F32 ? 12 : 6;
+    const uint64_t short_tile = in_rows * products + 1 < least_tile ? least_tile : in_rows * products + 1;
+    UnitPlan       best{};
     double         least = 0;
     for (const uint32_t columns : {256u, 128u}) {
         if (dtype == BT_F32 && columns == 256) continue;
-        const uint64_t tiles = round_up_div(rows, 256) * round_up_div(d_in, columns);
-        for (uint32_t splits = 1; splits <= 32 && (splits == 1 || blocks / splits >= 4); ++splits) {
+        const uint64_t tiles = dx ? tiles_of(grid_of(rows, d_in, columns)) : 0;
+        for (const uint32_t splits : {1u, 2u, 3u, 4u, 5u, 6u, 8u, 10u, 12u, 16u, 20u, 24u, 32u}) {
             const uint64_t each = round_up_div(blocks, splits);
-            if (round_up_div(blocks, each) != splits) continue;         // (a unit would be empty)
-            double cost = tiles_ns(tiles * splits, each * each_block, columns, pairs);
-            if (splits > 1) cost += 3000 + static_cast<double>(tiles * splits) * 30 * (columns / 128.0);
-            if (least == 0 || cost < least) least = cost, best = SplitPlan{columns, splits, static_cast<uint32_t>(each), tiles};
+            if (splits > 1 && (!dx || each < 4 || round_up_div(blocks, each) != splits)) continue;
+            UnitPlan p{columns, splits, static_cast<uint32_t>(each), {tiles * splits, weights ? 2 * tiles_of(grid_of(d_ff, d_in, columns)) : 0}, most, 0};
+            if (p.units[0] + p.units[1] < most) p.pairs = p.units[0] + p.units[1];
+            double cost = static_cast<double>(level(p.units, each * products + (splits > 1 ? 4 : 0), short_tile, p.pairs, p.common)) * block_ns(columns, p.pairs);
+            if (splits > 1) cost += 3000 + static_cast<double>(p.units[0]) * 40 * (columns / 128.0);
+            if (least == 0 || cost < least) least = cost, best = p;
         }
     }
     return best;
 }
-uint64_t partial_bytes(const SplitPlan &s) { return s.splits == 1 ? 0 : s.tiles * s.splits * 256 * s.columns * sizeof(float); }
+uint64_t partial_bytes(const UnitPlan &p) { return p.splits <= 1 ? 0 : p.units[0] * 256 * p.columns * sizeof(float); }
 
 template <int DT, int kN>
-cudaError_t input_grad_of(const GluCall &c, const SplitPlan &s, int sms, cudaStream_t stream)
+cudaError_t backward_of(const GluCall &c, const UnitPlan &plan, cudaStream_t stream)
 {
-    MmaArgs    p{};
-    const bool ok = map_of(p.a[0], DT, c.dg, c.rows, c.d_ff, kRows) && map_of(p.a[1], DT, c.du, c.rows, c.d_ff, kRows) &&
-                    map_of(p.b[0], DT, c.w_gate, c.d_ff, c.d_in, kDepth) && map_of(p.b[1], DT, c.w_up, c.d_ff, c.d_in, kDepth) &&
-                    out_map(p.out[0], DT, c.dx, c.rows, c.d_in);
-    if (!ok || !set_tiles(p, c.rows, c.d_in, kN, 1)) return cudaErrorInvalidValue;
-    p.blocks     = static_cast<uint32_t>(round_up_div(c.d_ff, kDepth));
+    MmaArgs p{};
+    bool    ok = map_of(p.a[0], DT, c.dg, c.rows, c.d_ff, 64) && map_of(p.a[1], DT, c.du, c.rows, c.d_ff, 64);
+    if (c.dx)
+        ok = ok && map_of(p.b[0], DT, c.w_gate, c.d_ff, c.d_in, 64) && map_of(p.b[1], DT, c.w_up, c.d_ff, c.d_in, 64) &&
+             out_map(p.out[0], DT, c.dx, c.rows, c.d_in);
+    if (c.dw_gate)
+        ok = ok && map_of(p.b[2], DT, c.x, c.rows, c.d_in, 64) && out_map(p.out[1], DT, c.dw_gate, c.d_ff, c.d_in) &&
+             out_map(p.out[2], DT, c.dw_up, c.d_ff, c.d_in);
+    if (!ok || plan.units[0] > 0x3FFFFFFFull || plan.units[1] > 0x3FFFFFFFull) return cudaErrorInvalidValue;
+    p.grid[0] = grid_of(c.rows, c.d_in, kN), p.grid[1] = grid_of(c.d_ff, c.d_in, kN);
+    p.blocks[0] = static_cast<uint32_t>(round_up_div(c.d_ff, kDepth)), p.blocks[1] = static_cast<uint32_t>(round_up_div(c.rows, kDepth));
+    p.units[0] = static_cast<uint32_t>(plan.units[0]), p.units[1] = static_cast<uint32_t>(plan.units[1]), p.common = static_cast<uint32_t>(plan.common);
+    p.splits = plan.splits, p.split_blocks = plan.split_blocks, p.partial = static_cast<float4 *>(c.scratch);
     p.dev_status = c.dev_status;
-    p.splits = s.splits, p.split_blocks = s.split_blocks, p.partial = static_cast<float4 *>(c.scratch);
-    const uint32_t tiles = p.tiles;
-    p.tiles *= s.splits;
-    const cudaError_t e = start<DT, kInputGrad, BT_ACT_RELU, kN>(p, stream, sms);
-    if (e != cudaSuccess || s.splits == 1) return e;
-    return launch(join_kernel<DT, kN>, tiles * 2 * (kN / 64) * 8, kRows, 0, stream, p.partial, s.splits, c.dx, c.rows, c.d_in, p);
-}
-
-template <int DT, int kN>
-cudaError_t weight_grad_of(const GluCall &c, int sms, cudaStream_t stream)
-{
-    MmaArgs    p{};
-    const bool ok = map_of(p.a[0], DT, c.dg, c.rows, c.d_ff, kDepth) && map_of(p.a[1], DT, c.du, c.rows, c.d_ff, kDepth) &&
-                    map_of(p.b[0], DT, c.x, c.rows, c.d_in, kDepth) && out_map(p.out[0], DT, c.dw_gate, c.d_ff, c.d_in) &&
-                    out_map(p.out[1], DT, c.dw_up, c.d_ff, c.d_in);
-    if (!ok || !set_tiles(p, c.d_ff, c.d_in, kN, 2)) return cudaErrorInvalidValue;
-    p.blocks     = static_cast<uint32_t>(round_up_div(c.rows, kDepth));
-    p.dev_status = c.dev_status;
-    return start<DT, kWeightGrad, BT_ACT_RELU, kN>(p, stream, sms);
+    const cudaError_t e = start<DT, kBackward, BT_ACT_RELU, kN>(p, plan.pairs, stream);
+    if (e != cudaSuccess || plan.splits == 1 || !c.dx) return e;
+    return launch(join_kernel<DT, kN>, static_cast<unsigned>(tiles_of(p.grid[0]) * 2 * (kN / 64) * 8), kRows, 0, stream, p.partial, plan.splits, c.dx, p.grid[0]);
 }
 
 template <int DT>
 cudaError_t forward(const GluCall &c, int sms, cudaStream_t stream)
 {
-    if constexpr (DT == BT_F32) return forward_of<DT, 128>(c, sms, stream);
-    else return wide_tiles(c.rows, c.d_ff, 1, 128, round_up_div(c.d_in, kDepth), c.d_in % 16 != 0, sms) ? forward_of<DT, 256>(c, sms, stream)
-                                                                                               : forward_of<DT, 128>(c, sms, stream);
+    const uint64_t pairs = static_cast<uint64_t>(sms) / 2;
+    if constexpr (DT == BT_F32) return forward_of<DT, 128>(c, pairs, stream);
+    else return wide_tiles(c, pairs) ? forward_of<DT, 256>(c, pairs, stream) : forward_of<DT, 128>(c, pairs, stream);
 }
 template <int DT>
 cudaError_t backward(const GluCall &c, int sms, cudaStream_t stream)
 {
-    if (c.dx) {
-        const SplitPlan s = input_grad_plan(c.rows, c.d_in, c.d_ff, DT, sms);
-        cudaError_t     e;
-        if constexpr (DT == BT_F32) e = input_grad_of<DT, 128>(c, s, sms, stream);
-        else e = s.columns == 256 ? input_grad_of<DT, 256>(c, s, sms, stream) : input_grad_of<DT, 128>(c, s, sms, stream);
-        if (e != cudaSuccess) return e;
-    }
-    if (!c.dw_gate) return cudaSuccess;
-    if constexpr (DT == BT_F32) return weight_grad_of<DT, 128>(c, sms, stream);
-    else return wide_tiles(c.d_ff, c.d_in, 2, 256, round_up_div(c.rows, kDepth), c.d_in % 16 != 0 || c.d_ff % 16 != 0, sms) ? weight_grad_of<DT, 256>(c, sms, stream)
-                                                                                               : weight_grad_of<DT, 128>(c, sms, stream);
+    const UnitPlan plan = unit_plan(c.rows, c.d_in, c.d_ff, DT, c.dx != nullptr, c.dw_gate != nullptr, sms);
+    if constexpr (DT == BT_F32) return backward_of<DT, 128>(c, plan, stream);
+    else return plan.columns == 256 ? backward_of<DT, 256>(c, plan, stream) : backward_of<DT, 128>(c, plan, stream);
 }
 
 }  // namespace
@@ -852,7 +887,12 @@ size_t glu_mma_scratch(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, b
 {
     if (!glu_mma_takes(d_in, d_ff, dtype)) return 0;
     const int    sms  = sm_count();
-    const size_t sums = backward ? partial_bytes(input_grad_plan(rows, d_in, d_ff, dtype, sms ? sms : 148)) : 0;
+    size_t       sums = 0;
+    if (backward)                                                       // with the weights' gradients, or dx alone
+        for (const bool weights : {false, true}) {
+            const size_t s = partial_bytes(unit_plan(rows, d_in, d_ff, dtype, true, weights, sms ? sms : 148));
+            sums           = s > sums ? s : sums;
+        }
     return dtype == BT_F32 ? glu_plane_bytes(rows * d_in) + 2 * glu_plane_bytes(d_ff * d_in) + sums : sums;
 }
 
