@@ -566,8 +566,8 @@ int bt_glu_fwd(const void *x, uint64_t rows, uint64_t d_in, uint64_t d_ff, int d
  *   grad_x = dg w_gate + du w_up,  grad_w_gate = dg^T x,  grad_w_up = du^T x
  * With BT_ACT_RELU a closed gate's dg and du are +0 whatever grad_h and u hold there.  grad_x may be NULL, or
  * grad_w_gate and grad_w_up both; what only the missing output needs (the weights, or x) may then be NULL too.
- * rows == 0 sets the weights' gradients to +0.  workspace_bytes >= bt_glu_workspace_bytes(.., 1).  Other
- * parameters and limits as bt_glu_fwd.
+ * rows == 0 sets the weights' gradients to +0.  workspace_bytes >= bt_glu_workspace_bytes(.., 1), asked with the
+ * same device current.  Other parameters and limits as bt_glu_fwd.
  */
 int bt_glu_bwd(const void *grad_h, uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, int activation,
                const void *g, const void *u, const void *x, const void *w_gate, const void *w_up, void *grad_x,

@@ -770,16 +770,18 @@ def _dense(t: Optional[torch.Tensor]) -> Optional[torch.Tensor]:
 class GLUStash(torch.autograd.Function):
     """h = act(x w_gate^T) * (x w_up^T) (``bt_glu_fwd`` / ``bt_glu_bwd``).  The backward pass needs both projections.  With a
     ReLU gate and a context they are kept as stashes: the gate compressed, the other projection and the output under
-    the gate's bitmap (``bt_mask_compress``), wherever the gate is sparse enough to gain by it."""
+    the gate's bitmap (``bt_mask_compress``), wherever the gate is sparse enough to gain by it.  The values keep their own type and
+    have storage of their own size, with an arena too: the number of kept elements is read on the host.  What an infinite or NaN projection leaves in the output behind a closed gate
+    is not kept.  `graph`: whether a backward pass may follow."""
 
     @staticmethod
     def forward(ctx, x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activation: str = "relu",
-                hooks: Optional[stash_saved_activations] = None):
+                hooks: Optional[stash_saved_activations] = None, graph: bool = True):
         _on_current_device("glu_stash", x, w_gate, w_up)
         xc, wg, wu = _flat_input(x), _flat_input(w_gate), _flat_input(w_up)
         d_ff, d_in = wg.shape
         h = torch.empty((*xc.shape[:-1], d_ff), dtype=xc.dtype, device=xc.device)
-        keep = any(ctx.needs_input_grad[:3])
+        keep = graph and any(ctx.needs_input_grad[:3])
         g, u = (torch.empty_like(h), torch.empty_like(h)) if keep else (None, None)
         rows = xc.numel() // max(d_in, 1)
         status = hooks.statuses.next(xc.device) if hooks is not None else None
@@ -789,7 +791,7 @@ class GLUStash(torch.autograd.Function):
             hooks.statuses.made(status)
         ctx.activation, ctx.packed = activation, None
         if keep:
-            if hooks is not None and activation == "relu" and h.numel() >= hooks.min_numel:
+            if hooks is not None and activation == "relu" and h.numel() >= max(hooks.min_numel, 1):
                 ctx.packed = GLUStash._stash(h, g, u, hooks)
             if ctx.packed is not None:
                 ctx.save_for_backward(xc, wg, wu)
@@ -831,7 +833,7 @@ class GLUStash(torch.autograd.Function):
         rows = xc.numel() // max(d_in, 1)
         B.bt_glu_bwd(dh, g, u, xc, wg, wu, dx, dwg, dwu, B.new_glu_workspace(rows, d_in, d_ff, xc.dtype, xc.device, backward=True),
                      activation=ctx.activation)
-        return dx, dwg if need_g else None, dwu if need_u else None, None, None
+        return dx, dwg if need_g else None, dwu if need_u else None, None, None, None
 
 
 def glu_stash(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activation: str = "relu",
@@ -839,7 +841,7 @@ def glu_stash(x: torch.Tensor, w_gate: torch.Tensor, w_up: torch.Tensor, activat
     """Gated feed-forward block of (..., d_in) tensors, weights (d_ff, d_in): ``act(x @ w_gate.T) * (x @ w_up.T)`` in one
     kernel; `activation` "relu", "silu", "gelu" or "gelu_tanh".  Pass the active context as `hooks` to keep what the
     backward pass needs as stashes (ReLU; see ``GLUStash``).  All three tensors have one element type."""
-    return GLUStash.apply(x, w_gate, w_up, activation, hooks)
+    return GLUStash.apply(x, w_gate, w_up, activation, hooks, torch.is_grad_enabled())
 
 
 class BlockNorm(torch.autograd.Function):
@@ -885,7 +887,7 @@ def block_norm(x: torch.Tensor, f: Optional[torch.Tensor] = None, *, gate: Optio
 
 
 def clip_grad_norm(parameters, max_norm: float) -> torch.Tensor:
-    """Scales the gradients of `parameters` (tensors; those without a gradient are skipped, the same one twice counts once) in
+    """Scales the gradients of `parameters` (tensors; those without a gradient are skipped, the same gradient twice counts once) in
     place by min(1, max_norm / (norm + 1e-6)), norm being that of all of them together, and returns the norm (float32,
     0-dimensional, on the device; nothing is read on the host).  Gradients of one element type: two launches; several: the sums
     type by type, then the products."""
@@ -893,7 +895,7 @@ def clip_grad_norm(parameters, max_norm: float) -> torch.Tensor:
         raise ValueError("clip_grad_norm: max_norm must not be negative")
     if isinstance(parameters, torch.Tensor):
         parameters = [parameters]
-    grads = list({id(p): p.grad for p in parameters if p.grad is not None}.values())
+    grads = list({id(p.grad): p.grad for p in parameters if p.grad is not None}.values())
     if not grads:
         return torch.zeros((), dtype=torch.float32, device="cuda")
     for g in grads:

@@ -232,7 +232,7 @@ cudaError_t pass(const bt_batch_item *items, uint32_t count, int dtype, bool sca
     uint64_t   tiles = 0;
     for (uint32_t k = 0; k <= count; ++k) {
         const uint64_t mine = k < count ? tiles_of(items[k].n, es) : 0;
-        if (m != 0 && (k == count || m == kMany || tiles + mine > 0xFFFFFFF0ull)) {
+        if (m != 0 && (k == count || m == kMany || tiles + mine > 0xFFFF0000ull)) {
             cudaError_t e;
             switch (dtype) {
             case BT_F32: e = launch_typed<BT_F32>(t, m, tiles, scale, partial, partials, max_norm, norm_out, stream); break;
@@ -268,7 +268,7 @@ size_t workspace_of(uint32_t count, const N &n)
     for (uint32_t k = 0; k < count; ++k) {
         if (n(k) == 0) continue;
         const uint64_t mine = tiles_of(n(k), 8);
-        if (in_group == kMany || tiles + mine > 0xFFFFFFF0ull) ++groups, in_group = 0, tiles = 0;
+        if (in_group == kMany || tiles + mine > 0xFFFF0000ull) ++groups, in_group = 0, tiles = 0;
         ++in_group;
         tiles += mine;
     }

@@ -167,6 +167,56 @@ def test_clipping_of_parameters(A, kinds):
     assert float(A.clip_grad_norm([params[-2]], 1.0)) == 0.0
 
 
+def test_one_gradient_of_two_parameters(A):
+    p, q = (torch.nn.Parameter(torch.zeros(300, device="cuda")) for _ in range(2))
+    p.grad = q.grad = torch.full((300,), 2.0, device="cuda")
+    norm = float(A.clip_grad_norm([p, q], 1.0))
+    assert norm == pytest.approx(1200 ** 0.5, rel=2 ** -20)
+    assert torch.allclose(p.grad, torch.full_like(p.grad, 2.0 / norm), rtol=2 ** -20)
+
+
+def test_without_a_graph_nothing_is_kept(A):
+    g = gen(17)
+    x, w = normal(g, (300, D), "bf16").requires_grad_(), normal(g, (FF, D), "bf16", D ** -0.5).requires_grad_()
+    with A.stash_saved_activations(min_numel=1) as hooks:
+        h = A.glu_stash(x, w, w, hooks=hooks)
+        with_graph = hooks.packed_bytes
+        assert with_graph > 0
+        with torch.no_grad():
+            assert torch.equal(A.glu_stash(x, w, w, hooks=hooks), h)
+        assert hooks.packed_bytes == with_graph
+        empty = A.glu_stash(x[:0], w, w, hooks=hooks)
+        assert empty.shape == (0, FF)
+
+
+def test_gradients_captured_and_replayed(A):
+    """Forward and backward of a block through autograd in one graph, replayed on new inputs."""
+    g = gen(37)
+    x, w_pre, dh = normal(g, (130, D), "bf16").requires_grad_(), normal(g, (D,), "bf16").requires_grad_(), normal(g, (130, FF), "bf16")
+    wg, wu = (normal(g, (FF, D), "bf16", D ** -0.5).requires_grad_() for _ in range(2))
+
+    def go():
+        h = A.glu_stash(A.block_norm(x, w_pre=w_pre), wg, wu)
+        return (h.detach(), *torch.autograd.grad(h, (x, w_pre, wg, wu), dh))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        go()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = go()
+    for seed in (1, 2):
+        with torch.no_grad():
+            x.copy_(normal(gen(seed), (130, D), "bf16"))
+        graph.replay()
+        torch.cuda.synchronize()
+        kept = [t.clone() for t in got]
+        assert all(torch.equal(a, b) for a, b in zip(kept, go()))
+
+
 def test_refusals(A):
     x, w = torch.zeros(4, 16, device="cuda"), torch.zeros(8, 16, device="cuda")
     with pytest.raises(ValueError, match="current CUDA device"):
