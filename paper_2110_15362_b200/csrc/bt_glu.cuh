@@ -29,10 +29,30 @@ __device__ __forceinline__ A act_of(const A g)
 // The same for values that are rounded to 16 bits: the logistic function by the fast exponential and reciprocal (a few units in
 // the 22nd bit).
 __device__ __forceinline__ float sigmoid_short(const float v) { return __fdividef(1.0f, 1.0f + __expf(-v)); }
+// The Gaussian's distribution likewise: with v = |g| / sqrt(2) and t = 1 / (1 + 0.45 v), erfc(v) exp(v^2) / (2t) is smooth on
+// (0, 1] and a polynomial of degree 7, fitted here for the least relative error (v up to 30: 4e-7), stands for it; the
+// negative tail keeps its relative digits.  With the exponential (which the slope needs as well) 2e-5 at g = -13, 1e-6 from -2.6 on.
+__device__ __forceinline__ float gauss_short(const float g, float &exponential)
+{
+    const float v = fabsf(g) * 0.70710678f, t = __fdividef(1.0f, fmaf(0.45f, v, 1.0f));
+    float       s = fmaf(0.034758285f, t, -0.12572007f);
+    s             = fmaf(s, t, 0.11414351f);
+    s             = fmaf(s, t, 0.011124996f);
+    s             = fmaf(s, t, 0.09911599f);
+    s             = fmaf(s, t, 0.1125899f);
+    s             = fmaf(s, t, 0.1270477f);
+    s             = fmaf(s, t, 0.12693986f);
+    exponential   = __expf(-v * v);
+    const float q = s * t * exponential;
+    return g > 0 ? 1.0f - q : q;
+}
 template <int kAct>
 __device__ __forceinline__ float act_short(const float g)
 {
-    if constexpr (kAct == BT_ACT_SILU) return g * sigmoid_short(g);
+    if constexpr (kAct == BT_ACT_GELU) {
+        float e;
+        return g * gauss_short(g, e);
+    } else if constexpr (kAct == BT_ACT_SILU) return g * sigmoid_short(g);
     else if constexpr (kAct == BT_ACT_GELU_TANH) return g * sigmoid_short(1.5957691216057307f * (g + 0.044715f * g * g * g));
     else return act_of<kAct>(g);
 }
@@ -51,9 +71,11 @@ __device__ __forceinline__ void act_and_slope(const typename Num<DT>::Acc g, typ
         act       = g * s;
         slope     = s * (A(1) + g * (A(1) - s));
     } else if constexpr (kAct == BT_ACT_GELU) {
-        const A c = A(0.5) * erfc_of(-A(0.70710678118654752440) * g);
-        act       = g * c;
-        slope     = c + g * A(0.39894228040143267794) * exp_of(A(-0.5) * g * g);
+        A c, e;
+        if constexpr (DT == BT_F16 || DT == BT_BF16) c = gauss_short(g, e);
+        else c = A(0.5) * erfc_of(-A(0.70710678118654752440) * g), e = exp_of(A(-0.5) * g * g);
+        act   = g * c;
+        slope = c + g * A(0.39894228040143267794) * e;
     } else {
         const A s = sigmoid(A(1.5957691216057307118) * (g + A(0.044715) * g * g * g));
         act       = g * s;

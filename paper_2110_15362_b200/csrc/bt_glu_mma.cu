@@ -815,11 +815,14 @@ uint64_t level(const uint64_t (&units)[2], uint64_t long_unit, uint64_t short_un
 // shorter (64 x 2048 x 8192: 2.2 us for 256 columns).  Parts of dx cost the store of their sums (4), a second launch and the last
 // stores (3 us), and 40 ns per 128 KB of sums that go out and in.  Each choice measured against the others: 1021 x 1024 x 2752 in 128
 // columns 23.8 us, in 256 33.4 whole and 25.9 with dx in two parts; 64 x 2048 x 8192 in 256 columns 80.6 us whole, 34.8 with dx in four.
+// Where rows do not begin on 32 bytes (wide_tiles) narrow tiles, which want more of the L2 for a product, take 1.4 times as long against
+// wide ones (4113 x 560 x 8248: 187 us in 256 columns, 260 in 128; 4096 x 576 x 8192 201 and 172).
 UnitPlan unit_plan(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, bool dx, bool weights, int sms)
 {
     const uint64_t most = static_cast<uint64_t>(sms) / 2, blocks = 2 * round_up_div(d_ff, kDepth), in_rows = round_up_div(rows, kDepth);
     const uint64_t products = dtype == BT_F32 ? 6 : 1, least_tile = dtype == BT_F32 ? 12 : 6;
     const uint64_t short_tile = in_rows * products + 1 < least_tile ? least_tile : in_rows * products + 1;
+    const bool     cross = d_in % 16 != 0 || d_ff % 16 != 0;
     UnitPlan       best{};
     double         least = 0;
     for (const uint32_t columns : {256u, 128u}) {
@@ -831,6 +834,7 @@ UnitPlan unit_plan(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, bool 
             UnitPlan p{columns, splits, static_cast<uint32_t>(each), {tiles * splits, weights ? 2 * tiles_of(grid_of(d_ff, d_in, columns)) : 0}, most, 0};
             if (p.units[0] + p.units[1] < most) p.pairs = p.units[0] + p.units[1];
             double cost = static_cast<double>(level(p.units, each * products + (splits > 1 ? 4 : 0), short_tile, p.pairs, p.common)) * block_ns(columns, p.pairs);
+            if (columns == 128 && cross) cost *= 1.4;
             if (splits > 1) cost += 3000 + static_cast<double>(p.units[0]) * 40 * (columns / 128.0);
             if (least == 0 || cost < least) least = cost, best = p;
         }
