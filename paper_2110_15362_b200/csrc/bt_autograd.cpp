@@ -485,17 +485,28 @@ PyObject *grad_items(PyObject *, PyObject *const *a, Py_ssize_t n)
     const auto release = c10::make_scope_exit([&] { PyBuffer_Release(&buffer); });
     if (buffer.len < count * static_cast<Py_ssize_t>(sizeof(bt_batch_item))) refuse(PyExc_ValueError, "grad_items: the array is too short");
     auto *const items = static_cast<bt_batch_item *>(buffer.buf);
-    for (Py_ssize_t k = 0; k < count; ++k) {
-        const Tensor g = tensor_or_none(PySequence_Fast_GET_ITEM(grads.get(), k)), y = tensor_or_none(PySequence_Fast_GET_ITEM(outs.get(), k));
-        if (!g.defined() || !y.defined()) refuse(PyExc_TypeError, "grad_items: tensors are wanted");
-        const Call c{"grad_items", k == 0 ? g : THPVariable_Unpack(PySequence_Fast_GET_ITEM(grads.get(), 0))};
-        c.same_kind({&g, &y});
+    // A step has hundreds of gradients: what they have in common is looked up once, and their tensors are borrowed.
+    const auto tensor_of = [](PyObject *o) -> const Tensor & {
+        if (!THPVariable_Check(o)) refuse(PyExc_TypeError, "grad_items: tensors are wanted");
+        return THPVariable_Unpack(o);
+    };
+    if (count != 0) {
+        const Call c{"grad_items", tensor_of(PySequence_Fast_GET_ITEM(grads.get(), 0))};
         c.code();
-        if (g.is_cuda()) c.on_current_device();
-        if (y.numel() != g.numel()) refuse(PyExc_ValueError, "grad_items: an output has another size than its gradient");
-        items[k].dense = g.data_ptr();
-        items[k].y_out = y.data_ptr();
-        items[k].n     = static_cast<uint64_t>(g.numel());
+        if (c.first.is_cuda()) c.on_current_device();
+        const auto type   = c.first.scalar_type();
+        const auto device = c.first.device();
+        const auto fits   = [&](const Tensor &t) { return t.scalar_type() == type && t.device() == device && t.is_contiguous(); };
+        for (Py_ssize_t k = 0; k < count; ++k) {
+            PyObject *const og = PySequence_Fast_GET_ITEM(grads.get(), k), *const oy = PySequence_Fast_GET_ITEM(outs.get(), k);
+            const Tensor   &g = tensor_of(og), &y = og == oy ? g : tensor_of(oy);
+            if (!fits(g) || !fits(y)) c.same_kind({&g, &y});
+            const int64_t elements = g.numel();
+            if (y.numel() != elements) refuse(PyExc_ValueError, "grad_items: an output has another size than its gradient");
+            items[k].dense = g.const_data_ptr();
+            items[k].y_out = y.mutable_data_ptr();
+            items[k].n     = static_cast<uint64_t>(elements);
+        }
     }
     Py_RETURN_NONE;
     END_HANDLE_TH_ERRORS

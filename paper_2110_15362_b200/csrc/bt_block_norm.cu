@@ -30,6 +30,7 @@ struct NormArgs {
     void       *stats;                             // backward, long rows: r, c, rf, mean(t q) of each row
     uint64_t    rows, d, gate_rows, chunk_rows;    // chunk_rows: consecutive rows of one team, at most
     uint32_t    chunks, group_chunks;              // group_chunks: chunks of one group of rows with a gate; 0: chunks go across groups
+    uint32_t    narrow;                            // lanes of a narrow row; 0: not a narrow row's call
     double      scale, eps;
 };
 
@@ -346,9 +347,19 @@ struct Columns {
             }
         }
     }
-    // partial sums, in the sums' type
+    // partial sums, in the sums' type (kVector: 16 bytes at a time, for one by one the warps' stores touch four times as many sectors:
+    // bf16 4 x 8192 backward 20.5 us)
     __device__ __forceinline__ void write_sums(Acc *row, const int j, const Pair (&v)[kP], const Extent &all) const
     {
+        if constexpr (kVector && sizeof(Acc) == 4) {
+            if (!has(j, 0, 0)) return;
+#pragma unroll
+            for (int k = 0; k < kP; k += 2) {
+                float4 *const o = reinterpret_cast<float4 *>(row + column(j, k, 0));
+                if (all.holds(o, 16)) *o = make_float4(v[k].low(), v[k].high(), v[k + 1].low(), v[k + 1].high());
+            }
+            return;
+        }
 #pragma unroll
         for (int k = 0; k < kP; ++k) {
             Acc *const lo = row + column(j, k, 0), *const hi = row + column(j, k, 1);
@@ -746,9 +757,253 @@ block_norm_bwd_ring_kernel(const NormArgs a, const uint32_t slot_bytes, const ui
 #pragma unroll
             for (int k = 0; k < kP; ++k) sum_f[j][k] = sum_f[j][k] * both(scale) * g[k];
         }
+        const Pair(&post)[kP] = kRowGate ? sum_post[kRowGate ? j : 0] : sum_f[j];
+        if (a.chunks == 1) {                                           // the sums of all rows
+            if (a.dw_pre) c.write(static_cast<Elem *>(a.dw_pre) + c.first, j, sum_pre[j], extent_of(a.dw_pre, a.d * sizeof(Elem)));
+            if (a.dw_post) c.write(static_cast<Elem *>(a.dw_post) + c.first, j, post, extent_of(a.dw_post, a.d * sizeof(Elem)));
+            continue;
+        }
         if (a.dw_pre) c.write_sums(reinterpret_cast<Acc *>(a.part_pre) + chunk * a.d + c.first, j, sum_pre[j], part_w);
-        if (a.dw_post) c.write_sums(reinterpret_cast<Acc *>(a.part_post) + chunk * a.d + c.first, j, kRowGate ? sum_post[kRowGate ? j : 0] : sum_f[j], part_p);
+        if (a.dw_post) c.write_sums(reinterpret_cast<Acc *>(a.part_post) + chunk * a.d + c.first, j, post, part_p);
     }
+}
+
+// ---------------------------------------------------------------------------------------------- narrow rows
+// Rows of whole vectors and at most 256 columns go to 8, 16 or 32 lanes of a warp, eight columns each, straight from memory to registers,
+// the next row's elements on their way while a row is worked on: no barriers, and sums of three to five exchanges
+// (bf16 16384 x 128: forward 8.7 -> 4.5 us, backward 22.7 -> 12.3; fp32 7.9 -> 5.6, 20.1 -> 14.9).  Sixteen columns a lane gain
+// nothing but for thousands of rows (bf16 16384 x 512 backward 36.8 -> 30.9 us, 100 x 360 6.8 -> 8.5), nor do rows of single
+// elements (bf16 16384 x 148 backward 35 -> 39 us): those take the ring.
+constexpr int kNarrowThreads = 256;
+constexpr int kNarrowColumns = 256;
+constexpr int kNarrowFwdCtas = 3, kNarrowBwdCtas = 2;                   // of an SM: what the registers are dealt for
+constexpr int narrow_hold(int dtype) { return dtype == BT_F32 ? 2 : 1; }  // vectors of 16 bytes with eight columns
+
+// What a lane holds of a row as it lies in memory; zeros beyond the row and for rows that are not there.
+template <int DT, int kHold>
+struct RawRow {
+    using C = Columns<DT, kHold, true>;
+    uint4 v[kHold];
+    __device__ __forceinline__ void load(const C &c, const void *base, const uint64_t row, const bool there)
+    {
+        const uint4 *const from = reinterpret_cast<const uint4 *>(static_cast<const typename C::Elem *>(base) + row * c.row_d);
+#pragma unroll
+        for (int j = 0; j < kHold; ++j) v[j] = there && c.has(j, 0, 0) ? from[j * c.team + c.t] : make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void get(const int j, typename C::Pair (&o)[C::kP]) const { widen_pairs<DT>(v[j], o); }
+};
+// the sum over a row's lanes, the same in each of them
+template <typename A>
+__device__ __forceinline__ A lanes_sum(A v, const uint32_t lanes)
+{
+#pragma unroll
+    for (uint32_t o = 16; o != 0; o /= 2)
+        if (o < lanes) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    return v;
+}
+
+// Forward.  x_out may be x and n_out f: an element is read and written by one lane, in that order.
+template <int DT, int kHold, bool kRowGate>
+__global__ void __launch_bounds__(kNarrowThreads, kNarrowFwdCtas)
+block_norm_fwd_narrow_kernel(const NormArgs a, const uint32_t lanes)
+{
+    in_stream_order();
+    using C    = Columns<DT, kHold, true>;
+    using Elem = typename C::Elem;
+    using Acc  = typename C::Acc;
+    using Pair = typename C::Pair;
+    constexpr int  kP    = C::kP;
+    const C        c{threadIdx.x % lanes, lanes, static_cast<uint32_t>(a.d), 0, a.d};
+    const uint64_t teams = kNarrowThreads / lanes, step = gridDim.x * teams, from = blockIdx.x * teams;
+    const Acc      eps = static_cast<Acc>(a.eps), of_d = Acc(1) / static_cast<Acc>(a.d);
+    const Extent   all_x = extent_of(a.x_out, a.rows * a.d * sizeof(Elem)), all_n = extent_of(a.n_out, a.rows * a.d * sizeof(Elem));
+    Pair           gw[kHold][kP], w_pre[kHold][kP];
+    branch_factors<DT, kHold, true, kRowGate>(a, 0, c, gw);
+#pragma unroll
+    for (int j = 0; j < kHold; ++j) {
+        c.fill(w_pre[j], 1);
+        if (a.w_pre) c.read(static_cast<const Elem *>(a.w_pre), j, w_pre[j]);
+    }
+    RawRow<DT, kHold> x, f, g;
+    uint64_t                   row = from + threadIdx.x / lanes;
+    const auto                 load = [&](const uint64_t r) {
+        x.load(c, a.x, r, r < a.rows);
+        f.load(c, a.f, r, a.f && r < a.rows);
+        if constexpr (kRowGate) g.load(c, a.gate, r / a.gate_rows, r < a.rows);
+    };
+    load(row);
+    // (a warp's rows together: its lanes meet in the sums)
+    for (uint64_t warp_row = from + threadIdx.x / 32 * (32 / lanes); warp_row < a.rows; warp_row += step, row += step) {
+        Pair y[kHold][kP], p[kHold][kP];
+#pragma unroll
+        for (int j = 0; j < kHold; ++j) x.get(j, y[j]), f.get(j, p[j]);
+        Pair rf = both(Acc(1));
+        if (a.w_post) {
+            Pair s = both(Acc(0));
+#pragma unroll
+            for (int j = 0; j < kHold; ++j)
+#pragma unroll
+                for (int k = 0; k < kP; ++k) s = fma2(p[j][k], p[j][k], s);
+            rf = both(root_of(lanes_sum(s.low() + s.high(), lanes) * of_d + eps));
+        }
+        Pair s = both(Acc(0));
+#pragma unroll
+        for (int j = 0; j < kHold; ++j) {
+            if constexpr (kRowGate) {
+                Pair gate[kP];
+                g.get(j, gate);
+#pragma unroll
+                for (int k = 0; k < kP; ++k) p[j][k] = p[j][k] * gate[k];
+            }
+#pragma unroll
+            for (int k = 0; k < kP; ++k) {
+                y[j][k] = fma2(p[j][k] * rf, gw[j][k], y[j][k]);
+                s       = fma2(y[j][k], y[j][k], s);
+            }
+        }
+        load(row + step);
+        const bool there = row < a.rows;
+#pragma unroll
+        for (int j = 0; j < kHold; ++j)
+            if (a.x_out && there) c.write(static_cast<Elem *>(a.x_out) + row * a.d, j, y[j], all_x);
+        if (!a.n_out) continue;
+        const Pair r = both(root_of(lanes_sum(s.low() + s.high(), lanes) * of_d + eps));
+#pragma unroll
+        for (int j = 0; j < kHold; ++j) {
+#pragma unroll
+            for (int k = 0; k < kP; ++k) y[j][k] = y[j][k] * r * w_pre[j][k];
+            if (there) c.write(static_cast<Elem *>(a.n_out) + row * a.d, j, y[j], all_n);
+        }
+    }
+}
+
+// Backward, a CTA per chunk of rows that share a gate row.  Where there is one chunk its sums are the weights' gradients.
+template <int DT, int kHold>
+__global__ void __launch_bounds__(kNarrowThreads, kNarrowBwdCtas)
+block_norm_bwd_narrow_kernel(const NormArgs a, const uint32_t lanes)
+{
+    in_stream_order();
+    using C    = Columns<DT, kHold, true>;
+    using Elem = typename C::Elem;
+    using Acc  = typename C::Acc;
+    using Pair = typename C::Pair;
+    constexpr int  kP = C::kP;
+    __shared__ Acc part[kNarrowThreads / 32][32 * kHold * kP * 2];
+    const C        c{threadIdx.x % lanes, lanes, static_cast<uint32_t>(a.d), 0, a.d};
+    const uint32_t chunk = blockIdx.x, teams = kNarrowThreads / lanes;
+    const Chunk    rows  = chunk_of(a, chunk);
+    const uint64_t group = chunk / a.group_chunks;
+    const Acc      scale = static_cast<Acc>(a.scale), eps = static_cast<Acc>(a.eps), of_d = Acc(1) / static_cast<Acc>(a.d);
+    const Extent   all_x = extent_of(a.x_out, a.rows * a.d * sizeof(Elem)), all_f = extent_of(a.n_out, a.rows * a.d * sizeof(Elem));
+    Pair           gw[kHold][kP], w_pre[kHold][kP], sum_pre[kHold][kP], sum_f[kHold][kP];
+    branch_factors<DT, kHold, true, false>(a, group, c, gw);
+#pragma unroll
+    for (int j = 0; j < kHold; ++j) {
+        c.fill(w_pre[j], 1), c.fill(sum_pre[j], 0), c.fill(sum_f[j], 0);
+        if (a.w_pre) c.read(static_cast<const Elem *>(a.w_pre), j, w_pre[j]);
+    }
+    RawRow<DT, kHold> raw_x, raw_f, raw_dn, raw_dy;
+    const auto                 load = [&](const uint64_t r) {
+        const bool there = r < rows.end;
+        raw_x.load(c, a.x, r, there), raw_f.load(c, a.f, r, there && a.f);
+        raw_dn.load(c, a.dn, r, there && a.dn), raw_dy.load(c, a.dy, r, there && a.dy);
+    };
+    uint64_t row = rows.first + threadIdx.x / lanes;
+    load(row);
+    // (a warp's rows together: its lanes meet in the sums)
+    for (uint64_t warp_row = rows.first + threadIdx.x / 32 * (32 / lanes); warp_row < rows.end; warp_row += teams, row += teams) {
+        Pair x[kHold][kP], f[kHold][kP], dn[kHold][kP], dy[kHold][kP], p[6];
+#pragma unroll
+        for (int k = 0; k < 6; ++k) p[k] = both(Acc(0));
+#pragma unroll
+        for (int j = 0; j < kHold; ++j) {
+            raw_x.get(j, x[j]), raw_f.get(j, f[j]), raw_dn.get(j, dn[j]), raw_dy.get(j, dy[j]);
+#pragma unroll
+            for (int k = 0; k < kP; ++k) {
+                const Pair wn = dn[j][k] * w_pre[j][k], q = gw[j][k] * f[j][k];
+                p[0] = fma2(x[j][k], x[j][k], p[0]);
+                p[1] = fma2(wn, x[j][k], p[1]);
+                p[2] = fma2(f[j][k], f[j][k], p[2]);
+                p[3] = fma2(dy[j][k], q, p[3]);
+                p[4] = fma2(wn, q, p[4]);
+                p[5] = fma2(x[j][k], q, p[5]);
+            }
+        }
+        load(row + teams);
+        Acc s[6];
+#pragma unroll
+        for (int k = 0; k < 6; ++k) s[k] = lanes_sum(p[k].low() + p[k].high(), lanes);
+        const RowFactors<Acc> q = factors_of(s, of_d, eps, a.w_post != nullptr);
+        const Pair r = both(q.r), rrc = both(-q.rrc), rf = both(q.rf), rf3m = both(-q.rf3m);
+        const bool there = row < rows.end;
+        if (!there) continue;                                          // (its zeros would add nothing, but for an eps of 0)
+#pragma unroll
+        for (int j = 0; j < kHold; ++j) {
+#pragma unroll
+            for (int k = 0; k < kP; ++k) {
+                const Pair tv = fma2(rrc, x[j][k], fma2(r, dn[j][k] * w_pre[j][k], dy[j][k]));
+                sum_pre[j][k] = fma2(dn[j][k], x[j][k] * r, sum_pre[j][k]);
+                sum_f[j][k]   = fma2(tv, f[j][k] * rf, sum_f[j][k]);
+                f[j][k]       = fma2(tv * gw[j][k], rf, rf3m * f[j][k]);
+                dy[j][k]      = tv;
+            }
+            if (a.x_out) c.write(static_cast<Elem *>(a.x_out) + row * a.d, j, dy[j], all_x);
+            if (a.n_out) c.write(static_cast<Elem *>(a.n_out) + row * a.d, j, f[j], all_f);
+        }
+    }
+    // The sums of all teams, column by column: over the teams of a warp, then over the warps.  put(column, sum)
+    const auto gather = [&](const Pair (&v)[kHold][kP], const auto &put) {
+#pragma unroll
+        for (int j = 0; j < kHold; ++j)
+#pragma unroll
+            for (int k = 0; k < 2 * kP; ++k) {
+                Acc s = k % 2 ? v[j][k / 2].high() : v[j][k / 2].low();
+#pragma unroll
+                for (uint32_t o = 8; o < 32; o *= 2)
+                    if (o >= lanes) s += __shfl_xor_sync(0xFFFFFFFFu, s, o);
+                if (threadIdx.x % 32 < lanes) part[threadIdx.x / 32][c.column(j, k / 2, k % 2)] = s;
+            }
+        __syncthreads();
+        for (uint32_t i = threadIdx.x; i < c.d; i += kNarrowThreads) {
+            Acc s = 0;
+#pragma unroll
+            for (int w = 0; w < kNarrowThreads / 32; ++w) s += part[w][i];
+            put(i, s);
+        }
+        __syncthreads();
+    };
+    const auto element = [](const void *base, const uint64_t i) { return base ? static_cast<Acc>(Num<DT>::widen(static_cast<const Elem *>(base)[i])) : Acc(1); };
+    const auto store   = [](void *base, const uint64_t i, const Acc v, const Extent &all) {
+        Elem *const o = static_cast<Elem *>(base) + i;
+        if (all.holds(o, sizeof(Elem))) *o = Num<DT>::narrow(v);
+    };
+    const auto store_sum = [](void *base, const uint64_t i, const Acc v, const Extent &all) {
+        Acc *const o = static_cast<Acc *>(base) + i;
+        if (all.holds(o, sizeof(Acc))) *o = v;
+    };
+    const Extent one = extent_of(a.dw_pre, a.d * sizeof(Elem)), one_p = extent_of(a.dw_post, a.d * sizeof(Elem));
+    const Extent part_w = extent_of(a.part_pre, a.chunks * a.d * sizeof(Acc)), part_p = extent_of(a.part_post, a.chunks * a.d * sizeof(Acc));
+    const Extent all_g  = extent_of(a.dgate, round_up_div(a.rows, a.gate_rows) * a.d * sizeof(Elem)), part_g = extent_of(a.part_gate, 2ull * a.chunks * a.d * sizeof(Acc));
+    if (a.dw_pre)
+        gather(sum_pre, [&](const uint32_t i, const Acc s) {
+            if (a.chunks == 1) store(a.dw_pre, i, s, one);
+            else store_sum(a.part_pre, static_cast<uint64_t>(chunk) * a.d + i, s, part_w);
+        });
+    if (!a.dw_post && !a.dgate) return;
+    uint64_t   slot;
+    const bool whole = whole_group(a, rows, group, chunk, slot), none = rows.first == rows.end;
+    gather(sum_f, [&](const uint32_t i, const Acc s) {
+        if (a.dw_post) {
+            const Acc v = s * scale * (a.gate ? element(a.gate, group * a.d + i) : Acc(1));
+            if (a.chunks == 1) store(a.dw_post, i, v, one_p);
+            else store_sum(a.part_post, static_cast<uint64_t>(chunk) * a.d + i, v, part_p);
+        }
+        if (a.dgate && !none) {
+            const Acc v = s * scale * element(a.w_post, i);
+            if (whole) store(a.dgate, group * a.d + i, v, all_g);
+            else store_sum(a.part_gate, slot * a.d + i, v, part_g);
+        }
+    });
 }
 
 // Rows that the ring kernel does not hold: dx and df by a kernel that reads a row twice and leaves its factors behind ...
@@ -962,12 +1217,27 @@ cudaError_t with_ring(const RingPlan &p, bool vector, const F &go)
     return vector ? go(More(), Yes(), No()) : go(More(), No(), No());
 }
 
+// Lanes for a narrow row; 0: the ring's.
+uint32_t narrow_lanes(uint64_t d, int es)
+{
+    if (d > kNarrowColumns || es == 8 || d % (16 / static_cast<uint64_t>(es)) != 0) return 0;
+    return d <= 64 ? 8 : d <= 128 ? 16 : 32;
+}
+
 template <int DT>
 cudaError_t forward(const NormArgs &a, cudaStream_t stream)
 {
     const int sms = sm_count();
     if (sms == 0) return cudaErrorInvalidDevice;
     const bool     vector = a.d % kLanes<DT> == 0, row_gate = a.gate && a.gate_rows < a.rows;
+    const uint32_t lanes = narrow_lanes(a.d, static_cast<int>(sizeof(typename Num<DT>::Elem)));
+    if constexpr (DT != BT_F64)
+        if (lanes) {
+            const uint64_t ctas = round_up_div(a.rows, kNarrowThreads / lanes), most = static_cast<uint64_t>(sms) * kNarrowFwdCtas;
+            const unsigned grid = static_cast<unsigned>(ctas < most ? ctas : most);
+            return row_gate ? launch(block_norm_fwd_narrow_kernel<DT, narrow_hold(DT), true>, grid, kNarrowThreads, 0, stream, a, lanes)
+                            : launch(block_norm_fwd_narrow_kernel<DT, narrow_hold(DT), false>, grid, kNarrowThreads, 0, stream, a, lanes);
+        }
     const RingPlan p      = ring_plan(a.d, static_cast<int>(sizeof(typename Num<DT>::Elem)), row_gate ? 3 : 2);
     if (p.hold == 0) {
         const uint64_t most = static_cast<uint64_t>(sms) * 4;
@@ -998,18 +1268,27 @@ cudaError_t bwd_ring(const NormArgs &a, cudaStream_t stream)
 }
 
 constexpr uint32_t kMaxChunks  = 4096;      // chunks of rows of a backward pass
+constexpr uint64_t kOneChunk   = 3;         // rows of a call that one chunk takes
 constexpr uint32_t kLongChunks = 64;        // the same for rows that the ring does not hold
 
 // The most chunks of a backward pass: as many teams as the SMs hold at a time.  (Few rows: four a chunk at least where that still
 // leaves a chunk for every SM; partial rows cost, too.)
 uint32_t chunks_of(uint64_t rows, uint64_t d, int es, int sms)
 {
+    if (rows <= kOneChunk) return 1;                                   // the second kernel would take longer
     uint64_t most = row_fits(d, es) ? resident_teams(ring_plan(d, es, 4), sms) : kLongChunks;
     if (most > kMaxChunks) most = kMaxChunks;
     const uint64_t least = most < static_cast<uint64_t>(sms) ? most : static_cast<uint64_t>(sms);
     if (most > rows / 4) most = rows / 4 > least ? rows / 4 : least;
     if (most == 0) most = 1;
     return static_cast<uint32_t>(most < rows ? most : rows);
+}
+// The same for narrow rows: CTAs of an SM's registers, a row for each of their teams.
+uint32_t narrow_chunks_of(uint64_t rows, uint32_t lanes, int sms)
+{
+    if (!lanes) return 0;
+    const uint64_t most = static_cast<uint64_t>(sms) * kNarrowBwdCtas, want = round_up_div(rows, kNarrowThreads / lanes);
+    return static_cast<uint32_t>(want < most ? want : most);
 }
 // how the rows are dealt: inside the groups of rows with a gate while every group can have a chunk
 void set_chunks(NormArgs &a, uint32_t most)
@@ -1032,8 +1311,10 @@ template <int DT>
 cudaError_t backward(const NormArgs &a, cudaStream_t stream)
 {
     constexpr int es = static_cast<int>(sizeof(typename Num<DT>::Elem));
-    cudaError_t   e;
-    if (!row_fits(a.d, es)) {
+    cudaError_t   e = cudaErrorInvalidValue;
+    if (a.narrow) {
+        if constexpr (DT != BT_F64) e = launch(block_norm_bwd_narrow_kernel<DT, narrow_hold(DT)>, a.chunks, kNarrowThreads, 0, stream, a, a.narrow);
+    } else if (!row_fits(a.d, es)) {
         const int sms = sm_count();
         if (sms == 0) return cudaErrorInvalidDevice;
         const uint64_t most = static_cast<uint64_t>(sms) * 4;
@@ -1044,7 +1325,7 @@ cudaError_t backward(const NormArgs &a, cudaStream_t stream)
     } else {
         e = bwd_ring<DT>(a, stream);
     }
-    if (e != cudaSuccess || (!a.dgate && !a.dw_pre && !a.dw_post)) return e;
+    if (e != cudaSuccess || (!a.dgate && !a.dw_pre && !a.dw_post) || (a.chunks == 1 && row_fits(a.d, es))) return e;
     const uint64_t groups = round_up_div(a.rows, a.gate_rows), borders = a.chunks - 1;
     const uint64_t shared = a.dgate ? (a.group_chunks || groups < borders ? groups : borders) : 0;
     return launch(block_norm_finish_kernel<DT>, static_cast<unsigned>(round_up_div(a.d, kFinishColumns) * (2 + shared)), kFinishColumns * kSplit, 0,
@@ -1054,7 +1335,7 @@ cudaError_t backward(const NormArgs &a, cudaStream_t stream)
 size_t round_up(size_t v) { return (v + 255) / 256 * 256; }
 
 struct Parts {
-    uint32_t chunks;                             // at most
+    uint32_t chunks, lanes, narrow_chunks;       // at most; of narrow rows
     size_t   pre, post, gate, stats, bytes;      // offsets
 };
 // the workspace of a backward pass; sms: 0 for the most that any GPU could ask for
@@ -1062,12 +1343,14 @@ Parts parts_of(uint64_t rows, uint64_t d, int es, int sms)
 {
     const size_t acc = es == 8 ? 8 : 4;
     Parts        p{};
-    p.chunks     = chunks_of(rows, d, es, sms);
-    const size_t row = d * acc;
+    p.chunks        = chunks_of(rows, d, es, sms);
+    p.lanes         = narrow_lanes(d, es);
+    p.narrow_chunks = narrow_chunks_of(rows, p.lanes, sms);
+    const size_t row = d * acc, most = p.chunks > p.narrow_chunks ? p.chunks : p.narrow_chunks;
     p.pre   = 0;
-    p.post  = round_up(p.chunks * row);
-    p.gate  = p.post + round_up(p.chunks * row);
-    p.stats = p.gate + round_up(2ull * p.chunks * row);
+    p.post  = round_up(most * row);
+    p.gate  = p.post + round_up(most * row);
+    p.stats = p.gate + round_up(2 * most * row);
     p.bytes = p.stats + (row_fits(d, es) ? 0 : round_up(rows * 4 * acc));
     return p;
 }
@@ -1162,7 +1445,9 @@ int bt_block_norm_bwd(const void *x_out, uint64_t rows, uint64_t d, uint64_t gat
         a.part_gate = reinterpret_cast<float *>(w + p.gate), a.stats = w + p.stats;
     }
     a.rows = rows, a.d = d, a.gate_rows = gate_rows;
-    bt::set_chunks(a, p.chunks);
+    // (a gate for each of many groups: the ring, whose chunks go across them)
+    a.narrow = p.lanes && (!gate || bt::round_up_div(rows, gate_rows) <= p.narrow_chunks) ? p.lanes : 0;
+    bt::set_chunks(a, a.narrow ? p.narrow_chunks : p.chunks);
     a.scale = scale, a.eps = eps;
     return bt::dispatch(dtype, [&](auto dt) { return bt::backward<decltype(dt)::value>(a, s); });
 }

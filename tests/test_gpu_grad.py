@@ -58,9 +58,9 @@ def test_clip(kind, max_norm):
 
 
 @pytest.mark.parametrize("kind", ["f32", "bf16"])
-@pytest.mark.parametrize("count", [1, 64, 65, 1024, 1025, 2500])
+@pytest.mark.parametrize("count", [1, 64, 65, 256, 257, 1024, 1025, 2500])
 def test_many_tensors(kind, count):
-    """Beyond 64 and 1024 tensors: other parameters, several launches."""
+    """Beyond 64, 256 and 1024 tensors: other parameters, several launches."""
     grads = make(kind, [(37 * k) % 1000 + (TILE[kind] if k % 100 == 0 else 0) for k in range(count)], seed=count)
     check(kind, grads, 0.25, clip(grads, 0.25))
 
