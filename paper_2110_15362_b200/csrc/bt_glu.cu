@@ -272,7 +272,7 @@ size_t workspace_of(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype, bool
 {
     if (rows == 0) return 0;
     if (backward) return 2 * slope_bytes(rows, d_in, d_ff, dtype) + glu_mma_scratch(rows, d_in, d_ff, dtype, true);
-    return glu_rows_takes(rows, d_in, dtype) ? 0 : glu_mma_scratch(rows, d_in, d_ff, dtype, false);
+    return glu_rows_takes(rows, d_in, d_ff, dtype) ? 0 : glu_mma_scratch(rows, d_in, d_ff, dtype, false);
 }
 
 }  // namespace
@@ -307,7 +307,7 @@ int bt_glu_fwd(const void *x, uint64_t rows, uint64_t d_in, uint64_t d_ff, int d
     bt::GluCall c{};
     c.x = x, c.w_gate = w_gate, c.w_up = w_up, c.h = h, c.g = g_out, c.u = u_out;
     c.rows = rows, c.d_in = d_in, c.d_ff = d_ff, c.dtype = dtype, c.act = activation, c.dev_status = dev_status;
-    if (bt::glu_rows_takes(rows, d_in, dtype)) return bt::launch_glu_rows(c, s) == cudaSuccess ? BT_OK : BT_ERR_CUDA;
+    if (bt::glu_rows_takes(rows, d_in, d_ff, dtype)) return bt::launch_glu_rows(c, s) == cudaSuccess ? BT_OK : BT_ERR_CUDA;
     c.scratch = workspace;
     if (bt::glu_mma_takes(d_in, d_ff, dtype)) {
         const uint64_t tail = bt::glu_mma_tail(c);

@@ -133,7 +133,7 @@ uint64_t    glu_mma_tail(const GluCall &c);    // rows at the end that a forward
 cudaError_t launch_glu_mma_bwd(const GluCall &c, cudaStream_t stream);
 
 // The forward pass for few rows (bt_glu_rows.cu).
-bool        glu_rows_takes(uint64_t rows, uint64_t d_in, int dtype);
+bool        glu_rows_takes(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype);
 cudaError_t launch_glu_rows(const GluCall &c, cudaStream_t stream);
 
 // calls go(std::integral_constant<int, DT>, std::integral_constant<int, ACT>) for a call's type and activation

@@ -6,7 +6,8 @@
 // elements of its row (16 bytes) as its part of two products, and the same elements of x: whole 64-byte pieces of a row per load,
 // no shuffles, no shared memory before the end.  All of a warp's loads of a turn are issued before the first is used.
 //
-// Binary32: a warp takes one row of Wg and of Wu, lanes along the summed axis, products on the CUDA cores.
+// Binary32: a warp takes one row of Wg and of Wu, lanes along the summed axis, products on the CUDA cores; from 9 rows on the
+// tensor cores, with operands split into planes of bfloat16 in registers (glu_rows_planes_kernel).
 #include <type_traits>
 
 #include "bt_glu.cuh"
@@ -167,6 +168,132 @@ glu_rows_f32_kernel(const RowsArgs p)
     }
 }
 
+// Binary32, more rows: the fragments of the 16-bit kernel from binary32 operands, each split into three planes of bfloat16 that add up to
+// it, and six of the nine products of planes, the largest in one sum and the others in another.  The tensor cores cut sums off, so a
+// warp's sums leave the registers every 256 of its elements.  The weights are read once per 32 rows of x and their planes never written, which
+// costs the tile kernel most of its time here (16 x 2048 x 8192: 119 us in tiles, 41 here; 32 rows
+// 120 and 95; 8 rows on the CUDA cores 54, 41 here).  Two steps of loads ahead: four take registers that more CTAs want (16 x 1640 x 5528 27 -> 31 us).  A CTA takes kFragments times 8 rows of Wg and of Wu,
+// for which x is read and split once.
+constexpr int kFragments = 2;
+constexpr int kStepsOfSum = 16;                                         // steps of 16 summed elements between two additions in shared memory
+struct Planes {
+    uint32_t p[3][2];                                                   // [plane][pair of elements]
+};
+__device__ __forceinline__ Planes planes_of(const uint4 v)
+{
+    const uint32_t e[4] = {v.x, v.y, v.z, v.w};
+    uint32_t       w[3][4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        w[0][k]       = e[k];
+        const float r = __uint_as_float(e[k]) - __uint_as_float(e[k] & 0xFFFF0000u);
+        w[1][k]       = __float_as_uint(r);
+        w[2][k]       = __float_as_uint(r - __uint_as_float(w[1][k] & 0xFFFF0000u));
+    }
+    Planes o;
+#pragma unroll
+    for (int s = 0; s < 3; ++s)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) o.p[s][k] = __byte_perm(w[s][2 * k], w[s][2 * k + 1], 0x7632);
+    return o;
+}
+template <int kTiles>
+constexpr size_t kPlanesShared = sizeof(float) * kWarps * kTiles * kFragments * 16 * (kColumns + 1);
+
+// kTiles: groups of 8 rows of x; blockIdx.y: its part of the rows
+template <int kAct, int kTiles>
+__global__ void __launch_bounds__(32 * kWarps)
+glu_rows_planes_kernel(const RowsArgs p)
+{
+    in_stream_order();
+    extern __shared__ float shared[];
+    float(*const sums)[kTiles][kFragments][16][kColumns + 1] = reinterpret_cast<float(*)[kTiles][kFragments][16][kColumns + 1]>(shared);
+    if (p.dev_status && blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) *p.dev_status = BT_OK;
+    const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, quad = lane / 4, part = lane % 4;
+    const uint32_t f0 = blockIdx.x * kColumns * kFragments, row0 = blockIdx.y * kTiles * 8;
+    const uint32_t vecs = p.d_in / 4, steps = (vecs + 3) / 4;          // of a row; of 16 elements
+    const uint4   *wg[kFragments], *wu[kFragments], *x[kTiles];
+#pragma unroll
+    for (int m = 0; m < kFragments; ++m) {
+        const uint32_t f = f0 + m * kColumns + quad < p.d_ff ? f0 + m * kColumns + quad : p.d_ff - 1;
+        wg[m] = static_cast<const uint4 *>(p.w_gate) + static_cast<uint64_t>(f) * vecs;
+        wu[m] = static_cast<const uint4 *>(p.w_up) + static_cast<uint64_t>(f) * vecs;
+    }
+#pragma unroll
+    for (int n = 0; n < kTiles; ++n) {
+        const uint32_t row = row0 + n * 8 + quad < p.rows ? row0 + n * 8 + quad : p.rows - 1;    // (a row beyond the last is computed and dropped)
+        x[n] = static_cast<const uint4 *>(p.x) + static_cast<uint64_t>(row) * vecs;
+    }
+    float      large[kTiles][kFragments][4] = {}, small[kTiles][kFragments][4] = {};
+    bool       first = true;
+    const auto flush = [&] {
+        // fragment: weight rows quad (of Wg) and quad + 8 (of Wu), rows of x 2 * part and 2 * part + 1
+#pragma unroll
+        for (int n = 0; n < kTiles; ++n)
+#pragma unroll
+            for (int m = 0; m < kFragments; ++m)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float &s = sums[warp][n][m][quad + e / 2 * 8][2 * part + e % 2];
+                    const float v = large[n][m][e] + small[n][m][e];
+                    s = first ? v : s + v;
+                    large[n][m][e] = small[n][m][e] = 0;
+                }
+        first = false;
+    };
+    constexpr int kLoads = 2;                                        // steps whose weights are loaded ahead
+    uint32_t      done   = 0;
+    for (uint32_t step0 = warp; step0 < steps; step0 += kWarps * kLoads) {
+        uint4 a[kLoads][kFragments], b[kLoads][kFragments];
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            const uint32_t v  = (step0 + k * kWarps) * 4 + part;
+            const bool     in = v < vecs;
+#pragma unroll
+            for (int m = 0; m < kFragments; ++m) {
+                a[k][m] = in ? load_stream(wg[m] + v) : make_uint4(0, 0, 0, 0);
+                b[k][m] = in ? load_stream(wu[m] + v) : make_uint4(0, 0, 0, 0);
+            }
+        }
+#pragma unroll
+        for (int k = 0; k < kLoads; ++k) {
+            const uint32_t v = (step0 + k * kWarps) * 4 + part;
+            uint4          c[kTiles];
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) c[n] = v < vecs ? __ldg(x[n] + v) : make_uint4(0, 0, 0, 0);
+            Planes g[kFragments], u[kFragments];
+#pragma unroll
+            for (int m = 0; m < kFragments; ++m) g[m] = planes_of(a[k][m]), u[m] = planes_of(b[k][m]);
+#pragma unroll
+            for (int n = 0; n < kTiles; ++n) {
+                const Planes q       = planes_of(c[n]);
+                const auto   product = [&](float (&d)[4], const int m, const int i, const int j) {
+                    mma16<BT_BF16>(d, g[m].p[i][0], u[m].p[i][0], g[m].p[i][1], u[m].p[i][1], q.p[j][0], q.p[j][1]);
+                };
+#pragma unroll
+                for (int m = 0; m < kFragments; ++m) {
+                    product(large[n][m], m, 0, 0);
+                    product(small[n][m], m, 2, 0), product(small[n][m], m, 0, 2), product(small[n][m], m, 1, 1);
+                    product(small[n][m], m, 1, 0), product(small[n][m], m, 0, 1);
+                }
+            }
+        }
+        done += kLoads;
+        if (done >= kStepsOfSum) flush(), done = 0;
+    }
+    if (done != 0 || first) flush();
+    __syncthreads();
+    for (uint32_t e = threadIdx.x; e < kTiles * 8 * kFragments * kColumns; e += 32 * kWarps) {
+        const uint32_t c = e % kColumns, m = e / kColumns % kFragments, row = e / (kColumns * kFragments) % 8, n = e / (kColumns * kFragments * 8);
+        const uint32_t f = f0 + m * kColumns + c;
+        if (row0 + n * 8 + row >= p.rows || f >= p.d_ff) continue;
+        float gs = 0, us = 0;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) gs += sums[w][n][m][c][row], us += sums[w][n][m][c + 8][row];
+        write_outputs<BT_F32, kAct>(p, row0 + n * 8 + row, f, gs, us);
+    }
+}
+
 template <int DT, int kTiles>
 cudaError_t start(const RowsArgs &p, int act, cudaStream_t stream)
 {
@@ -187,11 +314,31 @@ cudaError_t start_f32(const RowsArgs &p, int act, cudaStream_t stream)
     return with_act<BT_F32>(act, [&](auto, auto a) { return launch(glu_rows_f32_kernel<decltype(a)::value, kRows>, grid, 32 * kWarps, 0, stream, p); });
 }
 
+template <int kTiles>
+cudaError_t start_planes(const RowsArgs &p, int act, cudaStream_t stream)
+{
+    const dim3 grid((p.d_ff + kColumns * kFragments - 1) / (kColumns * kFragments), (p.rows + kTiles * 8 - 1) / (kTiles * 8));
+    return with_act<BT_F32>(act, [&](auto, auto a) {
+        const auto        kernel = glu_rows_planes_kernel<decltype(a)::value, kTiles>;
+        const cudaError_t e      = reported(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kPlanesShared<kTiles>)));
+        if (e != cudaSuccess) return e;
+        cudaLaunchAttribute attr;
+        attr.id                                         = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr.val.programmaticStreamSerializationAllowed = 1;
+        cudaLaunchConfig_t c{};
+        c.gridDim = grid, c.blockDim = dim3(32 * kWarps), c.dynamicSmemBytes = kPlanesShared<kTiles>, c.stream = stream, c.attrs = &attr, c.numAttrs = 1;
+        return reported(cudaLaunchKernelEx(&c, kernel, p));
+    });
+}
+
 }  // namespace
 
-bool glu_rows_takes(uint64_t rows, uint64_t d_in, int dtype)
+// Binary32: 33 to 64 rows, which read the weights twice, where their CTAs run at once (64 x 4096 x 600 66 -> 32 us, 64 x 512 x 1376 17 -> 11;
+// 64 x 2048 x 8192 in tiles 120 us, here 163).
+bool glu_rows_takes(uint64_t rows, uint64_t d_in, uint64_t d_ff, int dtype)
 {
-    return dtype == BT_F32 ? rows <= 8 && d_in % 4 == 0 : (dtype == BT_F16 || dtype == BT_BF16) && rows <= 32 && d_in % 8 == 0;
+    if (dtype == BT_F32) return d_in % 4 == 0 && (rows <= 32 || (rows <= 64 && d_ff <= static_cast<uint64_t>(kColumns * kFragments) * static_cast<uint64_t>(sm_count())));
+    return (dtype == BT_F16 || dtype == BT_BF16) && rows <= 32 && d_in % 8 == 0;
 }
 
 cudaError_t launch_glu_rows(const GluCall &c, cudaStream_t stream)
@@ -199,7 +346,8 @@ cudaError_t launch_glu_rows(const GluCall &c, cudaStream_t stream)
     const RowsArgs p{c.x, c.w_gate, c.w_up, c.h, c.g, c.u, static_cast<uint32_t>(c.rows), static_cast<uint32_t>(c.d_in), static_cast<uint32_t>(c.d_ff), c.dev_status};
     if (c.dtype == BT_BF16) return start_rows<BT_BF16>(p, c.act, stream);
     if (c.dtype == BT_F16) return start_rows<BT_F16>(p, c.act, stream);
-    return c.rows == 1 ? start_f32<1>(p, c.act, stream) : c.rows <= 2 ? start_f32<2>(p, c.act, stream) : c.rows <= 4 ? start_f32<4>(p, c.act, stream) : start_f32<8>(p, c.act, stream);
+    return c.rows == 1 ? start_f32<1>(p, c.act, stream) : c.rows <= 2 ? start_f32<2>(p, c.act, stream) : c.rows <= 4 ? start_f32<4>(p, c.act, stream) : c.rows <= 8 ? start_planes<1>(p, c.act, stream)
+           : c.rows <= 16 ? start_planes<2>(p, c.act, stream) : start_planes<4>(p, c.act, stream);
 }
 
 }  // namespace bt

@@ -165,7 +165,7 @@ def test_backward_of_each_activation_and_of_some_outputs(act, kind):
 
 
 @pytest.mark.parametrize("sign", [False, True])
-@pytest.mark.parametrize("size", [(64, 512, 128), (300, 4096, 264), (96, 11264, 72), (2056, 264, 520)])
+@pytest.mark.parametrize("size", [(64, 512, 128), (300, 4096, 264), (96, 11264, 72), (2056, 264, 520), (16, 11264, 72), (40, 4096, 264)])
 def test_binary32_keeps_its_digits(size, sign):
     """Sums of equal signs and of random ones, over every axis: the error, in norm, of a binary32 sum of 256-element pieces.
     A piece drifts by 16 additions of at most 2^-23 of it and half that on average; 16 pieces and the planes' remainder (2^-24
