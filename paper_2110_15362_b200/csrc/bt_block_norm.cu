@@ -358,13 +358,13 @@ struct Columns {
                 float4 *const o = reinterpret_cast<float4 *>(row + column(j, k, 0));
                 if (all.holds(o, 16)) *o = make_float4(v[k].low(), v[k].high(), v[k + 1].low(), v[k + 1].high());
             }
-            return;
-        }
+        } else {
 #pragma unroll
-        for (int k = 0; k < kP; ++k) {
-            Acc *const lo = row + column(j, k, 0), *const hi = row + column(j, k, 1);
-            if (has(j, k, 0) && all.holds(lo, sizeof(Acc))) *lo = v[k].low();
-            if (has(j, k, 1) && all.holds(hi, sizeof(Acc))) *hi = v[k].high();
+            for (int k = 0; k < kP; ++k) {
+                Acc *const lo = row + column(j, k, 0), *const hi = row + column(j, k, 1);
+                if (has(j, k, 0) && all.holds(lo, sizeof(Acc))) *lo = v[k].low();
+                if (has(j, k, 1) && all.holds(hi, sizeof(Acc))) *hi = v[k].high();
+            }
         }
     }
 };

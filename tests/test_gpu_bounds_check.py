@@ -129,6 +129,9 @@ def test_gated_feed_forward(checked, kind):
     for size in [(1, 72, 136), (5, 72, 136), (65, 129, 67), (257, 520, 392), (33, 64, 104)]:
         test_gpu_glu.test_forward(size, kind)
         test_gpu_glu.test_backward(size, kind)
+    if kind != "f64":
+        test_gpu_glu.test_many_tiles((520, 1000, 2728), kind)
+        test_gpu_glu.test_many_tiles((40, 512, 11264), kind)
 
 
 @pytest.mark.parametrize("kind", KINDS)
@@ -137,6 +140,7 @@ def test_block_norms(checked, kind):
         test_gpu_block_norm.test_forward(size, kind)
         test_gpu_block_norm.test_backward(size, kind)
     test_gpu_block_norm.test_gate_groups(6000, 5, 72, "bf16")
+    test_gpu_block_norm.test_gate_groups(6001, 1, 72, "f32")
     test_gpu_block_norm.test_gate_groups(6000, 3000, 33, "f32")
 
 

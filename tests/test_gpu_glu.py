@@ -154,6 +154,20 @@ def test_backward(size, kind):
     check_backward(*args, act, kind, backward(*args, act))
 
 
+@pytest.mark.parametrize("kind", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("size", [(70, 2056, 1032), (520, 1000, 2728), (2056, 520, 4104), (3001, 264, 2056), (1500, 1288, 3000), (40, 512, 11264)])
+def test_many_tiles(size, kind):
+    """More tiles than run at once, of both kinds of gradients, dealt unevenly; sums over d_ff in parts; one kind alone."""
+    args = make_backward(*size, kind, "silu", seed=9)
+    whole = backward(*args, "silu")
+    check_backward(*args, "silu", kind, whole)
+    check_backward(*args, "silu", kind, backward(*args, "silu", dw=False))
+    check_backward(*args, "silu", kind, backward(*args, "silu", dx=False))
+    assert all(torch.equal(a, b) for a, b in zip(backward(*args, "silu"), whole))
+    x, wg, wu = make(*size, kind, seed=9)
+    check_forward(x, wg, wu, "gelu", kind, forward(x, wg, wu, "gelu"))
+
+
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("kind", KINDS)
 def test_backward_of_each_activation_and_of_some_outputs(act, kind):
